@@ -425,7 +425,7 @@ def _power(e):
 def _step_exp(amax):
     """The least e in [EXP_MIN, EXP_MAX] with amax <= 127 * 2^e."""
     f, e = torch.frexp(amax)
-    return (e - 7 + (f > 127 / 128)).clamp(EXP_MIN, EXP_MAX)
+    return torch.where(amax > 0, e - 7 + (f > 127 / 128), EXP_MIN).clamp(EXP_MIN, EXP_MAX)
 
 
 def _plain_bounds(st):
