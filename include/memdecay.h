@@ -105,6 +105,10 @@ enum {
 #define MD_DEV_CORRUPT    0x8   /* a session's counters, page table or region   */
                                 /* codes are out of range; the session is      */
                                 /* skipped for the step                         */
+#define MD_DEV_BAD_BLOCK  0x20  /* md_attend_token got a list of blocks that    */
+                                /* does not ascend, names a page the session    */
+                                /* lacks or counts more entries than a row has; */
+                                /* those entries are left out                   */
 #define MD_DEV_TIMEOUT    0x10  /* a bounded wait between the workgroups of the */
                                 /* fused observation kernel ran out; the step's */
                                 /* attention mass is not valid (the session     */
@@ -512,6 +516,153 @@ md_status md_calib_accumulate(md_handle h, const float* abar, int32_t bucket_ste
 md_status md_calib_fit(const uint64_t* mass_fx, const uint64_t* count, const uint64_t* age_sum,
                        int32_t n_sessions, int32_t n_regions, int32_t n_buckets, double* lambda_hat,
                        double* log_c);
+
+/*
+ * Decode operators: what a decode engine runs around the retention step, on
+ * the same cache.  One decode step of a model of L layers is, per layer,
+ *
+ *     md_norm_rope -> [md_select_blocks ->] md_attend_token
+ *
+ * and once per step, with the queries and keys that md_norm_rope left,
+ *
+ *     md_observe_step -> md_append_values [-> md_key_bounds] -> md_select_compact
+ *
+ * They follow the conventions above: device pointers, the handle's stream, no
+ * synchronisation, no allocation (work space is the caller's), and they can
+ * be captured into a graph.  They leave the current device as it was.  None
+ * of them changes the retention state.  The values of the cache sit in a pool
+ * of the caller's,
+ *  v_pool       uint16 bf16 bits [NP][L][Hkv][P/16][d/32][4][16][2][4]: for each
+ *               (layer, KV head) of a page, blocks of 16 tokens; element
+ *               (t, e) of a (page, l, kv) tile sits at (t & ~15) * d
+ *               + (e / 32) * 512 + ((t / 4) % 4) * 128 + (e % 16) * 8
+ *               + ((e / 16) % 2) * 4 + t % 4
+ * 16-byte aligned, as large as the key pool; the quantised tier leaves it as
+ * it is (only keys become codes).
+ */
+
+/* Types of a call's arrays. */
+enum { MD_F32 = 0, MD_BF16 = 1, MD_F16 = 2 };
+
+/*
+ * md_norm_rope — the heads of fused projection rows: each query and key head
+ * x becomes x * weight / sqrt(mean(x^2) + eps) (left out where the weight is
+ * NULL), then its first rope_dims elements turn by the row's position: pair i
+ * (elements i and i + rope_dims / 2; interleaved: 2 i and 2 i + 1) by the
+ * angle position * inv_freq[i], as (a cos - b sin, b cos + a sin).  Sums and
+ * products are float32; angles are reduced in float64, so positions in the
+ * millions keep their precision; the key and value rows are rounded to bf16
+ * once, at the end.
+ */
+typedef struct md_rope_args {
+    const void* qkv;          /* [n_rows][(Hq + 2 Hkv) d]: query, key and value heads        */
+    int64_t qkv_stride;       /* elements between rows, a multiple of 8                      */
+    int32_t qkv_type;         /* MD_F32, MD_BF16 or MD_F16                                   */
+    int32_t n_rows;           /* >= 0                                                        */
+    const float* q_weight;    /* [d] or NULL: query heads are not normalised                 */
+    const float* k_weight;    /* [d] or NULL                                                 */
+    float eps;                /* >= 0                                                        */
+    int32_t rope_dims;        /* 0 .. d, a multiple of 16; 0: no rotation                    */
+    const double* inv_freq;   /* [rope_dims / 2] radians per position                        */
+    const int32_t* position;  /* [n_rows]; NULL (n_rows = S only): each session's clock,     */
+                              /* the position of the token it appends next                   */
+    int32_t interleaved;      /* 0 or 1                                                      */
+    float* q_out;             /* [n_rows][Hq d], rows q_stride elements apart (a multiple    */
+    int64_t q_stride;         /* of 4): e.g. a layer of md_observe_step's q                  */
+    uint16_t* k_out;          /* bf16 [n_rows][Hkv d], rows kv_stride apart (a multiple of   */
+    uint16_t* v_out;          /* 8): e.g. a layer of md_observe_step's new_k; v_out may be   */
+    int64_t kv_stride;        /* NULL                                                        */
+} md_rope_args;
+md_status md_norm_rope(md_handle h, const md_rope_args* a);
+
+/*
+ * md_append_values — the values of the tokens that the last md_observe_step
+ * appended: new_v bf16 bits [S][L][Hkv][d] to the slots of v_pool that the
+ * keys took.  Sessions that took no token (MD_DEV_CAPACITY, MD_DEV_CORRUPT)
+ * are left alone.  MD_E_STATE unless the last md_observe_step had keys and no
+ * compaction has followed; MD_E_UNSUPPORTED with an offload tier (its pages
+ * come and go without values).
+ */
+md_status md_append_values(md_handle h, const uint16_t* new_v, uint16_t* v_pool);
+
+/*
+ * md_attend_token — attention of one new token of every session in one layer:
+ *   out_h = sum_i softmax_i(q_h . k_i / sqrt(d)) v_i,  lse_h = ln sum_i exp(q_h . k_i / sqrt(d))
+ * over the session's cached tokens (every page, or the listed ones) and, with
+ * new_k and new_v, the token itself, whose key md_observe_step appends later.
+ * Query head h reads KV head h / (Hq / Hkv).  Logits, statistics and sums are
+ * float32 or exact (queries as three bf16 terms); softmax weights enter the
+ * products with the values as two bf16 terms (relative error 2^-17).  A
+ * session without any token gets zeros and lse = -infinity.  Handles of every
+ * page size, layout and of the quantised tier; MD_E_UNSUPPORTED with an
+ * offload tier.
+ */
+typedef struct md_attend_args {
+    const float* q;           /* [S][Hq d], sessions q_stride elements apart (a multiple of  */
+    int64_t q_stride;         /* 4): e.g. a layer of md_observe_step's q                     */
+    const uint16_t* new_k;    /* bf16 [S][Hkv d], sessions kv_stride elements apart (a       */
+    const uint16_t* new_v;    /* multiple of 8); both or neither NULL                        */
+    int64_t kv_stride;
+    const uint16_t* v_pool;
+    const int32_t* blocks;    /* NULL, or [S][Hkv][max_blocks]: the first block_count[s][kv] */
+    const int32_t* block_count; /* entries of a row are logical pages, strictly ascending    */
+    int32_t max_blocks;       /* >= 1 with blocks                                            */
+    int32_t out_type;         /* MD_F32 or MD_BF16                                           */
+    void* out;                /* [S][Hq d], sessions out_stride elements apart (a multiple   */
+    int64_t out_stride;       /* of 8)                                                       */
+    float* lse;               /* [S][Hq] or NULL                                             */
+    void* workspace;          /* md_decode_workspace's attend_bytes, 16-byte aligned, zeroed */
+                              /* once by the caller; calls that may run at the same time     */
+                              /* (graphs on several streams) need one each                   */
+} md_attend_args;
+md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a);
+
+/*
+ * md_key_bounds — elementwise bounds of each page's keys, for md_select_blocks:
+ * for every (layer, KV head) of a page, the whole multiples lo <= k <= hi, in
+ * units of 2^e, of its tokens' keys: e the least exponent in [-100, 100] with
+ * max |k| <= 127 2^e, lo = floor(min k / 2^e), hi = ceil(max k / 2^e) (no
+ * more than 127 in magnitude, which only keys beyond 127 2^100 reach).  A NaN
+ * counts as an infinity of its sign.
+ * bounds:    int8 [NP][L][Hkv][2][d], lo then hi; 16-byte aligned.
+ * bound_exp: int8 [NP][L][Hkv], the exponents e.
+ * all_pages: 1 for every page of every session (after the prompts are
+ *   loaded, or when pages have turned into codes), 0 for each session's last
+ *   page (after md_observe_step, the page that took the token).
+ * The keys of a page that holds 8-bit codes are the float32 products of scale
+ * and code.  MD_E_UNSUPPORTED with an offload tier.
+ */
+md_status md_key_bounds(md_handle h, int32_t all_pages, int8_t* bounds, int8_t* bound_exp);
+
+/*
+ * md_select_blocks — the pages of a session that one layer's query attends
+ * to, per KV head: the first `first` pages, the last `last` ones, and of the
+ * others the best by score up to max_blocks in all (every page of a session
+ * with no more than that).  A page's score is the largest, over the query
+ * heads of the KV head's group, of
+ *   2^(e + f_h) sum_j (c_hj > 0 ? c_hj hi_j : c_hj lo_j),
+ * c_hj = round-to-even(q_hj / 2^f_h), f_h the least exponent in [-100, 100]
+ * with max |q_h| <= 127 2^f_h: an upper bound of the page's logits but for the
+ * query's rounding.  Scores are whole numbers times powers of two, exact in
+ * float32 (unless e + f_h leaves its range), so no order of adding can change
+ * a choice; equal scores go to the older page.  A NaN in a query counts as 0.
+ */
+typedef struct md_select_args {
+    const float* q;           /* as in md_attend_args                                        */
+    int64_t q_stride;
+    const int8_t* bounds;     /* md_key_bounds' */
+    const int8_t* bound_exp;
+    int32_t first, last;      /* >= 0, first + last <= max_blocks                            */
+    int32_t max_blocks;       /* >= 1                                                        */
+    int32_t* blocks;          /* [S][Hkv][max_blocks]: the pages, ascending, then -1         */
+    int32_t* block_count;     /* [S][Hkv]                                                    */
+    void* workspace;          /* md_decode_workspace's select_bytes; as in md_attend_args    */
+} md_select_args;
+md_status md_select_blocks(md_handle h, int32_t layer, const md_select_args* a);
+
+/* Bytes of the work space of md_attend_token and of md_select_blocks for this
+ * handle.  Host-only, no device work. */
+md_status md_decode_workspace(md_handle h, uint64_t* attend_bytes, uint64_t* select_bytes);
 
 /* Release the scratch and the handle (synchronises the stream first). */
 md_status md_destroy(md_handle h);

@@ -26,6 +26,9 @@ MD_DEV_NONFINITE = 0x2
 MD_DEV_BAD_EVICT = 0x4
 MD_DEV_CORRUPT = 0x8
 MD_DEV_TIMEOUT = 0x10
+MD_DEV_BAD_BLOCK = 0x20
+
+MD_F32, MD_BF16, MD_F16 = range(3)   # types of a call's arrays
 
 MD_FLAG_NO_FUSED = 0x1
 MD_FLAG_FUSED = 0x2
@@ -39,7 +42,8 @@ EXPORTS = ("md_abi_version", "md_status_str", "md_init", "md_init_static", "md_o
            "md_score_pages", "md_select_evict", "md_compact", "md_select_compact", "md_read_device_status",
            "md_profile_enable", "md_profile_read", "md_read_counters", "md_kernel_config", "md_observe_path",
            "md_calib_accumulate", "md_calib_fit",
-           "md_destroy")
+           "md_norm_rope", "md_append_values", "md_attend_token", "md_key_bounds", "md_select_blocks",
+           "md_decode_workspace", "md_destroy")
 
 # paths of md_observe_path
 PATHS = ("multi-kernel", "fused", "session")
@@ -73,6 +77,30 @@ class md_cache_view(ctypes.Structure):
         "n_pages", "n_tokens", "clock", "next_serial", "budget", "free_list", "free_count", "n_live",
         "page_format", "host_keys", "off_count", "off_serial", "off_slot", "off_region", "off_t_ins",
         "off_t_ref", "off_importance", "off_format", "off_score", "off_abar")]
+
+
+class md_rope_args(ctypes.Structure):
+    _fields_ = [("qkv", ctypes.c_void_p), ("qkv_stride", ctypes.c_int64), ("qkv_type", ctypes.c_int32),
+                ("n_rows", ctypes.c_int32), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("rope_dims", ctypes.c_int32), ("inv_freq", ctypes.c_void_p),
+                ("position", ctypes.c_void_p), ("interleaved", ctypes.c_int32), ("q_out", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
+                ("kv_stride", ctypes.c_int64)]
+
+
+class md_attend_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("new_k", ctypes.c_void_p),
+                ("new_v", ctypes.c_void_p), ("kv_stride", ctypes.c_int64), ("v_pool", ctypes.c_void_p),
+                ("blocks", ctypes.c_void_p), ("block_count", ctypes.c_void_p), ("max_blocks", ctypes.c_int32),
+                ("out_type", ctypes.c_int32), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p)]
+
+
+class md_select_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("bounds", ctypes.c_void_p),
+                ("bound_exp", ctypes.c_void_p), ("first", ctypes.c_int32), ("last", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("blocks", ctypes.c_void_p), ("block_count", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p)]
 
 
 class MemDecayError(RuntimeError):
@@ -155,6 +183,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.md_kernel_config.argtypes = [vp, ctypes.POINTER(i32)]
     lib.md_observe_path.restype = i32
     lib.md_observe_path.argtypes = [vp, ctypes.POINTER(i32)]
+    lib.md_norm_rope.restype = i32
+    lib.md_norm_rope.argtypes = [vp, ctypes.POINTER(md_rope_args)]
+    lib.md_append_values.restype = i32
+    lib.md_append_values.argtypes = [vp, vp, vp]
+    lib.md_attend_token.restype = i32
+    lib.md_attend_token.argtypes = [vp, i32, ctypes.POINTER(md_attend_args)]
+    lib.md_key_bounds.restype = i32
+    lib.md_key_bounds.argtypes = [vp, i32, vp, vp]
+    lib.md_select_blocks.restype = i32
+    lib.md_select_blocks.argtypes = [vp, i32, ctypes.POINTER(md_select_args)]
+    lib.md_decode_workspace.restype = i32
+    lib.md_decode_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
     lib.md_destroy.restype = i32
     lib.md_destroy.argtypes = [vp]
     _lib = lib
@@ -293,6 +333,33 @@ def md_observe_path(h: int) -> dict:
     _check("md_observe_path", load_library().md_observe_path(h, out))
     return {"first": PATHS[out[0]], "steady": PATHS[out[1]], "first_ranges": int(out[2]),
             "steady_ranges": int(out[3])}
+
+
+def md_norm_rope(h: int, args: md_rope_args) -> int:
+    return _check("md_norm_rope", load_library().md_norm_rope(h, ctypes.byref(args)))
+
+
+def md_append_values(h: int, new_v: int, v_pool: int) -> int:
+    return _check("md_append_values", load_library().md_append_values(h, new_v, v_pool))
+
+
+def md_attend_token(h: int, layer: int, args: md_attend_args) -> int:
+    return _check("md_attend_token", load_library().md_attend_token(h, layer, ctypes.byref(args)))
+
+
+def md_key_bounds(h: int, all_pages: int, bounds: int, bound_exp: int) -> int:
+    return _check("md_key_bounds", load_library().md_key_bounds(h, all_pages, bounds, bound_exp))
+
+
+def md_select_blocks(h: int, layer: int, args: md_select_args) -> int:
+    return _check("md_select_blocks", load_library().md_select_blocks(h, layer, ctypes.byref(args)))
+
+
+def md_decode_workspace(h: int):
+    """Bytes of the work space of (md_attend_token, md_select_blocks)."""
+    out = (ctypes.c_uint64(0), ctypes.c_uint64(0))
+    _check("md_decode_workspace", load_library().md_decode_workspace(h, ctypes.byref(out[0]), ctypes.byref(out[1])))
+    return int(out[0].value), int(out[1].value)
 
 
 def md_destroy(h: int) -> int:

@@ -24,7 +24,10 @@ class PagedCache:
     """Device buffers of one batch of sessions (layouts as in memdecay.h)."""
 
     def __init__(self, *, L: int, Hq: int, Hkv: int, d: int, P: int, S: int,
-                 max_pages: int, n_phys: int, device="cuda", offload_pages: int = 0):
+                 max_pages: int, n_phys: int, device="cuda", offload_pages: int = 0, values: bool = False,
+                 bounds: bool = False):
+        # values: a pool of values beside the keys (MemDecay.attend);
+        # bounds: 8-bit bounds of each page's keys (MemDecay.select_blocks)
         self.L, self.Hq, self.Hkv, self.d, self.P = L, Hq, Hkv, d, P
         self.S, self.max_pages, self.n_phys = S, max_pages, n_phys
         self.device = torch.device(device)
@@ -48,6 +51,12 @@ class PagedCache:
         self.budget = torch.zeros(S, **i32)
         self.free_list = torch.zeros(n_phys, **i32)
         self.free_count = torch.zeros(1, **i32)
+        # pages past a session's table are never read, so the pools are left
+        # uninitialised
+        self.v_pool = torch.empty((n_phys, L, Hkv, P // 16, d // 32, 4, 16, 2, 4), dtype=torch.bfloat16,
+                                  device=dev) if values else None
+        self.key_bounds = torch.empty((n_phys, L, Hkv, 2, d), dtype=torch.int8, device=dev) if bounds else None
+        self.bound_exp = torch.empty((n_phys, L, Hkv), dtype=torch.int8, device=dev) if bounds else None
         # offload tier: offload_pages host-memory pages per session, their
         # keys in pinned host memory (hipHostMalloc underneath), their
         # per-token state on the device
@@ -92,6 +101,19 @@ class PagedCache:
         itself) -> keys [m][P][L][Hkv][d]."""
         m, L, Hkv, nb, db = pages.shape[:5]
         return pages.permute(0, 3, 5, 1, 2, 4, 6).reshape(m, nb * 16, L, Hkv, db * 8)
+
+    @staticmethod
+    def to_value_layout(v: torch.Tensor) -> torch.Tensor:
+        """Values [m][P][L][Hkv][d] of m pages -> the value pool's page layout
+        [m][L][Hkv][P/16][d/32][4][16][2][4] (memdecay.h)."""
+        m, P, L, Hkv, d = v.shape
+        return v.view(m, P // 16, 4, 4, L, Hkv, d // 32, 2, 16).permute(0, 4, 5, 1, 6, 2, 8, 7, 3).contiguous()
+
+    @staticmethod
+    def from_value_layout(pages: torch.Tensor) -> torch.Tensor:
+        """The inverse: value pool pages -> values [m][P][L][Hkv][d]."""
+        m, L, Hkv, nb, db = pages.shape[:5]
+        return pages.permute(0, 3, 5, 8, 1, 2, 4, 7, 6).reshape(m, nb * 16, L, Hkv, db * 32)
 
     @staticmethod
     def positions(region, P: int, region_aligned: bool) -> np.ndarray:
@@ -164,6 +186,20 @@ class PagedCache:
         self.next_serial[s] = m
         self.budget[s] = budget
 
+    def load_values(self, s: int, values: torch.Tensor, region=None):
+        """Place the values bf16 [n][L][Hkv][d] of a session's prompt next to
+        the keys that ``load_session`` placed; region: the same codes, with
+        region-aligned pages only."""
+        n, P = int(values.shape[0]), self.P
+        if n == 0:
+            return
+        pos = self.positions(np.zeros(n) if region is None else region, P, region is not None)
+        m = int(pos[-1]) // P + 1
+        full = torch.zeros((m * P,) + tuple(values.shape[1:]), dtype=torch.bfloat16, device=self.device)
+        full[torch.as_tensor(pos, device=self.device)] = values.to(self.device, torch.bfloat16)
+        ids = self.page_table[s, :m].long()
+        self.v_pool.index_copy_(0, ids, self.to_value_layout(full.view(m, P, self.L, self.Hkv, self.d)))
+
     def set_free_pages(self, ids: Sequence[int]):
         """The free list: ids pop from the end."""
         ids = np.ascontiguousarray(ids, dtype=np.int32)
@@ -215,6 +251,32 @@ class MemDecay:
         self.evict_count = torch.zeros(S, dtype=torch.int32, device=dev)
         self.infeasible = torch.zeros(S, dtype=torch.uint8, device=dev)
 
+        # work space of the decode operators (one per handle: calls on its
+        # stream run one after another)
+        self._attend_ws = self._select_ws = None
+        if cache.v_pool is not None:   # now, so that a captured call allocates nothing
+            self._workspace(True)
+        if cache.key_bounds is not None:
+            self._workspace(False)
+
+    def _here(self, *tensors):
+        dev = self.cache.k_pool.device
+        for t in tensors:
+            if t is not None and t.device != dev:
+                raise ValueError(f"expected a tensor on {dev}, got one on {t.device}")
+
+    def _workspace(self, attend: bool) -> torch.Tensor:
+        ws = self._attend_ws if attend else self._select_ws
+        if ws is None:
+            n = B.md_decode_workspace(self.handle)[0 if attend else 1]
+            with torch.cuda.stream(self.stream):
+                ws = torch.zeros(max(n, 16), dtype=torch.uint8, device=self.cache.device)
+            if attend:
+                self._attend_ws = ws
+            else:
+                self._select_ws = ws
+        return ws
+
     # ---- the four calls of one step
     def observe(self, step: int, q: torch.Tensor, new_k: Optional[torch.Tensor] = None,
                 new_region: Optional[torch.Tensor] = None, abar_out: Optional[torch.Tensor] = None):
@@ -254,6 +316,123 @@ class MemDecay:
             return
         self.score(page_score=page_scores)
         self.select_compact()
+
+    # ---- what a decode engine runs around the step (memdecay.h)
+    def norm_rope(self, qkv: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor,
+                  v_out: Optional[torch.Tensor] = None, *, q_weight: Optional[torch.Tensor] = None,
+                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  inv_freq: Optional[torch.Tensor] = None, position: Optional[torch.Tensor] = None,
+                  interleaved: bool = False):
+        """Norms of the query and key heads and their rotation by position.
+
+        qkv [n][(Hq + 2 Hkv) d] float32, bfloat16 or float16 rows; q_out
+        float32 [n][Hq][d]; k_out, v_out bfloat16 [n][Hkv][d].  Rows may be
+        any distance apart (a layer of the step's q and new_k buffers).
+        q_weight, k_weight [d]: None leaves those heads as they are.
+        inv_freq float64 [r / 2]: the first r elements of each head turn (None:
+        none).  position int32 [n]; None: each session's clock (n = S)."""
+        c = self.cache
+        self._here(qkv, q_out, k_out, v_out, q_weight, k_weight, inv_freq, position)
+        n = qkv.shape[0]
+        half = 0 if inv_freq is None else inv_freq.numel()
+        if qkv.dim() != 2 or qkv.shape[1] != (c.Hq + 2 * c.Hkv) * c.d:
+            raise ValueError("qkv holds the query, key and value heads of a row side by side")
+        if (v_out is not None and _stride(v_out, torch.bfloat16, n, c.Hkv, c.d) !=
+                _stride(k_out, torch.bfloat16, n, c.Hkv, c.d)):
+            raise ValueError("k_out and v_out have rows the same distance apart")
+        if position is not None and position.numel() != n:
+            raise ValueError("one position per row")
+        for w in (q_weight, k_weight):
+            if w is not None and w.numel() != c.d:
+                raise ValueError("one weight per element of a head")
+        if n == 0:
+            return
+        B.md_norm_rope(self.handle, B.md_rope_args(
+            qkv=_rows(qkv), qkv_stride=_pitch(qkv), qkv_type=_type(qkv), n_rows=n,
+            q_weight=None if q_weight is None else _ptr(q_weight, torch.float32),
+            k_weight=None if k_weight is None else _ptr(k_weight, torch.float32), eps=eps, rope_dims=2 * half,
+            inv_freq=None if half == 0 else _ptr(inv_freq, torch.float64),
+            position=None if position is None else _ptr(position, torch.int32), interleaved=int(interleaved),
+            q_out=q_out.data_ptr(), q_stride=_stride(q_out, torch.float32, n, c.Hq, c.d), k_out=k_out.data_ptr(),
+            v_out=None if v_out is None else v_out.data_ptr(),
+            kv_stride=_stride(k_out, torch.bfloat16, n, c.Hkv, c.d)))
+
+    def append_values(self, new_v: torch.Tensor):
+        """The values bf16 [S][L][Hkv][d] of the tokens that the last observe
+        appended (before anything is compacted)."""
+        c = self.cache
+        self._here(new_v, c.v_pool)
+        if new_v.numel() != c.S * c.L * c.Hkv * c.d:
+            raise ValueError("new_v holds [S][L][Hkv][d]")
+        B.md_append_values(self.handle, _ptr(new_v, torch.bfloat16), self._values())
+
+    def _values(self) -> int:
+        if self.cache.v_pool is None:
+            raise ValueError("the cache has no values (PagedCache(values=True))")
+        return _ptr(self.cache.v_pool, torch.bfloat16)
+
+    def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, *, new_k: Optional[torch.Tensor] = None,
+               new_v: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+               blocks: Optional[torch.Tensor] = None, block_count: Optional[torch.Tensor] = None):
+        """Attention of one token of every session in one layer over its
+        cached tokens (or the listed pages) and, with new_k and new_v bf16
+        [S][Hkv][d], itself.  q float32 and out (float32 or bfloat16)
+        [S][Hq][d], lse float32 [S][Hq]; sessions of q, out and of the new
+        keys and values may be any distance apart."""
+        c = self.cache
+        self._here(q, out, new_k, new_v, lse, blocks, block_count, c.v_pool)
+        kv = 0
+        if new_k is not None and new_v is not None:
+            kv = _stride(new_k, torch.bfloat16, c.S, c.Hkv, c.d)
+            if _stride(new_v, torch.bfloat16, c.S, c.Hkv, c.d) != kv:
+                raise ValueError("new_k and new_v have sessions the same distance apart")
+        if out.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"expected float32 or bfloat16 outputs, got {out.dtype}")
+        if lse is not None and lse.numel() != c.S * c.Hq:
+            raise ValueError("lse holds [S][Hq]")
+        most = 0
+        if blocks is not None:
+            most = self._lists(blocks, block_count)
+        B.md_attend_token(self.handle, layer, B.md_attend_args(
+            q=q.data_ptr(), q_stride=_stride(q, torch.float32, c.S, c.Hq, c.d),
+            new_k=None if new_k is None else new_k.data_ptr(), new_v=None if new_v is None else new_v.data_ptr(),
+            kv_stride=kv, v_pool=self._values(), blocks=None if blocks is None else _ptr(blocks, torch.int32),
+            block_count=None if blocks is None else _ptr(block_count, torch.int32), max_blocks=most, out_type=_type(out),
+            out=out.data_ptr(), out_stride=_stride(out, out.dtype, c.S, c.Hq, c.d),
+            lse=None if lse is None else _ptr(lse, torch.float32), workspace=self._workspace(True).data_ptr()))
+
+    def _lists(self, blocks: torch.Tensor, count: torch.Tensor) -> int:
+        c = self.cache
+        if blocks.dim() != 3 or tuple(blocks.shape[:2]) != (c.S, c.Hkv) or count is None or \
+                count.numel() != c.S * c.Hkv:
+            raise ValueError("blocks hold [S][Hkv][max_blocks], their counts [S][Hkv]")
+        return blocks.shape[2]
+
+    def _bounds(self):
+        c = self.cache
+        self._here(c.key_bounds, c.bound_exp)
+        if c.key_bounds is None or c.bound_exp is None:
+            raise ValueError("the cache has no bounds (PagedCache(bounds=True))")
+        return _ptr(c.key_bounds, torch.int8), _ptr(c.bound_exp, torch.int8)
+
+    def update_bounds(self, all_pages: bool = False):
+        """Bounds of the keys of each session's last page (after an append),
+        or of every page (after the prompts are loaded)."""
+        B.md_key_bounds(self.handle, int(all_pages), *self._bounds())
+
+    def select_blocks(self, layer: int, q: torch.Tensor, blocks: torch.Tensor, block_count: torch.Tensor, *,
+                      first: int = 1, last: int = 1):
+        """The pages each session's query q float32 [S][Hq][d] attends to in
+        one layer: blocks int32 [S][Hkv][max_blocks], block_count int32
+        [S][Hkv]; always the ``first`` and ``last`` pages of the session."""
+        c = self.cache
+        self._here(q, blocks, block_count)
+        most = self._lists(blocks, block_count)
+        bounds, exp = self._bounds()
+        B.md_select_blocks(self.handle, layer, B.md_select_args(
+            q=q.data_ptr(), q_stride=_stride(q, torch.float32, c.S, c.Hq, c.d), bounds=bounds, bound_exp=exp,
+            first=first, last=last, max_blocks=most, blocks=_ptr(blocks, torch.int32),
+            block_count=_ptr(block_count, torch.int32), workspace=self._workspace(False).data_ptr()))
 
     def calib_accumulate(self, abar: torch.Tensor, bucket_steps: int, stats) -> None:
         """Add this observation to stats = (mass_fx, count, age_sum), int64
@@ -300,3 +479,31 @@ def _ptr(t: torch.Tensor, dtype) -> int:
     if t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"expected a contiguous {dtype} tensor, got {t.dtype}")
     return t.data_ptr()
+
+
+TYPES = {torch.float32: B.MD_F32, torch.bfloat16: B.MD_BF16, torch.float16: B.MD_F16}
+
+
+def _type(t: torch.Tensor) -> int:
+    if t.dtype not in TYPES:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}")
+    return TYPES[t.dtype]
+
+
+def _pitch(t: torch.Tensor) -> int:
+    """Elements between the rows of t (its first axis; one row has no next)."""
+    return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
+
+
+def _rows(t: torch.Tensor) -> int:
+    if t.shape[0] and not t[0].is_contiguous():
+        raise ValueError("expected contiguous rows")
+    return t.data_ptr()
+
+
+def _stride(t: torch.Tensor, dtype, n: int, heads: int, d: int) -> int:
+    """Elements between the n rows [heads][d] of t."""
+    if t.dtype != dtype or t.shape[0] != n or t.numel() != n * heads * d:
+        raise ValueError(f"expected {dtype} [{n}][{heads}][{d}], got {t.dtype} {tuple(t.shape)}")
+    _rows(t)
+    return _pitch(t)

@@ -12,6 +12,7 @@
 #include <new>
 #include <vector>
 
+#include "md_decode.h"
 #include "md_internal.h"
 
 namespace {
@@ -50,6 +51,8 @@ struct md_handle_s {
     int64_t appended;    // appends enqueued (md_observe_step calls with keys)
     int64_t observed;    // observes enqueued
     bool compacted;      // a compaction was enqueued
+    bool fresh;          // the last step's tokens are where it appended them
+    int n_cu;
     Phase phase;
     const int32_t* sel_serial;   // md_select_evict's lists since the last observe
     const int32_t* sel_count;    // (NULL: no selection yet)
@@ -642,6 +645,8 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
     h->appended = 0;
     h->observed = 0;
     h->compacted = false;
+    h->fresh = false;
+    h->n_cu = n_cu;
     h->word_tag = 0;
     h->phase = kNone;
     h->sel_serial = nullptr;
@@ -679,6 +684,7 @@ md_status md_observe_step(md_handle h, int32_t step, const float* q, const uint1
         h->last_step = step;
         h->phase = kNone;
         h->appended += new_k != nullptr;
+        h->fresh = new_k != nullptr;
         h->sel_serial = h->sel_count = nullptr;
         return MD_OK;
     }
@@ -691,6 +697,7 @@ md_status md_observe_step(md_handle h, int32_t step, const float* q, const uint1
         if (e != hipSuccess) return MD_E_HIP;
         h->observed += 1;
         h->appended += new_k != nullptr;
+        h->fresh = new_k != nullptr;
         h->have_step = true;
         h->last_step = step;
         h->phase = kObserved;
@@ -724,6 +731,7 @@ md_status md_observe_step(md_handle h, int32_t step, const float* q, const uint1
     if (e != hipSuccess) return MD_E_HIP;
     h->observed += 1;
     h->appended += new_k != nullptr;
+    h->fresh = new_k != nullptr;
     h->have_step = true;
     h->last_step = step;
     h->phase = kObserved;
@@ -790,6 +798,7 @@ md_status md_compact(md_handle h, const int32_t* evict_serial, const int32_t* ev
         return MD_E_HIP;
     h->phase = kCompacted;
     h->compacted = true;
+    h->fresh = false;
     h->sel_serial = h->sel_count = nullptr;
     return MD_OK;
 }
@@ -811,6 +820,7 @@ md_status md_select_compact(md_handle h, int32_t* evict_serial, int32_t* evict_c
         return MD_E_HIP;
     h->phase = kCompacted;
     h->compacted = true;
+    h->fresh = false;
     h->sel_serial = h->sel_count = nullptr;
     return MD_OK;
 }
@@ -949,6 +959,123 @@ md_status md_observe_path(md_handle h, int32_t* out) {
     out[1] = path(steady, h->fused_steady);
     out[2] = first > 0 ? first : h->rg_first;
     out[3] = steady > 0 ? steady : h->rg_steady;
+    return MD_OK;
+}
+
+// Makes the handle's device current for one call.
+struct OnDevice {
+    int before = -1;
+    bool ok;
+    explicit OnDevice(int device) {
+        ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess);
+        if (before == device) before = -1;
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+md_status md_norm_rope(md_handle h, const md_rope_args* a) {
+    if (h == nullptr || a == nullptr) return MD_E_INVALID;
+    const int64_t hq = (int64_t)h->dm.Hq * md::kHeadDim, hkv = (int64_t)h->dm.Hkv * md::kHeadDim;
+    if (a->n_rows < 0 || a->qkv_type < MD_F32 || a->qkv_type > MD_F16 || !(a->eps >= 0.0f) || !isfinite(a->eps))
+        return MD_E_INVALID;
+    if (a->rope_dims < 0 || a->rope_dims > md::kHeadDim || a->rope_dims % 16 != 0) return MD_E_INVALID;
+    if ((a->interleaved & ~1) != 0) return MD_E_INVALID;
+    if (a->qkv == nullptr || !aligned(a->qkv, 16) || a->q_out == nullptr || !aligned(a->q_out, 16) ||
+        a->k_out == nullptr || !aligned(a->k_out, 16) || !aligned(a->v_out, 16))
+        return MD_E_INVALID;
+    if (!aligned(a->q_weight, 4) || !aligned(a->k_weight, 4) || !aligned(a->position, 4)) return MD_E_INVALID;
+    if (a->rope_dims > 0 && (a->inv_freq == nullptr || !aligned(a->inv_freq, 8))) return MD_E_INVALID;
+    if (a->position == nullptr && a->n_rows != h->dm.S) return MD_E_INVALID;
+    if (a->qkv_stride < hq + (a->v_out != nullptr ? 2 : 1) * hkv || a->qkv_stride % 8 != 0 || a->q_stride < hq ||
+        a->q_stride % 4 != 0 || a->kv_stride < hkv || a->kv_stride % 8 != 0)
+        return MD_E_INVALID;
+    if (a->n_rows == 0) return MD_OK;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_norm_rope(h->dm, h->v, *a, h->n_cu, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_append_values(md_handle h, const uint16_t* new_v, uint16_t* v_pool) {
+    if (h == nullptr || new_v == nullptr || v_pool == nullptr || !aligned(new_v, 16) || !aligned(v_pool, 16))
+        return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    if (!h->fresh) return MD_E_STATE;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_append_values(h->dm, h->v, new_v, v_pool, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a) {
+    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L) return MD_E_INVALID;
+    const int64_t hq = (int64_t)h->dm.Hq * md::kHeadDim, hkv = (int64_t)h->dm.Hkv * md::kHeadDim;
+    if (a->q == nullptr || !aligned(a->q, 16) || a->q_stride < hq || a->q_stride % 4 != 0) return MD_E_INVALID;
+    if ((a->new_k == nullptr) != (a->new_v == nullptr)) return MD_E_INVALID;
+    if (a->new_k != nullptr && (!aligned(a->new_k, 16) || !aligned(a->new_v, 16) || a->kv_stride < hkv ||
+                                a->kv_stride % 8 != 0))
+        return MD_E_INVALID;
+    if (a->v_pool == nullptr || !aligned(a->v_pool, 16)) return MD_E_INVALID;
+    if (a->blocks != nullptr && (a->block_count == nullptr || !aligned(a->blocks, 4) || !aligned(a->block_count, 4) ||
+                                 a->max_blocks < 1 || a->max_blocks > md::kMaxPages))
+        return MD_E_INVALID;
+    if (a->out == nullptr || !aligned(a->out, 16) || a->out_stride < hq || a->out_stride % 8 != 0 ||
+        (a->out_type != MD_F32 && a->out_type != MD_BF16) || !aligned(a->lse, 4))
+        return MD_E_INVALID;
+    if (a->workspace == nullptr || !aligned(a->workspace, 16)) return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    md::TokenCall c{};
+    c.q = a->q;
+    c.q_stride = a->q_stride;
+    c.new_k = a->new_k;
+    c.new_v = a->new_v;
+    c.kv_stride = a->kv_stride;
+    c.v_pool = a->v_pool;
+    c.blocks = a->blocks;
+    c.block_count = a->block_count;
+    c.max_blocks = a->max_blocks;
+    c.out_bf16 = a->out_type == MD_BF16;
+    c.out = a->out;
+    c.out_stride = a->out_stride;
+    c.lse = a->lse;
+    c.layer = layer;
+    c.splits = md::attend_splits(h->dm, h->n_cu);
+    c.part = static_cast<float*>(a->workspace);
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_token(h->dm, h->v, h->sc, c, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_key_bounds(md_handle h, int32_t all_pages, int8_t* bounds, int8_t* bound_exp) {
+    if (h == nullptr || (all_pages & ~1) != 0 || bounds == nullptr || bound_exp == nullptr || !aligned(bounds, 16))
+        return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_bounds(h->dm, h->v, h->sc, all_pages, bounds, bound_exp, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_select_blocks(md_handle h, int32_t layer, const md_select_args* a) {
+    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L) return MD_E_INVALID;
+    if (a->q == nullptr || !aligned(a->q, 16) || a->q_stride < (int64_t)h->dm.Hq * md::kHeadDim || a->q_stride % 4 != 0)
+        return MD_E_INVALID;
+    if (a->bounds == nullptr || !aligned(a->bounds, 16) || a->bound_exp == nullptr) return MD_E_INVALID;
+    if (a->max_blocks < 1 || a->max_blocks > md::kMaxPages || a->first < 0 || a->last < 0 ||
+        (int64_t)a->first + a->last > a->max_blocks)
+        return MD_E_INVALID;
+    if (a->blocks == nullptr || !aligned(a->blocks, 4) || a->block_count == nullptr || !aligned(a->block_count, 4))
+        return MD_E_INVALID;
+    if (a->workspace == nullptr || !aligned(a->workspace, 16)) return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_blocks(h->dm, h->v, h->sc, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_decode_workspace(md_handle h, uint64_t* attend_bytes, uint64_t* select_bytes) {
+    if (h == nullptr || attend_bytes == nullptr || select_bytes == nullptr) return MD_E_INVALID;
+    *attend_bytes = md::attend_workspace(h->dm, h->n_cu);
+    *select_bytes = md::select_workspace(h->dm);
     return MD_OK;
 }
 

@@ -1,0 +1,49 @@
+// Launchers of the decode operators: head preparation, attention over the
+// paged cache, page bounds and page selection.
+#pragma once
+
+#include "md_internal.h"
+
+namespace md {
+
+constexpr int kMinExp = -100, kMaxExp = 100;   // exponents of bounds and query codes
+
+// One call's arrays (md_attend_args) and place.
+struct TokenCall {
+    const float* q;
+    int64_t q_stride;
+    const uint16_t* new_k;
+    const uint16_t* new_v;
+    int64_t kv_stride;
+    const uint16_t* v_pool;
+    const int32_t* blocks;
+    const int32_t* block_count;
+    int max_blocks;
+    int out_bf16;
+    void* out;
+    int64_t out_stride;
+    float* lse;
+    int layer;
+    int splits;     // parts of every row
+    float* part;    // [S Hkv][splits][G][kPartWords] their results (splits > 1)
+};
+
+// Partial result of one query head: unnormalised sums of the 128 dims, then
+// the maximum (base 2) and the sum of the weights.
+constexpr int kPartWords = kHeadDim + 4;
+
+int attend_splits(const Dims& dm, int n_cu);
+uint64_t attend_workspace(const Dims& dm, int n_cu);
+hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, const TokenCall& c, hipStream_t st);
+
+hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a, int n_cu, hipStream_t st);
+hipError_t launch_append_values(const Dims& dm, const View& v, const uint16_t* new_v, uint16_t* v_pool,
+                                hipStream_t st);
+
+hipError_t launch_bounds(const Dims& dm, const View& v, const Scratch& sc, int all, int8_t* bounds, int8_t* bound_exp,
+                         hipStream_t st);
+uint64_t select_workspace(const Dims& dm);
+hipError_t launch_blocks(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_select_args& a,
+                         hipStream_t st);
+
+}  // namespace md

@@ -1,0 +1,731 @@
+"""The decode operators on the device against the 64-bit oracle.
+
+Tolerances, before any run.  A bf16 result is off by at most half a step,
+2^-8 relative; everything else is float32 (2^-24 a rounding):
+
+* rotation: the norm's sum of squares takes at most 12 roundings one after
+  another (halved by the root), root, reciprocal, two products and the
+  rotation 7 more; the angle is rounded once, as a fraction of a half turn
+  below 1 (pi 2^-25), sine and cosine by 2 units.  In all under 2^-19 of the
+  turned pair's length.
+* attention: a logit is 3 * 128 exact products summed in float32, at most
+  2^-24 * 384 * sum |q_e k_e| / sqrt(d) off; weights follow it twice over
+  (their own and the sum's), and take two bf16 terms (2^-17), the exponential
+  and the sums 2^-20.  An output is off by at most that times the largest
+  value, the log-sum by the logit's error and 2^-20 relative.
+* bounds and selections are whole numbers: equal.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import decode_oracle as O
+from paper_2607_10582_amd import binding as B
+from paper_2607_10582_amd.cache import MemDecay, PagedCache
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm device")
+    B.load_library()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+class World:
+    """A cache with prompts, its tokens by session on the host, and NaN in
+    every slot that holds no token."""
+
+    def __init__(self, L, Hq, Hkv, P, lens, seed=1, aligned=False, quant=0.0, window=1, extra=4, spare=2, scale=1.0,
+                 stream=None, static=False):
+        self.L, self.Hq, self.Hkv, self.P, self.S = L, Hq, Hkv, P, len(lens)
+        self.G = Hq // Hkv
+        self.lens = lens
+        g = torch.Generator().manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        regions = [np.repeat(rng.integers(0, 7, n // 5 + 1), 5)[:n].astype(np.uint8) for n in lens]
+        pages = [PagedCache.pages_for(r, P, aligned) for r in regions]
+        NP = sum(pages) + spare * self.S + 1
+        self.cache = c = PagedCache(L=L, Hq=Hq, Hkv=Hkv, d=D, P=P, S=self.S, max_pages=max(pages) + extra, n_phys=NP,
+                                    values=True, bounds=True)
+        c.k_pool.fill_(math.nan)
+        c.v_pool.fill_(math.nan)
+        c.key_bounds.fill_(-128)
+        c.bound_exp.fill_(99)
+        ids = rng.permutation(NP)
+        self.k, self.v = [], []     # per session [n][L][Hkv][d] float32 on the host, as the cache holds them
+        at = 0
+        for s, n in enumerate(lens):
+            k = (torch.randn((n, L, Hkv, D), generator=g) * scale).to(BF16)
+            v = torch.randn((n, L, Hkv, D), generator=g).to(BF16)
+            mine = ids[at:at + pages[s]]
+            at += pages[s]
+            if n:
+                c.load_session(s, k, regions[s], mine, budget=n, clock=n, region_aligned=aligned)
+                c.load_values(s, v, regions[s] if aligned else None)
+                pos = PagedCache.positions(regions[s], P, aligned)
+                dead = np.setdiff1d(np.arange(pages[s] * P), pos)
+                for pool, back, layout in ((c.k_pool, PagedCache.from_pool_layout, PagedCache.to_pool_layout),
+                                           (c.v_pool, PagedCache.from_value_layout, PagedCache.to_value_layout)):
+                    own = torch.as_tensor(mine, device=c.device)
+                    x = back(pool[own])
+                    x.view(-1, L, Hkv, D)[torch.as_tensor(dead, device=c.device)] = math.nan
+                    pool[own] = layout(x)
+            self.k.append(k.float())
+            self.v.append(v.float())
+            if n and quant > 0:
+                self._codes(s, mine, pages[s], regions[s], aligned, rng, quant)
+        self.regions, self.pages = regions, pages
+        c.set_free_pages(ids[at:])
+        self.dev = c.device
+        ones = torch.ones((self.S, 7))
+        self.md = MemDecay(c, ones, ones * 0.01, rho=0.9, alpha=1.0, tau_scale=2.0, pinned_mask=0, region_aligned=aligned,
+                           quant_threshold=0.3 if quant > 0 else 0.0, window=window, stream=stream, static=static)
+        self.aligned = aligned
+        self.g = g
+
+    def _codes(self, s, ids, m, region, aligned, rng, share):
+        """Some full pages of a session become codes and scales."""
+        c, P = self.cache, self.P
+        pos = PagedCache.positions(region, P, aligned)
+        for o in range(m - 1):
+            if rng.random() > share:
+                continue
+            toks = np.flatnonzero(pos // P == o)
+            x = torch.zeros((P, self.L, self.Hkv, D))
+            x[pos[toks] % P] = self.k[s][toks]
+            x = x.view(P // 16, 16, self.L, self.Hkv, D)
+            scale = x.abs().amax((1, 4)) / 448.0                               # [block][L][Hkv]
+            codes = (x / torch.where(scale > 0, scale, 1.0)[:, None, :, :, None]).to(torch.float8_e4m3fn)
+            back = codes.float() * scale[:, None, :, :, None]
+            self.k[s][toks] = back.view(P, self.L, self.Hkv, D)[pos[toks] % P]
+            raw = torch.full((self.L, self.Hkv, P // 16, 4096), 0xFF, dtype=torch.uint8)
+            e = torch.arange(D)
+            for t in range(16):
+                raw[..., 1024 * (e // 64) + 16 * (t + 16 * ((e // 8) % 4)) + 8 * ((e // 32) % 2) + e % 8] = \
+                    codes.view(torch.uint8)[:, t].permute(1, 2, 0, 3)
+            raw[..., 2048:2064] = scale.permute(1, 2, 0).contiguous().view(-1, 1).repeat(1, 4).view(torch.uint8) \
+                .view(self.L, self.Hkv, P // 16, 16)
+            page = int(ids[o])
+            c.k_pool.view(torch.uint8).view(c.n_phys, self.L, self.Hkv, P // 16, 4096)[page] = raw.to(c.device)
+            c.page_format[page] = 1
+
+    def token_pages(self, s):
+        """Logical page of each token."""
+        return PagedCache.positions(self.regions[s], self.P, self.aligned) // self.P
+
+    def normal(self, *shape, dtype=torch.float32):
+        return torch.randn(shape, generator=self.g).to(dtype).to(self.dev)
+
+
+def check_attend(w, layer, q, out, lse, new_k=None, new_v=None, lists=None, seen=""):
+    """out, lse against the oracle; lists[s][kv]: the pages attended to."""
+    q, out, lse = q.cpu(), out.cpu().double(), lse.cpu().double()
+    for s in range(w.S):
+        page = w.token_pages(s)
+        for kv in range(w.Hkv):
+            k, v = w.k[s][:, layer, kv], w.v[s][:, layer, kv]
+            if lists is not None:
+                at = torch.as_tensor(np.isin(page, lists[s][kv]))
+                k, v = k[at], v[at]
+            if new_k is not None:
+                k = torch.cat([k, new_k[s, kv].cpu().float()[None]])
+                v = torch.cat([v, new_v[s, kv].cpu().float()[None]])
+            qq = q[s].view(w.Hq, D)[kv * w.G:(kv + 1) * w.G]
+            ref, rl = O.attend(qq, k, v)
+            got, gl = out[s].view(w.Hq, D)[kv * w.G:(kv + 1) * w.G], lse[s, kv * w.G:(kv + 1) * w.G]
+            if k.shape[0] == 0:
+                assert torch.equal(got, ref) and torch.equal(gl, rl), (seen, s, kv)
+                continue
+            off = float((qq.double().abs() @ k.double().abs().T).max()) / math.sqrt(D) * 384 * 2.0 ** -24
+            tol = (2 * off + 2.0 ** -17 + 2.0 ** -20) * float(v.abs().max())
+            step = 2.0 ** -8 * ref.abs() if w.out == BF16 else 0.0
+            err = (got - ref).abs()
+            assert torch.isfinite(got).all() and bool((err <= tol + step).all()), (seen, s, kv, float(err.max()), tol)
+            assert bool(((gl - rl).abs() <= off + 2.0 ** -20 * (1 + rl.abs())).all()), (seen, s, kv)
+
+
+def run_attend(w, layer=None, new=True, lists=None, out_type=torch.float32, **kw):
+    layer = w.L - 1 if layer is None else layer
+    w.out = out_type
+    q = w.normal(w.S, w.Hq, D) * 2
+    nk, nv = (w.normal(w.S, w.Hkv, D, dtype=BF16) for _ in range(2)) if new else (None, None)
+    out = torch.full((w.S, w.Hq, D), math.nan, dtype=out_type, device=w.dev)
+    lse = torch.full((w.S, w.Hq), math.nan, device=w.dev)
+    blocks = {}
+    if lists is not None:
+        most = max(1, max(len(x) for r in lists for x in r))
+        b = torch.full((w.S, w.Hkv, most), -7, dtype=torch.int32)
+        n = torch.zeros((w.S, w.Hkv), dtype=torch.int32)
+        for s in range(w.S):
+            for kv in range(w.Hkv):
+                b[s, kv, :len(lists[s][kv])] = torch.tensor(lists[s][kv], dtype=torch.int32)
+                n[s, kv] = len(lists[s][kv])
+        blocks = dict(blocks=b.to(w.dev), block_count=n.to(w.dev))
+    w.md.attend(layer, q, out, new_k=nk, new_v=nv, lse=lse, **blocks)
+    torch.cuda.synchronize()
+    assert w.md.device_status() == 0
+    check_attend(w, layer, q, out, lse, nk, nv, lists, **kw)
+
+
+LENS = {"one": [1], "edges": [0, 1, 15, 16, 17, 31, 33, 63, 64, 65], "chat": [450], "uneven": [1700, 3, 640, 0, 5000],
+        "long": [20011]}
+
+
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("new", [True, False])
+@pytest.mark.parametrize("lens", sorted(LENS))
+def test_attention_over_every_page(lens, new, P):
+    say("[attend]", lens, new, P)
+    w = World(2, 12, 2, P, LENS[lens], seed=3)
+    run_attend(w, new=new)
+    run_attend(w, layer=0, new=new, out_type=BF16)
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1), (3, 5, 5), (2, 16, 1), (1, 32, 8), (2, 12, 4), (1, 14, 2)])
+def test_head_layouts(shape):
+    say("[attend]", shape)
+    w = World(*shape, 16, [300, 0, 1, 2049], seed=4)
+    run_attend(w)
+    run_attend(w, out_type=BF16, new=False)
+
+
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("aligned,quant", [(True, 0.0), (False, 0.6), (True, 0.6)])
+def test_holes_and_codes(aligned, quant, P):
+    say("[attend]", aligned, quant, P)
+    w = World(2, 12, 2, P, [700, 0, 1, 16, 2500], seed=5, aligned=aligned, quant=quant)
+    run_attend(w)
+    run_attend(w, new=False, out_type=BF16)
+    lists = [[sorted(np.random.default_rng(s * 9 + kv).choice(w.pages[s], min(w.pages[s], 9), replace=False).tolist())
+              if w.pages[s] else [] for kv in range(w.Hkv)] for s in range(w.S)]
+    run_attend(w, lists=lists)
+
+
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("most", [1, 2, 7, 40])
+def test_attention_over_listed_pages(most, P):
+    say("[sparse]", most, P)
+    w = World(2, 16, 2, P, [1700, 0, 1, 5000, 64], seed=6)
+    rng = np.random.default_rng(7)
+    lists = [[sorted(rng.choice(w.pages[s], min(w.pages[s], rng.integers(0, most + 1)), replace=False).tolist())
+              if w.pages[s] else [] for _ in range(w.Hkv)] for s in range(w.S)]
+    run_attend(w, lists=lists)
+    run_attend(w, lists=lists, new=False, out_type=BF16)
+
+
+def test_many_sessions():
+    lens = [(37 * i) % 211 for i in range(300)]
+    w = World(1, 4, 2, 16, lens, seed=8)
+    run_attend(w)
+
+
+def test_large_logits():
+    # logits in the hundreds: weights underflow, the maximum moves late
+    w = World(1, 12, 2, 16, [900], seed=9, scale=8.0)
+    run_attend(w)
+
+
+def test_weights_of_equal_keys_are_equal():
+    w = World(1, 8, 1, 16, [513], seed=10)
+    w.cache.k_pool.copy_(torch.where(torch.isnan(w.cache.k_pool), w.cache.k_pool, 0.5))
+    w.k[0].fill_(0.5)
+    run_attend(w, new=False)
+
+
+def test_strided_rows_and_untouched_neighbours():
+    # the layer's rows of the step's buffers, outputs between other rows
+    L, Hq, Hkv, S = 3, 12, 2, 4
+    w = World(L, Hq, Hkv, 16, [40, 333, 0, 900], seed=11)
+    w.out = torch.float32
+    q = w.normal(S, 1, L, Hq, D)
+    nk, nv = w.normal(S, L, Hkv, D, dtype=BF16), w.normal(S, L, Hkv, D, dtype=BF16)
+    out = torch.full((S, 2, Hq, D), 7.0, device=w.dev)
+    lse = torch.empty((S, Hq), device=w.dev)
+    for layer in range(L):
+        w.md.attend(layer, q[:, 0, layer], out[:, 1], new_k=nk[:, layer], new_v=nv[:, layer], lse=lse)
+        torch.cuda.synchronize()
+        check_attend(w, layer, q[:, 0, layer], out[:, 1], lse, nk[:, layer], nv[:, layer])
+        assert bool((out[:, 0] == 7.0).all())
+    w.md.attend(0, q[:, 0, 0], out[:, 1])   # no new token, no log-sum
+    torch.cuda.synchronize()
+    check_attend(w, 0, q[:, 0, 0], out[:, 1], _lse(w, 0, q[:, 0, 0]))
+
+
+def _lse(w, layer, q):
+    out = torch.empty((w.S, w.Hq))
+    for s in range(w.S):
+        for kv in range(w.Hkv):
+            out[s, kv * w.G:(kv + 1) * w.G] = O.attend(q[s].cpu()[kv * w.G:(kv + 1) * w.G], w.k[s][:, layer, kv],
+                                                      w.v[s][:, layer, kv])[1]
+    return out.to(w.dev)
+
+
+def test_nan_stays_in_its_head():
+    w = World(1, 12, 2, 16, [450, 300], seed=12)
+    q = w.normal(2, 12, D)
+    q[0, 3, 5] = math.nan
+    out, lse = torch.zeros((2, 12, D), device=w.dev), torch.zeros((2, 12), device=w.dev)
+    w.md.attend(0, q, out, lse=lse)
+    torch.cuda.synchronize()
+    bad = torch.isnan(out).all(-1).cpu()
+    assert bool(bad[0, 3]) and int(torch.isnan(out).any(-1).sum()) == 1
+    assert int(torch.isnan(lse).sum()) == 1 and w.md.device_status() == 0
+
+
+def test_broken_lists_and_tables_are_left_out():
+    # entries that do not ascend, are not there or are too many, a page
+    # table's entry out of range, counters that contradict each other
+    w = World(1, 8, 2, 16, [320, 200, 100], seed=13)
+    q = w.normal(3, 8, D)
+    out, lse = torch.zeros((3, 8, D), device=w.dev), torch.zeros((3, 8), device=w.dev)
+    blocks = torch.zeros((3, 2, 4), dtype=torch.int32)
+    blocks[0, 0], blocks[0, 1] = torch.tensor([2, 2, 5, 3]), torch.tensor([-1, 4, 20, 1 << 30])
+    blocks[1, 0], blocks[1, 1] = torch.tensor([0, 1, 2, 3]), torch.tensor([0, 1, 2, 3])
+    count = torch.tensor([[4, 4], [2, 9], [-3, 0]], dtype=torch.int32)
+    w.md.attend(0, q, out, lse=lse, blocks=blocks.to(w.dev), block_count=count.to(w.dev))
+    torch.cuda.synchronize()
+    assert w.md.device_status() == B.MD_DEV_BAD_BLOCK
+    w.out = torch.float32
+    check_attend(w, 0, q, out, lse, lists=[[[2, 5], [4]], [[0, 1], [0, 1, 2, 3]], [[], []]])
+    c = w.cache
+    keep = c.page_table.clone()
+    c.page_table[0, 3] = 1 << 29
+    c.n_pages[1] = 40
+    w.md.attend(0, q, out, lse=lse)
+    torch.cuda.synchronize()
+    assert w.md.device_status() == B.MD_DEV_CORRUPT
+    assert torch.equal(out[1].cpu(), torch.zeros(8, D)) and bool((lse[1] == -math.inf).all())
+    c.page_table.copy_(keep)
+    c.n_pages[1] = w.pages[1]
+    w.md.attend(0, q, out, lse=lse)
+    torch.cuda.synchronize()
+    assert w.md.device_status() == 0
+    check_attend(w, 0, q, out, lse)
+
+
+# ------------------------------------------------------------------ norm and rotation
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16, torch.float16])
+@pytest.mark.parametrize("rot,interleaved", [(128, False), (128, True), (64, False), (96, False), (16, False), (48, True),
+                                             (0, False)])
+@pytest.mark.parametrize("n,weights", [(1, True), (3, False), (70, True)])
+def test_norm_rope(n, weights, rot, interleaved, dtype):
+    w = World(2, 6, 2, 16, [5], seed=14)
+    g = torch.Generator().manual_seed(n + rot)
+    wide = (w.Hq + 2 * w.Hkv) * D
+    room = torch.randn((n, wide + 24), generator=g).mul_(3).to(dtype).to(w.dev)
+    qkv = room[:, 16:16 + wide]
+    inv = None if rot == 0 else torch.as_tensor(10000.0 ** (-np.arange(0, rot, 2) / rot), device=w.dev)
+    pos = torch.randint(0, 2 ** 31 - 1, (n,), generator=g, dtype=torch.int32).to(w.dev)
+    pos[0] = 0
+    wq, wk = ((torch.rand(D, generator=g) + 0.5).to(w.dev) for _ in range(2)) if weights else (None, None)
+    q = torch.full((n, 2, w.Hq, D), 9.0, device=w.dev)
+    k, v = (torch.full((n, 3, w.Hkv, D), 9.0, dtype=BF16, device=w.dev) for _ in range(2))
+    w.md.norm_rope(qkv, q[:, 1], k[:, 2], v[:, 2], q_weight=wq, k_weight=wk, eps=1e-5, inv_freq=inv, position=pos,
+                   interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert bool((q[:, 0] == 9.0).all()) and bool((k[:, :2] == 9.0).all()) and bool((v[:, :2] == 9.0).all())
+    x = qkv.cpu().double().view(n, -1, D)
+    heads = (x[:, :w.Hq], x[:, w.Hq:w.Hq + w.Hkv], x[:, w.Hq + w.Hkv:])
+    cpu = [None if t is None else t.cpu() for t in (wq, wk, inv, pos)]
+    for got, x, wt, step in ((q[:, 1], heads[0], cpu[0], 0.0), (k[:, 2], heads[1], cpu[1], 2.0 ** -8)):
+        ref = O.norm_rope(x, wt, float(np.float32(1e-5)), cpu[3], cpu[2], interleaved)
+        size = O.norm_rope(x, wt, float(np.float32(1e-5)), cpu[3], None, False)   # lengths of the pairs
+        r = size.clone()
+        half = rot // 2
+        for i in range(half):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+            r[..., a] = r[..., b] = torch.hypot(size[..., a], size[..., b])
+        err = (got.cpu().double() - ref).abs()
+        assert bool((err <= 2.0 ** -19 * r.abs() * (1 + step) + step * ref.abs()).all()), float((err / r.abs()).max())
+    assert torch.equal(v[:, 2].cpu(), qkv.cpu().view(n, -1, D)[:, w.Hq + w.Hkv:].to(BF16))
+
+
+def test_norm_rope_defaults():
+    # the session's clock as position; keys and queries without values; rows of zeros, no rows
+    w = World(2, 6, 2, 16, [5, 0, 77], seed=15)
+    w.cache.clock.copy_(torch.tensor([5, 0, 1000003], dtype=torch.int32))
+    wide = (w.Hq + 2 * w.Hkv) * D
+    qkv = w.normal(3, wide)
+    qkv[1] = 0
+    inv = torch.as_tensor(10000.0 ** (-np.arange(0, D, 2) / D), device=w.dev)
+    one = torch.ones(D, device=w.dev)
+    out = []
+    for pos in (None, w.cache.clock.clone()):
+        q, k = torch.zeros((3, w.Hq, D), device=w.dev), torch.zeros((3, w.Hkv, D), dtype=BF16, device=w.dev)
+        w.md.norm_rope(qkv, q, k, q_weight=one, k_weight=one, inv_freq=inv, position=pos)
+        torch.cuda.synchronize()
+        out.append((q.cpu(), k.cpu()))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    assert bool((out[0][0][1] == 0).all()) and bool((out[0][0][0] != 0).any())
+    w.md.norm_rope(qkv[:0], q[:0], k[:0], inv_freq=inv)
+    with pytest.raises(B.MemDecayError):
+        w.md.norm_rope(qkv[:2], q[:2], k[:2], inv_freq=inv)   # two rows, three clocks
+
+
+# ------------------------------------------------------------------ bounds and selection
+
+def check_bounds(w, pages):
+    c = w.cache
+    got, exp, table = c.key_bounds.cpu().numpy(), c.bound_exp.cpu().numpy(), c.page_table.cpu().numpy()
+    for s, o in pages:
+        k = w.k[s][torch.as_tensor(w.token_pages(s) == o)].numpy()
+        for layer in range(w.L):
+            for kv in range(w.Hkv):
+                lo, hi, e = O.bounds(k[:, layer, kv])
+                at = (table[s, o], layer, kv)
+                assert exp[at] == e and (got[at][0] == lo).all() and (got[at][1] == hi).all(), (s, o, layer, kv)
+
+
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("aligned,quant", [(False, 0.0), (True, 0.0), (False, 0.6), (True, 0.6)])
+def test_key_bounds(aligned, quant, P):
+    w = World(3, 6, 2, P, [450, 0, 1, 65, 16], seed=16, aligned=aligned, quant=quant)
+    w.md.update_bounds()
+    torch.cuda.synchronize()
+    last = [(s, m - 1) for s, m in enumerate(w.pages) if m]
+    check_bounds(w, last)
+    touched = {int(w.cache.page_table[s, o]) for s, o in last}
+    rest = [p for p in range(w.cache.n_phys) if p not in touched]
+    assert bool((w.cache.key_bounds[rest] == -128).all()) and bool((w.cache.bound_exp[rest] == 99).all())
+    w.md.update_bounds(all_pages=True)
+    torch.cuda.synchronize()
+    check_bounds(w, [(s, o) for s, m in enumerate(w.pages) for o in range(m)])
+    assert w.md.device_status() == 0
+
+
+def test_bounds_of_unusual_keys():
+    # zeros, the largest and smallest numbers, infinities and NaNs, the borders of a step
+    w = World(1, 1, 1, 16, [16 * 6], seed=17)
+    k = torch.zeros((96, D))
+    k[16:32, 0] = 3.3e38
+    k[16:32, 1] = -1e-39
+    k[32:48, 0] = 127.0
+    k[32:48, 1] = 126.5
+    k[48:64, 0] = 127.5
+    k[64] = 2.0 ** -133
+    k = k.to(BF16).float()
+    w.k[0] = k.view(96, 1, 1, D)
+    w.cache.k_pool[w.cache.page_table[0, :6].long()] = PagedCache.to_pool_layout(w.k[0].to(BF16).to(w.dev).view(6, 16, 1, 1, D))
+    w.md.update_bounds(all_pages=True)
+    torch.cuda.synchronize()
+    check_bounds(w, [(0, o) for o in range(6)])
+    bad = k.clone()
+    bad[0, 0], bad[1, 1], bad[2, 2], bad[3, 3] = math.inf, -math.inf, math.nan, -math.nan
+    w.cache.k_pool[w.cache.page_table[0, :6].long()] = PagedCache.to_pool_layout(bad.to(BF16).to(w.dev).view(6, 16, 1, 1, D))
+    w.md.update_bounds(all_pages=True)
+    torch.cuda.synchronize()
+    page = int(w.cache.page_table[0, 0])
+    lo, hi = w.cache.key_bounds[page, 0, 0].cpu()
+    assert int(w.cache.bound_exp[page, 0, 0]) == 100 and int(hi[0]) == 127 and int(lo[1]) == -127
+    assert abs(int(hi[2]) - int(lo[2])) == 127 and abs(int(hi[3]) - int(lo[3])) == 127 and not lo[4:].any()
+
+
+def oracle_lists(w, layer, q, most, first, last):
+    got, exp, table = w.cache.key_bounds.cpu().numpy(), w.cache.bound_exp.cpu().numpy(), w.cache.page_table.cpu().numpy()
+    out = []
+    for s in range(w.S):
+        rows = []
+        for kv in range(w.Hkv):
+            qq = q[s].cpu().numpy()[kv * w.G:(kv + 1) * w.G]
+            sc = [O.block_score(qq, got[p, layer, kv, 0].astype(np.int64), got[p, layer, kv, 1].astype(np.int64),
+                                int(exp[p, layer, kv])) for p in table[s, :w.pages[s]]]
+            rows.append(O.select(sc, most, first, last))
+        out.append(rows)
+    return out
+
+
+def run_select(w, layer, q, most, first, last):
+    blocks = torch.full((w.S, w.Hkv, most), -9, dtype=torch.int32, device=w.dev)
+    count = torch.full((w.S, w.Hkv), -9, dtype=torch.int32, device=w.dev)
+    w.md.select_blocks(layer, q, blocks, count, first=first, last=last)
+    torch.cuda.synchronize()
+    b, n = blocks.cpu().numpy(), count.cpu().numpy()
+    lists = [[b[s, kv, :n[s, kv]].tolist() for kv in range(w.Hkv)] for s in range(w.S)]
+    assert all((b[s, kv, n[s, kv]:] == -1).all() for s in range(w.S) for kv in range(w.Hkv))
+    return lists, blocks, count
+
+
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("shape", [(2, 12, 2), (1, 16, 1), (2, 5, 5)])
+@pytest.mark.parametrize("most,first,last", [(1, 0, 0), (3, 1, 2), (8, 1, 1), (50, 0, 3), (400, 5, 9)])
+def test_selected_blocks_and_attention_over_them(most, first, last, shape, P):
+    say("[select]", most, first, last, shape, P)
+    w = World(*shape, P, [0, 1, P * 3, 1700, 3333], seed=18)
+    w.md.update_bounds(all_pages=True)
+    q = w.normal(w.S, w.Hq, D)
+    layer = w.L - 1
+    lists, blocks, count = run_select(w, layer, q, most, first, last)
+    assert lists == oracle_lists(w, layer, q, most, first, last)
+    w.out = torch.float32
+    out, lse = torch.zeros((w.S, w.Hq, D), device=w.dev), torch.zeros((w.S, w.Hq), device=w.dev)
+    w.md.attend(layer, q, out, lse=lse, blocks=blocks, block_count=count)
+    torch.cuda.synchronize()
+    check_attend(w, layer, q, out, lse, lists=lists)
+    assert w.md.device_status() == 0
+
+
+def test_equal_scores_go_to_the_older_page():
+    w = World(1, 4, 2, 16, [16 * 500, 16 * 300], seed=19)
+    w.cache.key_bounds.fill_(3)
+    w.cache.bound_exp.fill_(-2)
+    q = w.normal(2, 4, D)
+    for most, first, last in ((7, 0, 0), (7, 1, 2), (299, 2, 1), (300, 0, 0), (499, 0, 1)):
+        lists, *_ = run_select(w, 0, q, most, first, last)
+        assert lists == oracle_lists(w, 0, q, most, first, last)
+    q.zero_()
+    lists, *_ = run_select(w, 0, q, 9, 1, 1)
+    assert lists[0][0] == list(range(8)) + [499]
+
+
+def test_selection_over_a_full_page_table():
+    # 8,192 pages, scores in few distinct values
+    w = World(1, 2, 1, 16, [16 * 8192], seed=20, extra=0)
+    g = torch.Generator().manual_seed(5)
+    w.cache.key_bounds.copy_(torch.randint(-2, 3, w.cache.key_bounds.shape, generator=g).to(torch.int8))
+    w.cache.bound_exp.fill_(-3)
+    q = w.normal(1, 2, D)
+    for most, first, last in ((1, 0, 0), (512, 1, 2), (8191, 4, 4), (8192, 0, 0)):
+        lists, *_ = run_select(w, 0, q, most, first, last)
+        assert lists == oracle_lists(w, 0, q, most, first, last)
+
+
+def test_nan_in_a_query_counts_as_zero():
+    w = World(1, 4, 2, 16, [800], seed=21)
+    w.md.update_bounds(all_pages=True)
+    q = w.normal(1, 4, D)
+    q[0, 1, 7], q[0, 2] = math.nan, math.nan
+    lists, *_ = run_select(w, 0, q, 9, 1, 1)
+    assert lists == oracle_lists(w, 0, q, 9, 1, 1)
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_refusals():
+    w = World(2, 12, 2, 16, [40, 50], seed=22)
+    md, c = w.md, w.cache
+    q, out = w.normal(2, 12, D), torch.zeros((2, 12, D), device=w.dev)
+    nk = w.normal(2, 2, D, dtype=BF16)
+    with pytest.raises(B.MemDecayError) as e:
+        md.attend(2, q, out)
+    assert e.value.status == B.MD_E_INVALID
+    with pytest.raises(B.MemDecayError):
+        md.attend(-1, q, out)
+    with pytest.raises(B.MemDecayError):
+        md.attend(0, q, out, new_k=nk)                              # a key without its value
+    for bad in (dict(q=q[:1]), dict(q=q.double()), dict(q=q.transpose(1, 2)), dict(out=out.half()), dict(out=out[:, :6]),
+                dict(q=q.cpu()), dict(new_k=nk.float(), new_v=nk.float()), dict(lse=torch.zeros(3, device=w.dev)),
+                dict(blocks=torch.zeros((2, 3), dtype=torch.int32, device=w.dev)),
+                dict(blocks=torch.zeros((2, 2, 3), dtype=torch.int32, device=w.dev))):
+        a = dict(dict(q=q, out=out), **bad)
+        with pytest.raises(ValueError):
+            md.attend(0, a.pop("q"), a.pop("out"), **a)
+    odd = torch.zeros(2 * 12 * D + 1, device=w.dev)[1:].view(2, 12, D)
+    with pytest.raises(B.MemDecayError):
+        md.attend(0, odd, out)                                      # 4 bytes off
+    blocks, count = torch.zeros((2, 2, 3), dtype=torch.int32, device=w.dev), torch.zeros((2, 2), dtype=torch.int32, device=w.dev)
+    for first, last in ((-1, 1), (1, -1), (2, 2)):
+        with pytest.raises(B.MemDecayError):
+            md.select_blocks(0, q, blocks, count, first=first, last=last)
+    with pytest.raises(B.MemDecayError):
+        md.select_blocks(2, q, blocks, count)
+    with pytest.raises(B.MemDecayError) as e:
+        md.append_values(w.normal(2, 2, 2, D, dtype=BF16))          # nothing was appended
+    assert e.value.status == B.MD_E_STATE
+    wide = w.normal(2, 16 * D)
+    k = torch.zeros((2, 2, D), dtype=BF16, device=w.dev)
+    for bad in (dict(eps=-1.0), dict(eps=math.nan), dict(inv_freq=torch.ones(7, dtype=torch.float64, device=w.dev)),
+                dict(inv_freq=torch.ones(72, dtype=torch.float64, device=w.dev))):
+        with pytest.raises(B.MemDecayError):
+            md.norm_rope(wide, q, k, **bad)
+    for a in ((wide[:, :-1], q, k), (wide.double(), q, k), (wide, q.to(BF16), k), (wide, q, k.float()), (wide, q[:1], k)):
+        with pytest.raises(ValueError):
+            md.norm_rope(*a)
+    with pytest.raises(ValueError):
+        md.norm_rope(wide, q, k, position=torch.zeros(3, dtype=torch.int32, device=w.dev))
+    c.v_pool = c.key_bounds = None
+    for call in (lambda: md.attend(0, q, out), lambda: md.update_bounds(), lambda: md.select_blocks(0, q, blocks, count)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_offload_handles_refuse_values():
+    c = PagedCache(L=1, Hq=2, Hkv=1, d=D, P=16, S=1, max_pages=4, n_phys=8, offload_pages=2, values=True, bounds=True)
+    one = torch.ones((1, 7))
+    md = MemDecay(c, one, one, rho=0.9, alpha=1.0, tau_scale=2.0, pinned_mask=0)
+    q, out = torch.zeros((1, 2, D), device="cuda"), torch.zeros((1, 2, D), device="cuda")
+    blocks, count = torch.zeros((1, 1, 1), dtype=torch.int32, device="cuda"), torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    for call in (lambda: md.attend(0, q, out), lambda: md.update_bounds(),
+                 lambda: md.select_blocks(0, q, blocks, count, first=0, last=0),
+                 lambda: md.append_values(torch.zeros((1, 1, 1, D), dtype=BF16, device="cuda"))):
+        with pytest.raises(B.MemDecayError) as e:
+            call()
+        assert e.value.status == B.MD_E_UNSUPPORTED
+
+
+# ------------------------------------------------------------------ a run of them together
+
+@pytest.mark.parametrize("kw", [dict(), dict(P=64), dict(aligned=True), dict(quant=True), dict(stream=True), dict(static=True)],
+                         ids=str)
+def test_decode_steps(kw):
+    """Decode steps of a two-layer model: per layer norm and rotation into the
+    step's buffers, selection, attention over the whole cache and over the
+    selected pages; then the retention step with its evictions.  The tokens
+    each session holds are read off its slots' insertion steps."""
+    P, L, Hq, Hkv = kw.get("P", 16), 2, 8, 2
+    lens = [150, 0, 97, 333]
+    stream = torch.cuda.Stream() if kw.get("stream") else None
+    w = World(L, Hq, Hkv, P, lens, seed=23, aligned=kw.get("aligned", False), extra=40, spare=40, stream=stream,
+              quant=1e-9 if kw.get("quant") else 0.0, static=kw.get("static", False))
+    c, md, S = w.cache, w.md, w.S
+    c.budget.copy_(torch.tensor([90, 60, 97, 200], dtype=torch.int32))
+    inv = torch.as_tensor(10000.0 ** (-np.arange(0, D, 2) / D), device=w.dev)
+    wq, wk = w.normal(D).abs() + 0.5, w.normal(D).abs() + 0.5
+    keys = [{t: w.k[s][t] for t in range(n)} for s, n in enumerate(lens)]       # by insertion step
+    vals = [{t: w.v[s][t] for t in range(n)} for s, n in enumerate(lens)]
+    q = torch.zeros((S, 1, L, Hq, D), device=w.dev)
+    nk, nv = (torch.zeros((S, L, Hkv, D), dtype=BF16, device=w.dev) for _ in range(2))
+    outs = [torch.zeros((S, Hq, D), device=w.dev) for _ in range(2)]
+    lses = [torch.zeros((S, Hq), device=w.dev) for _ in range(2)]
+    blocks = torch.zeros((S, Hkv, 5), dtype=torch.int32, device=w.dev)
+    count = torch.zeros((S, Hkv), dtype=torch.int32, device=w.dev)
+    reg = torch.zeros(S, dtype=torch.uint8, device=w.dev)
+    w.out = torch.float32
+    torch.cuda.synchronize()
+    md.update_bounds(all_pages=True)
+    evicted = 0
+    for step in range(1, 41):
+        qkv = w.normal(S, L, (Hq + 2 * Hkv) * D, dtype=BF16)
+        torch.cuda.synchronize()
+        table, npg, slot_t, region, fmt = (x.cpu().numpy() for x in (c.page_table, c.n_pages, c.t_ins, c.region, c.page_format))
+        ntok, clock = c.n_tokens.cpu().numpy(), c.clock.cpu().numpy()
+        pool = PagedCache.from_pool_layout(c.k_pool).float().cpu()
+        for s in range(S):     # the tokens held now
+            at = [(o, table[s, o], j) for o in range(npg[s]) for j in range(P)
+                  if o * P + j < ntok[s] and region[table[s, o], j] != B.MD_REGION_HOLE]
+            t = [int(slot_t[p, j]) for _, p, j in at]
+            zero = torch.zeros((0, L, Hkv, D))
+            for (o, p, j), i in zip(at, t):
+                if not fmt[p]:
+                    assert torch.equal(pool[p, j], keys[s][i]), (step, s, i)
+                else:
+                    raw = c.k_pool.view(torch.uint8).view(c.n_phys, L, Hkv, P // 16, 4096)[p].cpu()
+                    e = torch.arange(D)
+                    tt = j % 16
+                    code = raw[:, :, j // 16, 1024 * (e // 64) + 16 * (tt + 16 * ((e // 8) % 4)) + 8 * ((e // 32) % 2) + e % 8]
+                    scale = raw[:, :, j // 16, 2048:2052].contiguous().view(torch.float32)
+                    keys[s][i] = code.contiguous().view(torch.float8_e4m3fn).float() * scale
+            w.k[s] = torch.stack([keys[s][i] for i in t]) if t else zero
+            w.v[s] = torch.stack([vals[s][i] for i in t]) if t else zero
+            w.pages[s] = int(npg[s])
+            w.held = getattr(w, "held", {})
+            w.held[s] = np.array([o for o, _, _ in at], np.int64)
+        w.token_pages = lambda s: w.held[s]
+        for layer in range(L):
+            md.norm_rope(qkv[:, layer], q[:, 0, layer], nk[:, layer], nv[:, layer], q_weight=wq, k_weight=wk, eps=1e-5,
+                         inv_freq=inv)
+            md.attend(layer, q[:, 0, layer], outs[0], new_k=nk[:, layer], new_v=nv[:, layer], lse=lses[0])
+            md.select_blocks(layer, q[:, 0, layer], blocks, count, first=1, last=2)
+            md.attend(layer, q[:, 0, layer], outs[1], new_k=nk[:, layer], new_v=nv[:, layer], lse=lses[1], blocks=blocks,
+                      block_count=count)
+            torch.cuda.synchronize()
+            ref = O.norm_rope(qkv[:, layer].cpu().double().view(S, -1, D)[:, :Hq], wq.cpu(), float(np.float32(1e-5)),
+                              torch.as_tensor(clock), inv.cpu(), False)
+            assert float((q[:, 0, layer].cpu() - ref).abs().max()) <= 2.0 ** -18 * float(ref.abs().max())
+            check_attend(w, layer, q[:, 0, layer], outs[0], lses[0], nk[:, layer], nv[:, layer], seen=step)
+            lists = [[blocks[s, kv, :int(count[s, kv])].tolist() for kv in range(Hkv)] for s in range(S)]
+            assert lists == oracle_lists(w, layer, q[:, 0, layer], 5, 1, 2), (step, layer)
+            check_attend(w, layer, q[:, 0, layer], outs[1], lses[1], nk[:, layer], nv[:, layer], lists, seen=step)
+        reg.fill_(step // 6 % 7)
+        torch.cuda.synchronize()
+        md.observe(step, q, nk, reg)
+        md.append_values(nv)
+        md.update_bounds()
+        for s in range(S):
+            keys[s][int(clock[s]) + 1] = nk[s].float().cpu()
+            vals[s][int(clock[s]) + 1] = nv[s].float().cpu()
+        md.score()
+        md.select_compact()
+        with pytest.raises(B.MemDecayError):
+            md.append_values(nv)                                    # pages may have moved
+        torch.cuda.synchronize()
+        evicted += int(md.evict_count.sum())
+        assert md.device_status() == 0
+    assert evicted >= (5 if P == 64 else 11)
+    assert not kw.get("quant") or int(c.page_format.sum()) > 0
+    md.close()
+
+
+def test_sessions_that_took_no_token_keep_their_values():
+    w = World(1, 2, 1, 16, [16, 5], seed=24, spare=0)
+    c = w.cache
+    c.free_count.zero_()                                            # session 0 needs a page and gets none
+    keep = c.v_pool.clone()
+    nk, nv = w.normal(2, 1, 1, D, dtype=BF16), w.normal(2, 1, 1, D, dtype=BF16)
+    w.md.observe(1, w.normal(2, 1, 1, 2, D), nk, torch.zeros(2, dtype=torch.uint8, device=w.dev))
+    w.md.append_values(nv)
+    torch.cuda.synchronize()
+    assert w.md.device_status() == B.MD_DEV_CAPACITY
+    p0, p1 = int(c.page_table[0, 0]), int(c.page_table[1, 0])
+    a, b = PagedCache.from_value_layout(c.v_pool), PagedCache.from_value_layout(keep)
+    assert torch.equal(a[p0].view(torch.int16), b[p0].view(torch.int16))
+    assert torch.equal(a[p1, 5], nv[1]) and torch.equal(a[p1, :5], b[p1, :5])
+    assert bool(torch.isnan(a[p1, 6:]).all())
+
+
+def test_captured_calls_replay():
+    # the calls of a layer in one graph, replayed while the cache and the
+    # inputs change, with eager calls in between
+    S, L, Hq, Hkv = 3, 2, 12, 2
+    side = torch.cuda.Stream()
+    w = World(L, Hq, Hkv, 16, [700, 64, 1], seed=25, stream=side)
+    c, md = w.cache, w.md
+    inv = torch.as_tensor(10000.0 ** (-np.arange(0, D, 2) / D), device=w.dev)
+    qkv = w.normal(S, (Hq + 2 * Hkv) * D, dtype=BF16)
+
+    def buffers():
+        return dict(q=torch.zeros((S, Hq, D), device=w.dev), k=torch.zeros((S, Hkv, D), dtype=BF16, device=w.dev),
+                    v=torch.zeros((S, Hkv, D), dtype=BF16, device=w.dev), out=torch.zeros((S, Hq, D), device=w.dev),
+                    lse=torch.zeros((S, Hq), device=w.dev),
+                    blocks=torch.zeros((S, Hkv, 6), dtype=torch.int32, device=w.dev),
+                    count=torch.zeros((S, Hkv), dtype=torch.int32, device=w.dev))
+
+    def calls(b):
+        md.update_bounds()
+        md.norm_rope(qkv, b["q"], b["k"], b["v"], inv_freq=inv)
+        md.select_blocks(1, b["q"], b["blocks"], b["count"], first=1, last=1)
+        md.attend(1, b["q"], b["out"], new_k=b["k"], new_v=b["v"], lse=b["lse"], blocks=b["blocks"],
+                  block_count=b["count"])
+
+    md.update_bounds(all_pages=True)
+    a, e = buffers(), buffers()
+    torch.cuda.synchronize()
+    calls(e)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls(a)
+    for i in range(4):
+        qkv.copy_(w.normal(S, (Hq + 2 * Hkv) * D, dtype=BF16))
+        c.n_tokens[0] = 700 - 17 * i
+        c.n_pages[0] = (700 - 17 * i + 15) // 16
+        c.clock.add_(1)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        calls(e)
+        torch.cuda.synchronize()
+        for name in a:
+            assert torch.equal(a[name], e[name]), (i, name)
+    assert md.device_status() == 0
