@@ -1039,8 +1039,7 @@ md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a) {
     c.out_stride = a->out_stride;
     c.lse = a->lse;
     c.layer = layer;
-    c.splits = md::attend_splits(h->dm, h->n_cu);
-    c.part = static_cast<float*>(a->workspace);
+    md::attend_carve(h->dm, h->n_cu, a->workspace, &c);
     const OnDevice on(h->device);
     if (!on.ok) return MD_E_HIP;
     return md::launch_token(h->dm, h->v, h->sc, c, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;

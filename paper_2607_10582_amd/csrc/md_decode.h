@@ -24,16 +24,18 @@ struct TokenCall {
     int64_t out_stride;
     float* lse;
     int layer;
-    int splits;     // parts of every row
-    float* part;    // [S Hkv][splits][G][kPartWords] their results (splits > 1)
+    int units;      // stretches the rows are cut into
+    int32_t* count; // arrivals (zero between launches)
+    float* part;    // [units][2][G][kPartWords] partial results
 };
 
 // Partial result of one query head: unnormalised sums of the 128 dims, then
 // the maximum (base 2) and the sum of the weights.
 constexpr int kPartWords = kHeadDim + 4;
 
-int attend_splits(const Dims& dm, int n_cu);
+int attend_units(const Dims& dm, int n_cu);
 uint64_t attend_workspace(const Dims& dm, int n_cu);
+void attend_carve(const Dims& dm, int n_cu, void* workspace, TokenCall* c);
 hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, const TokenCall& c, hipStream_t st);
 
 hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a, int n_cu, hipStream_t st);
