@@ -1023,26 +1023,10 @@ md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a) {
         (a->out_type != MD_F32 && a->out_type != MD_BF16) || !aligned(a->lse, 4))
         return MD_E_INVALID;
     if (a->workspace == nullptr || !aligned(a->workspace, 16)) return MD_E_INVALID;
-    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
-    md::TokenCall c{};
-    c.q = a->q;
-    c.q_stride = a->q_stride;
-    c.new_k = a->new_k;
-    c.new_v = a->new_v;
-    c.kv_stride = a->kv_stride;
-    c.v_pool = a->v_pool;
-    c.blocks = a->blocks;
-    c.block_count = a->block_count;
-    c.max_blocks = a->max_blocks;
-    c.out_bf16 = a->out_type == MD_BF16;
-    c.out = a->out;
-    c.out_stride = a->out_stride;
-    c.lse = a->lse;
-    c.layer = layer;
-    md::attend_carve(h->dm, h->n_cu, a->workspace, &c);
+    if (h->dm.H > 0 || !md::attend_fits(h->dm)) return MD_E_UNSUPPORTED;
     const OnDevice on(h->device);
     if (!on.ok) return MD_E_HIP;
-    return md::launch_token(h->dm, h->v, h->sc, c, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+    return md::launch_token(h->dm, h->v, h->sc, h->n_cu, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
 }
 
 md_status md_key_bounds(md_handle h, int32_t all_pages, int8_t* bounds, int8_t* bound_exp) {

@@ -8,8 +8,20 @@ namespace md {
 
 constexpr int kMinExp = -100, kMaxExp = 100;   // exponents of bounds and query codes
 
-// One call's arrays (md_attend_args) and place.
+// What one call of the attention over the cache reads and writes: the parts
+// of the handle's dimensions and view that it needs (a few scalar registers,
+// not three structs' worth), and the call's arrays.
 struct TokenCall {
+    int S, Hq, Hkv, G, P, Pshift, MP, NP, aligned;
+    int layer;
+    size_t page_elems;      // elements of a page's keys, and of its values
+    const uint16_t* k_pool;
+    const uint8_t* region;
+    const int32_t* page_table;
+    const int32_t* n_pages;
+    const int32_t* n_tokens;
+    const uint8_t* page_format;
+    int32_t* status;
     const float* q;
     int64_t q_stride;
     const uint16_t* new_k;
@@ -23,9 +35,8 @@ struct TokenCall {
     void* out;
     int64_t out_stride;
     float* lse;
-    int layer;
-    int units;      // stretches the rows are cut into
-    int32_t* count; // arrivals (zero between launches)
+    int units;      // workgroups
+    int32_t* count; // [3 units] arrivals (zero between launches)
     float* part;    // [units][2][G][kPartWords] partial results
 };
 
@@ -33,10 +44,12 @@ struct TokenCall {
 // the maximum (base 2) and the sum of the weights.
 constexpr int kPartWords = kHeadDim + 4;
 
-int attend_units(const Dims& dm, int n_cu);
 uint64_t attend_workspace(const Dims& dm, int n_cu);
-void attend_carve(const Dims& dm, int n_cu, void* workspace, TokenCall* c);
-hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, const TokenCall& c, hipStream_t st);
+// Whether the sessions' rows at the page tables' capacity can be counted in
+// steps (int32).
+bool attend_fits(const Dims& dm);
+hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
+                        hipStream_t st);
 
 hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a, int n_cu, hipStream_t st);
 hipError_t launch_append_values(const Dims& dm, const View& v, const uint16_t* new_v, uint16_t* v_pool,

@@ -21,6 +21,7 @@
 // few hundred tokens by its chain of loads (counters, page table, keys).
 
 #include <algorithm>
+#include <type_traits>
 
 #include "md_arrive.h"
 #include "md_decode.h"
@@ -30,10 +31,15 @@ namespace md {
 
 namespace {
 
-constexpr int kTokWaves = 4;
-constexpr int kTokThreads = 64 * kTokWaves;
-constexpr int kMinUnitSteps = kTokWaves;   // a step is two tiles of 16 tokens, whose values meet in one product of 32
-constexpr int kJoin = 16;          // partial results that one workgroup joins
+// A step is two tiles of 16 tokens, whose values meet in one product of 32;
+// a cell is two steps per wave or more.
+constexpr int kMinWaveSteps = 2;
+constexpr int kStreamSteps = 8192;   // a line this long (128 MiB) is read past the caches
+constexpr int kJoin = 16;            // partial results that one workgroup joins
+
+__device__ __forceinline__ bool counts_ok(const TokenCall& c, int np, int nt) {
+    return np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
+}
 
 struct Desc {       // one 16-token tile, per lane
     int phys;       // page
@@ -64,7 +70,7 @@ __device__ __forceinline__ int tokens_before_holes(const uint8_t* region) {
 // Tile u of step t of a row: two tiles of its pages a step, then a step for
 // the new token.
 template <bool SPARSE, bool QT>
-__device__ __forceinline__ Desc tile_desc(const Dims& dm, const View& v, const TokenCall& c, const Row& r, int step, int u,
+__device__ __forceinline__ Desc tile_desc(const TokenCall& c, const Row& r, int step, int u,
                                           int& status) {
     Desc d{0, 0, 0};
     const int t = 2 * step + u;
@@ -72,11 +78,11 @@ __device__ __forceinline__ Desc tile_desc(const Dims& dm, const View& v, const T
         if (r.ok && c.new_k != nullptr && u == 0 && step == (r.tiles + 1) >> 1) d.live = -1;
         return d;
     }
-    const int per = dm.P >> 4;
-    int page = t >> (dm.Pshift - 4);
+    const int per = c.P >> 4;
+    int page = t >> (c.Pshift - 4);
     const int sub = t & (per - 1);
     if constexpr (SPARSE) {
-        const int32_t* list = c.blocks + ((size_t)r.s * dm.Hkv + r.kv) * c.max_blocks;
+        const int32_t* list = c.blocks + ((size_t)r.s * c.Hkv + r.kv) * c.max_blocks;
         const int o = page;
         page = list[o];
         if (page < 0 || page >= r.np || (o > 0 && page <= list[o - 1])) {
@@ -84,15 +90,15 @@ __device__ __forceinline__ Desc tile_desc(const Dims& dm, const View& v, const T
             return d;
         }
     }
-    const int p = v.page_table[(size_t)r.s * dm.MP + page];
-    if ((unsigned)p >= (unsigned)dm.NP) {
+    const int p = c.page_table[(size_t)r.s * c.MP + page];
+    if ((unsigned)p >= (unsigned)c.NP) {
         status |= kDevCorrupt;
         return d;
     }
     d.phys = p;
-    d.live = min(16, max(0, r.nt - (page * dm.P + 16 * sub)));
-    if (dm.aligned) d.live = min(d.live, tokens_before_holes(v.region + (size_t)p * dm.P + 16 * sub));
-    if constexpr (QT) d.quant = v.page_format[p];
+    d.live = min(16, max(0, r.nt - (page * c.P + 16 * sub)));
+    if (c.aligned) d.live = min(d.live, tokens_before_holes(c.region + (size_t)p * c.P + 16 * sub));
+    if constexpr (QT) d.quant = c.page_format[p];
     return d;
 }
 
@@ -115,380 +121,540 @@ __device__ __forceinline__ float2 get2(const float* p) {
     return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
 }
 
-// A thread's share of a row's result: eight dims of one query head, 16
-// threads a head.
+// A thread's share of a row's result: N dims of one query head.
+template <int N>
 struct Share {
-    float m, l, y[8];
+    float m, l, y[N];
 };
 
-__device__ __forceinline__ float* part_at(const Dims& dm, const TokenCall& c, int unit, int slot, int hh) {
-    return c.part + ((size_t)(2 * unit + slot) * dm.G + hh) * kPartWords;
+__device__ __forceinline__ float* part_at(const TokenCall& c, int cell, int slot, int hh) {
+    return c.part + ((size_t)(2 * cell + slot) * c.G + hh) * kPartWords;
 }
 
-__device__ __forceinline__ void part_store(float* p, int e8, const Share& r) {
+template <int N>
+__device__ __forceinline__ void part_store(float* p, int part, const Share<N>& r) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) put2(p + 8 * e8 + 2 * i, r.y[2 * i], r.y[2 * i + 1]);
-    if (e8 == 0) put2(p + kHeadDim, r.m, r.l);
+    for (int i = 0; i < N; i += 2) put2(p + N * part + i, r.y[i], r.y[i + 1]);
+    if (part == 0) put2(p + kHeadDim, r.m, r.l);
 }
 
-__device__ __forceinline__ Share part_load(const float* p, int e8) {
-    Share r;
+template <int N>
+__device__ __forceinline__ Share<N> part_load(const float* p, int part) {
+    Share<N> r;
     const float2 st = get2(p + kHeadDim);
     r.m = st.x;
     r.l = st.y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 w = get2(p + 8 * e8 + 2 * i);
-        r.y[2 * i] = w.x;
-        r.y[2 * i + 1] = w.y;
+    for (int i = 0; i < N; i += 2) {
+        const float2 w = get2(p + N * part + i);
+        r.y[i] = w.x;
+        r.y[i + 1] = w.y;
     }
     return r;
 }
 
-__device__ __forceinline__ void share_add(Share& a, const Share& b) {
+template <int N>
+__device__ __forceinline__ Share<N> no_share() {
+    Share<N> r;
+    r.m = -INFINITY;
+    r.l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.y[i] = 0.0f;
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ void share_add(Share<N>& a, const Share<N>& b) {
     const float M = fmaxf(a.m, b.m);
     const float fa = M == -INFINITY ? 0.0f : hw_exp2(a.m - M), fb = M == -INFINITY ? 0.0f : hw_exp2(b.m - M);
     a.m = M;
     a.l = a.l * fa + b.l * fb;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a.y[i] = fmaf(b.y[i], fb, a.y[i] * fa);
+    for (int i = 0; i < N; ++i) a.y[i] = fmaf(b.y[i], fb, a.y[i] * fa);
 }
 
-__device__ __forceinline__ void write_out(const Dims& dm, const TokenCall& c, const Row& r, int hh, int e8, const Share& a) {
+template <int N>
+__device__ __forceinline__ void write_out(const TokenCall& c, const Row& r, int hh, int part, const Share<N>& a) {
     const float inv = a.l > 0.0f ? 1.0f / a.l : a.l == 0.0f ? 0.0f : a.l;   // NaN stays NaN
-    const int64_t at = (int64_t)r.s * c.out_stride + (r.kv * dm.G + hh) * kHeadDim + 8 * e8;
-    if (c.out_bf16) {
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(c.out) + at) =
-            u32x4{pack_bf16(a.y[0] * inv, a.y[1] * inv), pack_bf16(a.y[2] * inv, a.y[3] * inv),
-                  pack_bf16(a.y[4] * inv, a.y[5] * inv), pack_bf16(a.y[6] * inv, a.y[7] * inv)};
-    } else {
-        f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(c.out) + at);
-        o[0] = f32x4{a.y[0] * inv, a.y[1] * inv, a.y[2] * inv, a.y[3] * inv};
-        o[1] = f32x4{a.y[4] * inv, a.y[5] * inv, a.y[6] * inv, a.y[7] * inv};
+    const int64_t at = (int64_t)r.s * c.out_stride + (r.kv * c.G + hh) * kHeadDim + N * part;
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        if (c.out_bf16) {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(c.out) + at + i) =
+                u32x2{pack_bf16(a.y[i] * inv, a.y[i + 1] * inv), pack_bf16(a.y[i + 2] * inv, a.y[i + 3] * inv)};
+        } else {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(c.out) + at + i) =
+                f32x4{a.y[i] * inv, a.y[i + 1] * inv, a.y[i + 2] * inv, a.y[i + 3] * inv};
+        }
     }
-    if (c.lse != nullptr && e8 == 0)
-        c.lse[(size_t)r.s * dm.Hq + r.kv * dm.G + hh] = (a.m + log2f(a.l)) * 0.69314718055994530942f;
+    if (c.lse != nullptr && part == 0)
+        c.lse[(size_t)r.s * c.Hq + r.kv * c.G + hh] = (a.m + log2f(a.l)) * 0.69314718055994530942f;
 }
 
 // The rows lie end to end on a line of steps of 32 tokens (sessions in order,
-// each session's KV heads one after another), and a unit, one workgroup, takes
-// an equal stretch of it, whatever the sessions' lengths: the whole of some
-// rows and parts of at most two.  A row in several units is joined by the
-// unit that finishes last: in groups of kJoin units by the last of each
+// each session's KV heads one after another), which is cut into cells, one
+// for each workgroup, whatever the sessions' lengths.  Where cells of the
+// line's even share each (or of kMinCellSteps) leave room for it, every row
+// is cut by itself, into the fewest cells of at most that length (rows of
+// equal length, mostly); else the line is, and a cell holds the whole of some
+// rows and parts of at most two.  A row in several cells is joined by the
+// workgroup that finishes last: in groups of kJoin cells by the last of each
 // group, then the groups by the last of those (arrivals, no waits).
 //
-// Within a stretch of one row the four waves take steps in turn.  The keys of
-// a wave's next step are requested as soon as this step's have been through
-// the matrix cores, its values after this step's, so about 12 KiB per wave
-// are under way at any time.  SPARSE: pages from the call's lists; QT: pages
-// may hold 8-bit codes.
-template <bool SPARSE, bool QT>
-__global__ void __launch_bounds__(kTokThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-k_token(Dims dm, View v, Scratch sc, TokenCall c) {
+// Within a cell's stretch of one row the waves take steps in turn.  The keys
+// of a wave's next step are requested as soon as this step's have been through
+// the matrix cores, its values after this step's, and the next stretch's first
+// step before this one's results are put together: 12 KiB per wave under way,
+// with which the CU's eight waves fill HBM (64 sessions of 32k tokens, two KV
+// heads: 2.15 GB in 335 us, 6.4 TB/s; a second step in registers, or twelve
+// waves, read no faster).  Two things cost a sixth each: a load behind a branch
+// turns the wait for the values into one for the next keys too, and cached
+// loads of a long line are 6 % slower than ones past the caches (short lines
+// the other way round: 54 MB that the cache still holds, 19 against 22 us).
+// Small cells at the end of the line, claimed from a queue by whichever
+// workgroup reads faster, cost more than they gave (390 us).
+//
+// What bounds short lines is the chain: counters, scan, page table, keys and
+// values (3 - 6 us), results through LDS, and where a row is cut its parts
+// through memory (4 us).
+// SPARSE: pages from the call's lists; QT: pages may hold 8-bit codes.
+template <int W, bool SPARSE, bool QT>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2)))
+k_token(TokenCall c) {
+    constexpr int kThreads = 64 * W;
+    constexpr int N = 32 / W;              // dims of a thread's share, 4 W threads a head
+    constexpr int kQ = W >= 4 ? 1 : 4 / W; // pieces of the query that a wave stages
+    using Mine = Share<N>;
     __shared__ __align__(16) u32x4 q_lds[3][4][64];
-    __shared__ __align__(16) f32x4 acc_lds[kTokWaves][8][64];
-    __shared__ float2 stat_lds[kTokWaves][16];
-    __shared__ int pref[kMaxSessions + 1];
+    __shared__ __align__(16) f32x4 acc_lds[W][8][64];
+    __shared__ float2 stat_lds[W][16];
     __shared__ int scan_lds[17];
     __shared__ int sh_last;
-    const int tid = threadIdx.x, lane = lane_id(), wv = tid >> 6;
+    extern __shared__ int2 session_lds[];
+    int2* held = session_lds;                             // [S] pages (-1: counters inconsistent) and slots in use
+    int* pref = reinterpret_cast<int*>(held + c.S);       // [S + 1] steps of one row of the sessions before
+    int* cpref = pref + c.S + 1;                          // [S + 1] cells of one row of the sessions before
+    const int tid = threadIdx.x, lane = lane_id(), wv = uni(tid >> 6);
     const int h = lane & 15, g = lane >> 4;
-    const int per = dm.P >> 4;
+    const int per = c.P >> 4;
     int status = 0;
-    // ---- the line: steps of each session's rows
-    {
-        int before = 0;
-        for (int b = 0; b < dm.S; b += kTokThreads) {
-            const int s = b + tid;
-            int n = 0;
-            if (s < dm.S) {
-                const int np = v.n_pages[s], nt = v.n_tokens[s];
-                const bool ok = counters_ok(np, nt, dm);
-                if (!ok) status = kDevCorrupt;
-                const int tiles = !ok ? 0 : SPARSE ? min(c.max_blocks, np) * per : (nt + 15) >> 4;
-                n = max(1, ((tiles + 1) >> 1) + (c.new_k != nullptr && ok ? 1 : 0));
-            }
-            int total;
-            const int ex = block_exclusive_scan(n, scan_lds, &total);
-            if (s < dm.S) pref[s] = before + ex;
-            before += total;
-        }
-        if (tid == 0) pref[dm.S] = before;
-        __syncthreads();
-    }
-    const int64_t T = (int64_t)pref[dm.S] * dm.Hkv;
-    const int64_t per_unit = max((int64_t)kMinUnitSteps, (T + c.units - 1) / c.units);
-    const int unit = blockIdx.x;
-    int64_t pos = per_unit * unit;
-    const int64_t end = min(T, pos + per_unit);
-    if (unit != 0) status = 0;   // one unit reports the counters
-
-    const size_t page_elems = (size_t)dm.LHkv * dm.P * kHeadDim;
-    const int hh = tid >> 4, e8 = tid & 15;   // this thread's share of a result
-    while (pos < end) {
-        // ---- the row at pos and the stretch of it that this unit walks
-        Row r;
-        r.s = find_session(pref, dm.S, (int)(pos / dm.Hkv));
-        const int steps = pref[r.s + 1] - pref[r.s];
-        const int64_t at_s = (int64_t)pref[r.s] * dm.Hkv;
-        r.kv = (int)((pos - at_s) / steps);
-        const int64_t row0 = at_s + (int64_t)r.kv * steps;
-        const int lo = (int)(pos - row0), hi = (int)min((int64_t)steps, end - row0);
-        r.np = v.n_pages[r.s];
-        r.nt = v.n_tokens[r.s];
-        r.ok = counters_ok(r.np, r.nt, dm);
-        if (!r.ok) r.np = r.nt = 0;
-        r.tiles = (r.nt + 15) >> 4;
-        if constexpr (SPARSE) {
-            const int most = min(c.max_blocks, r.np);
-            int n = c.block_count[(size_t)r.s * dm.Hkv + r.kv];
-            if (n < 0 || n > most) {
-                status |= MD_DEV_BAD_BLOCK;
-                n = min(max(n, 0), most);
-            }
-            r.tiles = n * per;
-        }
-        // ---- the heads' queries: three bf16 terms, exactly; wave j has dims 32 j + 8 g ..
-        f32x4 qa[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-        if (h < dm.G) {
-            const f32x4* qp = reinterpret_cast<const f32x4*>(c.q + (int64_t)r.s * c.q_stride +
-                                                             (r.kv * dm.G + h) * kHeadDim + 32 * wv + 8 * g);
-            qa[0] = qp[0];
-            qa[1] = qp[1];
-        }
-        const size_t tile_row = ((size_t)c.layer * dm.Hkv + r.kv) * dm.P * kHeadDim;   // elements into a page
-        const int nw = max(0, (hi - lo - wv + kTokWaves - 1) / kTokWaves);   // this wave's steps: lo + wv + 4 i
-        float m = -INFINITY, l = 0.0f;
-        f32x4 o[8];
+    // ---- the line and its cells
+    constexpr int kPer = kMaxSessions / kThreads;
+    int n[kPer], before = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < kPer; ++k) {
+        const int s = k * kThreads + tid;
+        n[k] = 0;
+        if (k * kThreads >= c.S) break;
+        if (s < c.S) {
+            const int np = c.n_pages[s], nt = c.n_tokens[s];
+            const bool ok = counts_ok(c, np, nt);
+            if (!ok && blockIdx.x == 0) status = kDevCorrupt;
+            held[s] = ok ? make_int2(np, nt) : make_int2(-1, 0);
+            const int tiles = !ok ? 0 : SPARSE ? min(c.max_blocks, np) * per : (nt + 15) >> 4;
+            n[k] = max(1, ((tiles + 1) >> 1) + (c.new_k != nullptr && ok ? 1 : 0));
+        }
+        int total;
+        const int ex = block_exclusive_scan(n[k], scan_lds, &total);
+        if (s < c.S) pref[s] = before + ex;
+        before += total;
+    }
+    const int T = uni(before) * c.Hkv;
+    const int big = max(kMinWaveSteps * W, (int)(((unsigned)T + c.units - 1) / (unsigned)c.units));
+    int cells = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int s = k * kThreads + tid;
+        if (k * kThreads >= c.S) break;
+        int total;
+        const int ex = block_exclusive_scan((int)((unsigned)(n[k] + big - 1) / (unsigned)big), scan_lds, &total);
+        if (s < c.S) cpref[s] = cells + ex;
+        cells += total;
+    }
+    if (tid == 0) {
+        pref[c.S] = before;
+        cpref[c.S] = cells;
+    }
+    __syncthreads();
+    cells = uni(cells) * c.Hkv;
+    const bool by_row = cells <= c.units;   // every row cut by itself
+    const int cell = blockIdx.x;
+    if (by_row ? cell >= cells : cell * big >= T) return;
+    const int hh = tid / (4 * W), ep = tid % (4 * W);   // this thread's share of a result
 
-        // descriptors of this wave's steps i .. i + 31: lane 2 k + u holds tile u of the k-th
+    // ---- one stretch: steps lo .. hi - 1 of row r
+    struct Stretch {
+        Row r;
+        int lo, hi;
+        int first, count;   // the row's cells
+        int next;           // the place on the line behind the stretch
+    };
+    // (past: reads past the caches, std::true_type or std::false_type)
+    auto run = [&](auto past) {
         Desc d;
-        auto describe = [&](int i) {
-            const int mine = lo + wv + (i + (lane >> 1)) * kTokWaves;
-            d = Desc{0, 0, 0};
-            if (mine < hi) d = tile_desc<SPARSE, QT>(dm, v, c, r, mine, lane & 1, status);
-        };
         u32x4 kt[2][4], vt[2][4];
-        auto elem_at = [&](int i, int u) {
-            const int phys = __builtin_amdgcn_readlane(d.phys, 2 * (i & 31) + u);
-            const int t = 2 * (lo + wv + i * kTokWaves) + u;
-            return (size_t)phys * page_elems + tile_row + (size_t)(t & (per - 1)) * 16 * kHeadDim;
+        f32x4 qa[kQ][2];
+        auto steps_of = [&](const Stretch& t) { return max(0, (t.hi - t.lo - wv + W - 1) / W); };
+        // descriptors of this wave's steps i .. i + 31 (lo + wv + 4 i ..): lane 2 k + u holds tile u of the k-th
+        auto describe = [&](const Stretch& t, int i) {
+            const int mine = t.lo + wv + (i + (lane >> 1)) * W;
+            d = Desc{0, 0, 0};
+            if (mine < t.hi) d = tile_desc<SPARSE, QT>(c, t.r, mine, lane & 1, status);
         };
-        auto load_k = [&](int i) {
+        auto elem_at = [&](const Stretch& t, int i, int u) {
+            const int phys = __builtin_amdgcn_readlane(d.phys, 2 * (i & 31) + u);
+            const int tile = 2 * (t.lo + wv + i * W) + u;
+            return (size_t)phys * c.page_elems +
+                   ((size_t)c.layer * c.Hkv + t.r.kv) * c.P * kHeadDim + (size_t)(tile & (per - 1)) * 16 * kHeadDim;
+        };
+        auto load_k = [&](const Stretch& t, int i) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint8_t* kp = reinterpret_cast<const uint8_t*>(v.k_pool + elem_at(i, u));
+                const gbytes kp = uni_ptr(c.k_pool + elem_at(t, i, u));
                 const bool codes = QT && __builtin_amdgcn_readlane(d.quant, 2 * (i & 31) + u) != 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)   // codes fill two loads; their scale sits at byte 2048
-                    kt[u][j] = *reinterpret_cast<const u32x4*>(kp + (QT && j >= 2 && codes ? 2048 : 1024 * j + 16 * lane));
-            }
-        };
-        auto load_v = [&](int i) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const u32x4* vp = reinterpret_cast<const u32x4*>(c.v_pool + elem_at(i, u)) + lane;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) vt[u][j] = vp[64 * j];
-            }
-        };
-        if (nw > 0) {
-            describe(0);
-            load_k(0);
-            load_v(0);
-        }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t a[3], b[3];
-                split3(qa[i >> 1][2 * (i & 1)], a[0], a[1], a[2]);
-                split3(qa[i >> 1][2 * (i & 1) + 1], b[0], b[1], b[2]);
-                w[i] = a[k] | (b[k] << 16);
-            }
-            q_lds[k][wv][lane] = w;
-        }
-        lds_sync();
-        for (int i = 0; i < nw; ++i) {
-            int live[2];
-            float qsc[2] = {1.0f, 1.0f};
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                live[u] = __builtin_amdgcn_readlane(d.live, 2 * (i & 31) + u);
-                if constexpr (QT) {
-                    if (__builtin_amdgcn_readlane(d.quant, 2 * (i & 31) + u)) {
-                        qsc[u] = __uint_as_float(__builtin_amdgcn_readfirstlane(kt[u][2][0]));
-                        kt[u][3] = codes_to_bf16<1>(kt[u][1]);
-                        kt[u][2] = codes_to_bf16<0>(kt[u][1]);
-                        kt[u][1] = codes_to_bf16<1>(kt[u][0]);
-                        kt[u][0] = codes_to_bf16<0>(kt[u][0]);
-                    }
+                for (int j = 0; j < 4; ++j) {   // codes fill two loads; their scale sits at byte 2048
+                    const gvec at = reinterpret_cast<gvec>(kp + (uint32_t)(QT && j >= 2 && codes ? 2048 : 1024 * j + 16 * lane));
+                    kt[u][j] = past.value ? __builtin_nontemporal_load(at) : *at;
                 }
             }
-            if (live[0] < 0) {   // the new token: every lane reads its dims, the other tokens count nothing
-                const uint16_t* nk = c.new_k + (int64_t)r.s * c.kv_stride + r.kv * kHeadDim;
-                const uint16_t* nv = c.new_v + (int64_t)r.s * c.kv_stride + r.kv * kHeadDim;
+        };
+        auto load_v = [&](const Stretch& t, int i) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const gbytes vp = uni_ptr(c.v_pool + elem_at(t, i, u));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    kt[0][j] = *reinterpret_cast<const u32x4*>(nk + 32 * j + 8 * g);
-                    vt[0][j] = u32x4{nv[32 * j + h], 0u, nv[32 * j + 16 + h], 0u};
+                    const gvec at = reinterpret_cast<gvec>(vp + (uint32_t)(1024 * j + 16 * lane));
+                    vt[u][j] = past.value ? __builtin_nontemporal_load(at) : *at;
                 }
-                live[0] = 1;
             }
-            f32x4 x[2];
+        };
+        // this cell's stretch at `pos` of the line, its query and this wave's
+        // first step requested
+        const int end = by_row ? 0 : min(T, (cell + 1) * big);
+        auto begin = [&](int pos) {
+            Stretch t;
+            Row& r = t.r;
+            const int* starts = by_row ? cpref : pref;   // by rows: pos is the cell
+            r.s = uni(find_session(starts, c.S, (int)((unsigned)pos / (unsigned)c.Hkv)));
+            const int length = uni(starts[r.s + 1] - starts[r.s]), at_s = uni(starts[r.s]) * c.Hkv;
+            r.kv = (int)((unsigned)(pos - at_s) / (unsigned)length);
+            const int row0 = at_s + r.kv * length;
+            if (by_row) {
+                const int steps = uni(pref[r.s + 1] - pref[r.s]);
+                t.first = row0;
+                t.count = length;
+                const int i = pos - row0;   // (steps * count fits: at most 2^15 steps and a cell per workgroup)
+                t.lo = (int)((unsigned)(steps * i) / (unsigned)length);
+                t.hi = (int)((unsigned)(steps * (i + 1)) / (unsigned)length);
+                t.next = end;
+            } else {
+                t.lo = pos - row0;
+                t.hi = min(length, end - row0);
+                t.first = (int)((unsigned)row0 / (unsigned)big);
+                t.count = (int)((unsigned)(row0 + length - 1) / (unsigned)big) - t.first + 1;
+                t.next = row0 + t.hi;
+            }
+            r.np = uni(max(0, held[r.s].x));
+            r.nt = uni(held[r.s].y);
+            r.ok = uni(held[r.s].x) >= 0;
+            r.tiles = (r.nt + 15) >> 4;
+            if constexpr (SPARSE) {
+                const int most = min(c.max_blocks, r.np);
+                int n = c.block_count[(size_t)r.s * c.Hkv + r.kv];
+                if (n < 0 || n > most) {
+                    status |= MD_DEV_BAD_BLOCK;
+                    n = min(max(n, 0), most);
+                }
+                r.tiles = n * per;
+            }
+            // wave w stages dims 32 j + 8 g .. of the heads' queries, j = w, w + W ..
 #pragma unroll
-            for (int u = 0; u < 2; ++u) x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < kQ; ++k) {
+                const int j = wv + k * W;
+                qa[k][0] = qa[k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (h < c.G && j < 4) {
+                    const f32x4* qp = reinterpret_cast<const f32x4*>(c.q + (int64_t)r.s * c.q_stride +
+                                                                     (r.kv * c.G + h) * kHeadDim + 32 * j + 8 * g);
+                    qa[k][0] = qp[0];
+                    qa[k][1] = qp[1];
+                }
+            }
+            if (steps_of(t) > 0) {
+                describe(t, 0);
+                load_k(t, 0);
+                load_v(t, 0);
+            }
+            return t;
+        };
+
+        Stretch t = begin(by_row ? cell : cell * big);
+        for (bool more = true; more;) {
+            // ---- the heads' queries: three bf16 terms, exactly
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int y = 0; y < kQ; ++y) {
+                const int j = wv + y * W;
+                if (j >= 4) break;
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {
-                    const bf16x8 bq = __builtin_bit_cast(bf16x8, q_lds[k][j][lane]);
+                    u32x4 w;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt[u][j]), bq, x[u], 0, 0, 0);
-                }
-            if (i + 1 < nw) {
-                if (((i + 1) & 31) == 0) describe(i + 1);
-                load_k(i + 1);
-            }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    x[u][k] = 4 * g + k < live[u] ? x[u][k] * (QT ? kLogitScale * qsc[u] : kLogitScale) : -INFINITY;
-                    mx = fmaxf(mx, x[u][k]);
-                }
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            if (__any(mx > m)) {
-                const float mn = fmaxf(m, mx);
-                const float f = mn == -INFINITY ? 1.0f : hw_exp2(m - mn);
-                l *= f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] *= f;
-                m = mn;
-            }
-            const float ms = m == -INFINITY ? 0.0f : m;
-            uint32_t ph[4], pl[4];   // weights as two bf16 terms
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float p[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    p[k] = hw_exp2(x[u][k] - ms);
-                    l += p[k];
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t w = pack_bf16(p[2 * k], p[2 * k + 1]);
-                    ph[2 * u + k] = w;
-                    pl[2 * u + k] = pack_bf16(p[2 * k] - bf16_lo(w), p[2 * k + 1] - bf16_hi(w));
-                }
-                // a slot that does not count may hold anything, and 0 times
-                // an infinity or NaN is NaN: its values become 0
-                if (live[u] < 16) {
-                    const int k4 = live[u] - 4 * g;   // tokens of this lane's four that count
-                    const uint32_t m0 = k4 >= 2 ? 0xFFFFFFFFu : k4 == 1 ? 0x0000FFFFu : 0u;
-                    const uint32_t m1 = k4 >= 4 ? 0xFFFFFFFFu : k4 == 3 ? 0x0000FFFFu : 0u;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) vt[u][j] = vt[u][j] & u32x4{m0, m1, m0, m1};
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t a[3], b[3];
+                        split3(qa[y][i >> 1][2 * (i & 1)], a[0], a[1], a[2]);
+                        split3(qa[y][i >> 1][2 * (i & 1) + 1], b[0], b[1], b[2]);
+                        w[i] = a[k] | (b[k] << 16);
+                    }
+                    q_lds[k][j][lane] = w;
                 }
             }
-            const bf16x8 bh = __builtin_bit_cast(bf16x8, u32x4{ph[0], ph[1], ph[2], ph[3]});
-            const bf16x8 bl = __builtin_bit_cast(bf16x8, u32x4{pl[0], pl[1], pl[2], pl[3]});
+            lds_sync();
+            float m = -INFINITY, l = 0.0f;
+            f32x4 o[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int nw = steps_of(t);
+            for (int i = 0; i < nw; ++i) {
+                int live[2];
+                float qsc[2] = {1.0f, 1.0f};
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const bf16x8 a = __builtin_bit_cast(
-                        bf16x8, u32x4{vt[0][j][2 * e], vt[0][j][2 * e + 1], vt[1][j][2 * e], vt[1][j][2 * e + 1]});
-                    o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bh, o[2 * j + e], 0, 0, 0);
-                    o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bl, o[2 * j + e], 0, 0, 0);
+                for (int u = 0; u < 2; ++u) {
+                    live[u] = __builtin_amdgcn_readlane(d.live, 2 * (i & 31) + u);
+                    if constexpr (QT) {
+                        if (__builtin_amdgcn_readlane(d.quant, 2 * (i & 31) + u)) {
+                            qsc[u] = __uint_as_float(__builtin_amdgcn_readfirstlane(kt[u][2][0]));
+                            kt[u][3] = codes_to_bf16<1>(kt[u][1]);
+                            kt[u][2] = codes_to_bf16<0>(kt[u][1]);
+                            kt[u][1] = codes_to_bf16<1>(kt[u][0]);
+                            kt[u][0] = codes_to_bf16<0>(kt[u][0]);
+                        }
+                    }
                 }
-            if (i + 1 < nw) load_v(i + 1);
-        }
-        // ---- the waves' results meet
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (g == 0) stat_lds[wv][h] = make_float2(m, l);
+                if (live[0] < 0) {   // the new token: every lane reads its dims, the other tokens count nothing
+                    const uint16_t* nk = c.new_k + (int64_t)t.r.s * c.kv_stride + t.r.kv * kHeadDim;
+                    const uint16_t* nv = c.new_v + (int64_t)t.r.s * c.kv_stride + t.r.kv * kHeadDim;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc_lds[wv][i][lane] = o[i];
-        lds_sync();
-        Share mine{-INFINITY, 0.0f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+                    for (int j = 0; j < 4; ++j) {
+                        kt[0][j] = *reinterpret_cast<const u32x4*>(nk + 32 * j + 8 * g);
+                        vt[0][j] = u32x4{nv[32 * j + h], 0u, nv[32 * j + 16 + h], 0u};
+                    }
+                    live[0] = 1;
+                }
+                // (the query terms are read from LDS in every step: kept over the
+                // steps they would take 48 registers)
+                asm volatile("" ::: "memory");
+                u32x4 bq[4][3];
 #pragma unroll
-        for (int w = 0; w < kTokWaves; ++w) {
-            const float2 st = stat_lds[w][hh];
-            Share b{st.x, st.y, {}};
-            // dim 8 e8 + i: tile e8 / 2, rows 8 (e8 & 1) + i, lane group (row / 4)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int q4 = 0; q4 < 2; ++q4) {
-                const f32x4 a = acc_lds[w][e8 >> 1][(2 * (e8 & 1) + q4) * 16 + hh];
+                    for (int k = 0; k < 3; ++k) bq[j][k] = q_lds[k][j][lane];
+                __builtin_amdgcn_sched_barrier(0);   // all of them before the products, not each before its own
+                f32x4 x[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) b.y[4 * q4 + i] = a[i];
+                for (int u = 0; u < 2; ++u) x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                __builtin_bit_cast(bf16x8, kt[u][j]), __builtin_bit_cast(bf16x8, bq[j][k]), x[u], 0, 0, 0);
+                // (unconditional: loads behind a branch would make the wait for the
+                // values one for these keys too; behind the last step it reads
+                // that step's tiles again, out of the cache)
+                const int nx = min(i + 1, nw - 1);
+                if ((nx & 31) == 0 && nx > i) describe(t, nx);
+                load_k(t, nx);
+                float mx = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        x[u][k] = 4 * g + k < live[u] ? x[u][k] * (QT ? kLogitScale * qsc[u] : kLogitScale) : -INFINITY;
+                        mx = fmaxf(mx, x[u][k]);
+                    }
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                if (__any(mx > m)) {
+                    const float mn = fmaxf(m, mx);
+                    const float f = mn == -INFINITY ? 1.0f : hw_exp2(m - mn);
+                    l *= f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] *= f;
+                    m = mn;
+                }
+                const float ms = m == -INFINITY ? 0.0f : m;
+                uint32_t ph[4], pl[4];   // weights as two bf16 terms
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float p[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        p[k] = hw_exp2(x[u][k] - ms);
+                        l += p[k];
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t w = pack_bf16(p[2 * k], p[2 * k + 1]);
+                        ph[2 * u + k] = w;
+                        pl[2 * u + k] = pack_bf16(p[2 * k] - bf16_lo(w), p[2 * k + 1] - bf16_hi(w));
+                    }
+                    // a slot that does not count may hold anything, and 0 times
+                    // an infinity or NaN is NaN: its values become 0
+                    if (live[u] < 16) {
+                        const int k4 = live[u] - 4 * g;   // tokens of this lane's four that count
+                        const uint32_t m0 = k4 >= 2 ? 0xFFFFFFFFu : k4 == 1 ? 0x0000FFFFu : 0u;
+                        const uint32_t m1 = k4 >= 4 ? 0xFFFFFFFFu : k4 == 3 ? 0x0000FFFFu : 0u;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) vt[u][j] = vt[u][j] & u32x4{m0, m1, m0, m1};
+                    }
+                }
+                const bf16x8 bh = __builtin_bit_cast(bf16x8, u32x4{ph[0], ph[1], ph[2], ph[3]});
+                const bf16x8 bl = __builtin_bit_cast(bf16x8, u32x4{pl[0], pl[1], pl[2], pl[3]});
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const bf16x8 a = __builtin_bit_cast(
+                            bf16x8, u32x4{vt[0][j][2 * e], vt[0][j][2 * e + 1], vt[1][j][2 * e], vt[1][j][2 * e + 1]});
+                        o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bh, o[2 * j + e], 0, 0, 0);
+                        o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bl, o[2 * j + e], 0, 0, 0);
+                    }
+                load_v(t, nx);
             }
-            share_add(mine, b);
-        }
-        pos = row0 + hi;
-        // ---- the row's other units
-        const int first = (int)(row0 / per_unit), last = (int)((row0 + steps - 1) / per_unit);
-        if (first == last) {
-            if (hh < dm.G) write_out(dm, c, r, hh, e8, mine);
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (g == 0) stat_lds[wv][h] = make_float2(m, l);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc_lds[wv][i][lane] = o[i];
+            // ---- the cell's next row is requested
+            const Stretch done = t;
+            more = t.next < end;
+            if (more) t = begin(t.next);
+            // ---- the waves' results meet
+            lds_sync();
+            Mine mine = no_share<N>();
+#pragma unroll
+            for (int w = 0; w < W; ++w) {   // dims N ep ..: tile (dim / 16), lane group (dim / 4) & 3
+                Mine b;
+                b.m = stat_lds[w][hh].x;
+                b.l = stat_lds[w][hh].y;
+#pragma unroll
+                for (int x = 0; x < N; x += 4) {
+                    const int e = N * ep + x;
+                    const f32x4 a = acc_lds[w][e >> 4][((e >> 2) & 3) * 16 + hh];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b.y[x + i] = a[i];
+                }
+                share_add(mine, b);
+            }
+            // ---- the row's other cells
+            const int first = done.first, n = done.count;
+            if (n == 1) {
+                if (hh < c.G) write_out(c, done.r, hh, ep, mine);
+                lds_sync();   // the LDS is reused
+                continue;
+            }
+            // A cell has at most two rows that others share: one begun before it
+            // (slot 1) and one that goes on behind it (slot 0).
+            const int i = cell - first;
+            auto slot_of = [&](int k) { return k == 0 ? 0 : 1; };
+            if (hh < c.G) part_store(part_at(c, cell, slot_of(i), hh), ep, mine);
+            auto arrived_last = [&](int* count, int want) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (tid == 0) sh_last = arrive_last(count, arrive(count), want) ? 1 : 0;
+                __syncthreads();
+                return sh_last != 0;
+            };
+            // The sum of n partial results, `step` cells apart: all threads load,
+            // gp of each `heads` threads' groups a part of them, and the groups
+            // meet in LDS.
+            const int heads = c.G <= 1 ? 1 : c.G <= 2 ? 2 : c.G <= 4 ? 4 : c.G <= 8 ? 8 : 16;
+            auto sum_parts = [&](int cell0, int k0, int step, int count) {
+                Mine sum = no_share<N>();
+                const int head = hh & (heads - 1), gp = 16 / heads;
+                if (head < c.G) {
+#pragma unroll 8
+                    for (int k = hh / heads; k < count; k += gp)
+                        share_add(sum, part_load<N>(part_at(c, cell0 + k * step, slot_of(k0 + k * step), head), ep));
+                }
+                // (the groups' sums reach the first one by halves, so that they fit the LDS of the waves' results)
+                for (int half = gp / 2; half > 0; half /= 2) {
+                    float* lds = reinterpret_cast<float*>(acc_lds) + (hh & (half * heads - 1)) * 4 * W * (N + 2) + ep * (N + 2);
+                    lds_sync();
+                    if (hh >= half * heads && hh < 2 * half * heads) {
+                        lds[0] = sum.m;
+                        lds[1] = sum.l;
+#pragma unroll
+                        for (int x = 0; x < N; ++x) lds[2 + x] = sum.y[x];
+                    }
+                    lds_sync();
+                    if (hh < half * heads) {
+                        Mine b;
+                        b.m = lds[0];
+                        b.l = lds[1];
+#pragma unroll
+                        for (int x = 0; x < N; ++x) b.y[x] = lds[2 + x];
+                        share_add(sum, b);
+                    }
+                }
+                return sum;
+            };
+            const int i0 = i / kJoin * kJoin, members = min(kJoin, n - i0);
+            bool go = arrived_last(c.count + 2 * (first + i0) + slot_of(i0), members);
+            if (go) {
+                Mine sum = sum_parts(first + i0, i0, 1, members);
+                const int groups = (n + kJoin - 1) / kJoin;
+                if (groups > 1) {
+                    if (hh < c.G) part_store(part_at(c, first + i0, slot_of(i0), hh), ep, sum);
+                    go = arrived_last(c.count + 2 * c.units + first, groups);
+                    if (go) sum = sum_parts(first, 0, kJoin, groups);
+                }
+                if (go && hh < c.G) write_out(c, done.r, hh, ep, sum);
+            }
             lds_sync();   // the LDS is reused
-            continue;
         }
-        // A unit has at most two rows that others share: one begun before it
-        // (slot 1) and one that goes on behind it (slot 0).
-        const int i = unit - first, n = last - first + 1;
-        auto slot_of = [&](int k) { return k == 0 ? 0 : 1; };
-        if (hh < dm.G) part_store(part_at(dm, c, unit, slot_of(i), hh), e8, mine);
-        auto arrived_last = [&](int* count, int want) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (tid == 0) sh_last = arrive_last(count, arrive(count), want) ? 1 : 0;
-            __syncthreads();
-            return sh_last != 0;
-        };
-        const int i0 = i / kJoin * kJoin, members = min(kJoin, n - i0);
-        bool go = arrived_last(c.count + 2 * (first + i0) + slot_of(i0), members);
-        if (go) {
-            Share sum{-INFINITY, 0.0f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-            if (hh < dm.G) {
-#pragma unroll 4
-                for (int k = 0; k < members; ++k)
-                    share_add(sum, part_load(part_at(dm, c, first + i0 + k, slot_of(i0 + k), hh), e8));
-            }
-            const int groups = (n + kJoin - 1) / kJoin;
-            if (groups > 1) {
-                if (hh < dm.G) part_store(part_at(dm, c, first + i0, slot_of(i0), hh), e8, sum);
-                go = arrived_last(c.count + 2 * c.units + first, groups);
-                if (go && hh < dm.G) {
-                    sum = Share{-INFINITY, 0.0f, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-#pragma unroll 4
-                    for (int k = 0; k < groups; ++k)
-                        share_add(sum, part_load(part_at(dm, c, first + k * kJoin, slot_of(k * kJoin), hh), e8));
-                }
-            }
-            if (go && hh < dm.G) write_out(dm, c, r, hh, e8, sum);
-        }
-    }
-    if (status != 0) atomicOr(sc.status, status);
+    };
+    if (T >= kStreamSteps) run(std::true_type{}); else run(std::false_type{});
+    if (status != 0) atomicOr(c.status, status);
+}
+
+template <int W>
+const void* token_kernel(bool sparse, bool codes) {
+    return sparse ? (codes ? reinterpret_cast<const void*>(&k_token<W, true, true>)
+                           : reinterpret_cast<const void*>(&k_token<W, true, false>))
+                  : (codes ? reinterpret_cast<const void*>(&k_token<W, false, true>)
+                           : reinterpret_cast<const void*>(&k_token<W, false, false>));
 }
 
 }  // namespace
 
-// Units: two workgroups per CU, fewer where the page tables' capacity leaves
-// them less than a step per wave.
-int attend_units(const Dims& dm, int n_cu) {
-    const int64_t steps = (int64_t)dm.S * dm.Hkv * ((((int64_t)dm.MP * dm.P + 15) / 16 + 1) / 2 + 1);
-    return (int)std::min<int64_t>(2 * n_cu, (steps + kMinUnitSteps - 1) / kMinUnitSteps);
+// Waves of a workgroup; there are eight waves a CU either way, fewer where the
+// page tables' capacity leaves the workgroups less than the shortest cell.
+// Four, as a rule.  Two where each CU has eight rows or more, most of them
+// whole in one cell (4,096 rows of 5 - 60 tokens: 44 against 61 us, of about
+// 1,000: 359 against 373).  Eight where a few long rows are cut into half as
+// many parts to join (two rows of 131k tokens: 37 against 41 us; 32 rows of
+// 32k: 82 either way).
+static int attend_waves(const Dims& dm, int n_cu) {
+    const int rows = dm.S * dm.Hkv;
+    if (rows >= 8 * n_cu) return 2;
+    return rows * 16 <= n_cu && (int64_t)dm.MP * dm.P >= 16384 ? 8 : 4;
 }
 
-// Counters (arrivals at each unit's two slots, and at a row's groups), then
-// two partial results per unit.
+static int attend_units(const Dims& dm, int n_cu) {
+    const int W = attend_waves(dm, n_cu), shortest = kMinWaveSteps * W;
+    const int64_t steps = (((int64_t)dm.MP * dm.P + 15) / 16 + 1) / 2 + 1;   // of a row
+    const int64_t cells = (int64_t)dm.S * dm.Hkv * ((steps + shortest - 1) / shortest);
+    return (int)std::min<int64_t>((int64_t)n_cu * 8 / W, cells);
+}
+
+// Counters (arrivals at each cell's two slots, and at a row's groups), then
+// two partial results per cell.
 static size_t count_words(int units) { return ((size_t)3 * units + 63) / 64 * 64; }
 
 uint64_t attend_workspace(const Dims& dm, int n_cu) {
@@ -496,23 +662,54 @@ uint64_t attend_workspace(const Dims& dm, int n_cu) {
     return (count_words(u) + (uint64_t)2 * u * dm.G * kPartWords) * sizeof(float);
 }
 
-void attend_carve(const Dims& dm, int n_cu, void* workspace, TokenCall* c) {
-    c->units = attend_units(dm, n_cu);
-    c->count = static_cast<int32_t*>(workspace);
-    c->part = static_cast<float*>(workspace) + count_words(c->units);
+bool attend_fits(const Dims& dm) {
+    return (int64_t)dm.S * dm.Hkv * ((int64_t)dm.MP * dm.P / 32 + 2) < (int64_t)1 << 31;
 }
 
-hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, const TokenCall& c, hipStream_t st) {
-    Dims d = dm;
-    View vv = v;
-    Scratch ss = sc;
-    TokenCall cc = c;
-    void* args[] = {&d, &vv, &ss, &cc};
-    const void* fn = c.blocks != nullptr ? (dm.quant ? reinterpret_cast<const void*>(&k_token<true, true>)
-                                                     : reinterpret_cast<const void*>(&k_token<true, false>))
-                                         : (dm.quant ? reinterpret_cast<const void*>(&k_token<false, true>)
-                                                     : reinterpret_cast<const void*>(&k_token<false, false>));
-    return hipLaunchKernel(fn, dim3((unsigned)c.units), dim3(kTokThreads), args, 0, st);
+hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
+                        hipStream_t st) {
+    TokenCall c{};
+    c.S = dm.S;
+    c.Hq = dm.Hq;
+    c.Hkv = dm.Hkv;
+    c.G = dm.G;
+    c.P = dm.P;
+    c.Pshift = dm.Pshift;
+    c.MP = dm.MP;
+    c.NP = dm.NP;
+    c.aligned = dm.aligned;
+    c.layer = layer;
+    c.page_elems = (size_t)dm.LHkv * dm.P * kHeadDim;
+    c.k_pool = v.k_pool;
+    c.region = v.region;
+    c.page_table = v.page_table;
+    c.n_pages = v.n_pages;
+    c.n_tokens = v.n_tokens;
+    c.page_format = v.page_format;
+    c.status = sc.status;
+    c.q = a.q;
+    c.q_stride = a.q_stride;
+    c.new_k = a.new_k;
+    c.new_v = a.new_v;
+    c.kv_stride = a.kv_stride;
+    c.v_pool = a.v_pool;
+    c.blocks = a.blocks;
+    c.block_count = a.block_count;
+    c.max_blocks = a.max_blocks;
+    c.out_bf16 = a.out_type == MD_BF16;
+    c.out = a.out;
+    c.out_stride = a.out_stride;
+    c.lse = a.lse;
+    c.units = attend_units(dm, n_cu);
+    c.count = static_cast<int32_t*>(a.workspace);
+    c.part = static_cast<float*>(a.workspace) + count_words(c.units);
+    void* args[] = {&c};
+    const int W = attend_waves(dm, n_cu);
+    const bool sparse = a.blocks != nullptr, codes = dm.quant != 0;
+    const void* fn = W == 8 ? token_kernel<8>(sparse, codes) : W == 4 ? token_kernel<4>(sparse, codes)
+                                                             : token_kernel<2>(sparse, codes);
+    const unsigned lds = (unsigned)(dm.S * sizeof(int2) + 2 * (dm.S + 1) * sizeof(int));
+    return hipLaunchKernel(fn, dim3((unsigned)c.units), dim3(64 * W), args, lds, st);
 }
 
 }  // namespace md
