@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libmemdecay.so")
@@ -103,6 +104,13 @@ class md_select_args(ctypes.Structure):
                 ("workspace", ctypes.c_void_p)]
 
 
+# The same three as bytes, packed in one step: what a call of a few
+# microseconds passes (a ctypes.Structure takes longer to fill than the call).
+ROPE_ARGS = struct.Struct("@PqiiPPfiPPiPqPPq")
+ATTEND_ARGS = struct.Struct("@PqPPqPPPiiPqPP")
+SELECT_ARGS = struct.Struct("@PqPPiiiPPP")
+
+
 class MemDecayError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
@@ -184,15 +192,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.md_observe_path.restype = i32
     lib.md_observe_path.argtypes = [vp, ctypes.POINTER(i32)]
     lib.md_norm_rope.restype = i32
-    lib.md_norm_rope.argtypes = [vp, ctypes.POINTER(md_rope_args)]
+    lib.md_norm_rope.argtypes = [vp, vp]   # a struct's address, or its bytes
     lib.md_append_values.restype = i32
     lib.md_append_values.argtypes = [vp, vp, vp]
     lib.md_attend_token.restype = i32
-    lib.md_attend_token.argtypes = [vp, i32, ctypes.POINTER(md_attend_args)]
+    lib.md_attend_token.argtypes = [vp, i32, vp]
     lib.md_key_bounds.restype = i32
     lib.md_key_bounds.argtypes = [vp, i32, vp, vp]
     lib.md_select_blocks.restype = i32
-    lib.md_select_blocks.argtypes = [vp, i32, ctypes.POINTER(md_select_args)]
+    lib.md_select_blocks.argtypes = [vp, i32, vp]
     lib.md_decode_workspace.restype = i32
     lib.md_decode_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
     lib.md_destroy.restype = i32
@@ -335,24 +343,30 @@ def md_observe_path(h: int) -> dict:
             "steady_ranges": int(out[3])}
 
 
-def md_norm_rope(h: int, args: md_rope_args) -> int:
-    return _check("md_norm_rope", load_library().md_norm_rope(h, ctypes.byref(args)))
+def _arg(args):
+    return args if isinstance(args, bytes) else ctypes.byref(args)
+
+
+def md_norm_rope(h: int, args) -> int:
+    """args: md_rope_args, or its fields packed by ROPE_ARGS (so for the other
+    two calls with an argument struct)."""
+    return _check("md_norm_rope", load_library().md_norm_rope(h, _arg(args)))
 
 
 def md_append_values(h: int, new_v: int, v_pool: int) -> int:
     return _check("md_append_values", load_library().md_append_values(h, new_v, v_pool))
 
 
-def md_attend_token(h: int, layer: int, args: md_attend_args) -> int:
-    return _check("md_attend_token", load_library().md_attend_token(h, layer, ctypes.byref(args)))
+def md_attend_token(h: int, layer: int, args) -> int:
+    return _check("md_attend_token", load_library().md_attend_token(h, layer, _arg(args)))
 
 
 def md_key_bounds(h: int, all_pages: int, bounds: int, bound_exp: int) -> int:
     return _check("md_key_bounds", load_library().md_key_bounds(h, all_pages, bounds, bound_exp))
 
 
-def md_select_blocks(h: int, layer: int, args: md_select_args) -> int:
-    return _check("md_select_blocks", load_library().md_select_blocks(h, layer, ctypes.byref(args)))
+def md_select_blocks(h: int, layer: int, args) -> int:
+    return _check("md_select_blocks", load_library().md_select_blocks(h, layer, _arg(args)))
 
 
 def md_decode_workspace(h: int):

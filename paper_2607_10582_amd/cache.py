@@ -254,16 +254,11 @@ class MemDecay:
         # work space of the decode operators (one per handle: calls on its
         # stream run one after another)
         self._attend_ws = self._select_ws = None
+        self._device = cache.k_pool.get_device()
         if cache.v_pool is not None:   # now, so that a captured call allocates nothing
             self._workspace(True)
         if cache.key_bounds is not None:
             self._workspace(False)
-
-    def _here(self, *tensors):
-        dev = self.cache.k_pool.device
-        for t in tensors:
-            if t is not None and t.device != dev:
-                raise ValueError(f"expected a tensor on {dev}, got one on {t.device}")
 
     def _workspace(self, attend: bool) -> torch.Tensor:
         ws = self._attend_ws if attend else self._select_ws
@@ -317,7 +312,9 @@ class MemDecay:
         self.score(page_score=page_scores)
         self.select_compact()
 
-    # ---- what a decode engine runs around the step (memdecay.h)
+    # ---- what a decode engine runs around the step (memdecay.h).  A call of
+    # a few sessions takes the device less than 10 us, so the checks keep to
+    # comparisons of the tensors' shapes, strides, types and devices.
     def norm_rope(self, qkv: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor,
                   v_out: Optional[torch.Tensor] = None, *, q_weight: Optional[torch.Tensor] = None,
                   k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -331,45 +328,41 @@ class MemDecay:
         q_weight, k_weight [d]: None leaves those heads as they are.
         inv_freq float64 [r / 2]: the first r elements of each head turn (None:
         none).  position int32 [n]; None: each session's clock (n = S)."""
-        c = self.cache
-        self._here(qkv, q_out, k_out, v_out, q_weight, k_weight, inv_freq, position)
+        c, dev = self.cache, self._device
         n = qkv.shape[0]
-        half = 0 if inv_freq is None else inv_freq.numel()
-        if qkv.dim() != 2 or qkv.shape[1] != (c.Hq + 2 * c.Hkv) * c.d:
-            raise ValueError("qkv holds the query, key and value heads of a row side by side")
-        if (v_out is not None and _stride(v_out, torch.bfloat16, n, c.Hkv, c.d) !=
-                _stride(k_out, torch.bfloat16, n, c.Hkv, c.d)):
-            raise ValueError("k_out and v_out have rows the same distance apart")
-        if position is not None and position.numel() != n:
-            raise ValueError("one position per row")
-        for w in (q_weight, k_weight):
-            if w is not None and w.numel() != c.d:
-                raise ValueError("one weight per element of a head")
+        if qkv.dtype not in TYPES:
+            raise ValueError(f"expected float32, bfloat16 or float16 rows, got {qkv.dtype}")
         if n == 0:
             return
-        B.md_norm_rope(self.handle, B.md_rope_args(
-            qkv=_rows(qkv), qkv_stride=_pitch(qkv), qkv_type=_type(qkv), n_rows=n,
-            q_weight=None if q_weight is None else _ptr(q_weight, torch.float32),
-            k_weight=None if k_weight is None else _ptr(k_weight, torch.float32), eps=eps, rope_dims=2 * half,
-            inv_freq=None if half == 0 else _ptr(inv_freq, torch.float64),
-            position=None if position is None else _ptr(position, torch.int32), interleaved=int(interleaved),
-            q_out=q_out.data_ptr(), q_stride=_stride(q_out, torch.float32, n, c.Hq, c.d), k_out=k_out.data_ptr(),
-            v_out=None if v_out is None else v_out.data_ptr(),
-            kv_stride=_stride(k_out, torch.bfloat16, n, c.Hkv, c.d)))
+        qkv_at, qkv_pitch = _rows(qkv, qkv.dtype, n, c.Hq + 2 * c.Hkv, c.d, dev)
+        q_at, q_pitch = _rows(q_out, torch.float32, n, c.Hq, c.d, dev)
+        k_at, kv_pitch = _rows(k_out, torch.bfloat16, n, c.Hkv, c.d, dev)
+        v_at = 0
+        if v_out is not None:
+            v_at, v_pitch = _rows(v_out, torch.bfloat16, n, c.Hkv, c.d, dev)
+            if v_pitch != kv_pitch:
+                raise ValueError("k_out and v_out have rows the same distance apart")
+        B.md_norm_rope(self.handle, B.ROPE_ARGS.pack(
+            qkv_at, qkv_pitch, TYPES[qkv.dtype], n,
+            0 if q_weight is None else _flat(q_weight, torch.float32, c.d, dev),
+            0 if k_weight is None else _flat(k_weight, torch.float32, c.d, dev), eps,
+            0 if inv_freq is None else 2 * inv_freq.numel(),
+            0 if inv_freq is None else _flat(inv_freq, torch.float64, inv_freq.numel(), dev),
+            0 if position is None else _flat(position, torch.int32, n, dev), int(interleaved), q_at, q_pitch, k_at, v_at,
+            kv_pitch))
 
     def append_values(self, new_v: torch.Tensor):
         """The values bf16 [S][L][Hkv][d] of the tokens that the last observe
         appended (before anything is compacted)."""
         c = self.cache
-        self._here(new_v, c.v_pool)
-        if new_v.numel() != c.S * c.L * c.Hkv * c.d:
-            raise ValueError("new_v holds [S][L][Hkv][d]")
-        B.md_append_values(self.handle, _ptr(new_v, torch.bfloat16), self._values())
+        B.md_append_values(self.handle, _flat(new_v, torch.bfloat16, c.S * c.L * c.Hkv * c.d, self._device),
+                           self._values())
 
     def _values(self) -> int:
-        if self.cache.v_pool is None:
+        v = self.cache.v_pool
+        if v is None:
             raise ValueError("the cache has no values (PagedCache(values=True))")
-        return _ptr(self.cache.v_pool, torch.bfloat16)
+        return _flat(v, torch.bfloat16, self.cache.k_pool.numel(), self._device)
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, *, new_k: Optional[torch.Tensor] = None,
                new_v: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
@@ -379,41 +372,36 @@ class MemDecay:
         [S][Hkv][d], itself.  q float32 and out (float32 or bfloat16)
         [S][Hq][d], lse float32 [S][Hq]; sessions of q, out and of the new
         keys and values may be any distance apart."""
-        c = self.cache
-        self._here(q, out, new_k, new_v, lse, blocks, block_count, c.v_pool)
-        kv = 0
-        if new_k is not None and new_v is not None:
-            kv = _stride(new_k, torch.bfloat16, c.S, c.Hkv, c.d)
-            if _stride(new_v, torch.bfloat16, c.S, c.Hkv, c.d) != kv:
-                raise ValueError("new_k and new_v have sessions the same distance apart")
+        c, dev = self.cache, self._device
+        S = c.S
+        q_at, q_pitch = _rows(q, torch.float32, S, c.Hq, c.d, dev)
         if out.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"expected float32 or bfloat16 outputs, got {out.dtype}")
-        if lse is not None and lse.numel() != c.S * c.Hq:
-            raise ValueError("lse holds [S][Hq]")
-        most = 0
-        if blocks is not None:
-            most = self._lists(blocks, block_count)
-        B.md_attend_token(self.handle, layer, B.md_attend_args(
-            q=q.data_ptr(), q_stride=_stride(q, torch.float32, c.S, c.Hq, c.d),
-            new_k=None if new_k is None else new_k.data_ptr(), new_v=None if new_v is None else new_v.data_ptr(),
-            kv_stride=kv, v_pool=self._values(), blocks=None if blocks is None else _ptr(blocks, torch.int32),
-            block_count=None if blocks is None else _ptr(block_count, torch.int32), max_blocks=most, out_type=_type(out),
-            out=out.data_ptr(), out_stride=_stride(out, out.dtype, c.S, c.Hq, c.d),
-            lse=None if lse is None else _ptr(lse, torch.float32), workspace=self._workspace(True).data_ptr()))
+        out_at, out_pitch = _rows(out, out.dtype, S, c.Hq, c.d, dev)
+        k_at = v_at = kv_pitch = 0
+        if new_k is not None:
+            k_at, kv_pitch = _rows(new_k, torch.bfloat16, S, c.Hkv, c.d, dev)
+        if new_v is not None:
+            v_at, v_pitch = _rows(new_v, torch.bfloat16, S, c.Hkv, c.d, dev)
+            if new_k is not None and v_pitch != kv_pitch:
+                raise ValueError("new_k and new_v have sessions the same distance apart")
+        b_at, n_at, most = (0, 0, 0) if blocks is None else self._lists(blocks, block_count)
+        B.md_attend_token(self.handle, layer, B.ATTEND_ARGS.pack(
+            q_at, q_pitch, k_at, v_at, kv_pitch, self._values(), b_at, n_at, most, TYPES[out.dtype], out_at, out_pitch,
+            0 if lse is None else _flat(lse, torch.float32, S * c.Hq, dev), self._workspace(True).data_ptr()))
 
-    def _lists(self, blocks: torch.Tensor, count: torch.Tensor) -> int:
-        c = self.cache
-        if blocks.dim() != 3 or tuple(blocks.shape[:2]) != (c.S, c.Hkv) or count is None or \
-                count.numel() != c.S * c.Hkv:
+    def _lists(self, blocks: torch.Tensor, count: torch.Tensor):
+        c, dev = self.cache, self._device
+        if count is None or blocks.dim() != 3 or blocks.shape[0] != c.S or blocks.shape[1] != c.Hkv:
             raise ValueError("blocks hold [S][Hkv][max_blocks], their counts [S][Hkv]")
-        return blocks.shape[2]
+        return _flat(blocks, torch.int32, blocks.numel(), dev), _flat(count, torch.int32, c.S * c.Hkv, dev), blocks.shape[2]
 
     def _bounds(self):
-        c = self.cache
-        self._here(c.key_bounds, c.bound_exp)
+        c, dev = self.cache, self._device
         if c.key_bounds is None or c.bound_exp is None:
             raise ValueError("the cache has no bounds (PagedCache(bounds=True))")
-        return _ptr(c.key_bounds, torch.int8), _ptr(c.bound_exp, torch.int8)
+        n = c.n_phys * c.L * c.Hkv
+        return _flat(c.key_bounds, torch.int8, 2 * n * c.d, dev), _flat(c.bound_exp, torch.int8, n, dev)
 
     def update_bounds(self, all_pages: bool = False):
         """Bounds of the keys of each session's last page (after an append),
@@ -426,13 +414,11 @@ class MemDecay:
         one layer: blocks int32 [S][Hkv][max_blocks], block_count int32
         [S][Hkv]; always the ``first`` and ``last`` pages of the session."""
         c = self.cache
-        self._here(q, blocks, block_count)
-        most = self._lists(blocks, block_count)
+        q_at, q_pitch = _rows(q, torch.float32, c.S, c.Hq, c.d, self._device)
+        b_at, n_at, most = self._lists(blocks, block_count)
         bounds, exp = self._bounds()
-        B.md_select_blocks(self.handle, layer, B.md_select_args(
-            q=q.data_ptr(), q_stride=_stride(q, torch.float32, c.S, c.Hq, c.d), bounds=bounds, bound_exp=exp,
-            first=first, last=last, max_blocks=most, blocks=_ptr(blocks, torch.int32),
-            block_count=_ptr(block_count, torch.int32), workspace=self._workspace(False).data_ptr()))
+        B.md_select_blocks(self.handle, layer, B.SELECT_ARGS.pack(q_at, q_pitch, bounds, exp, first, last, most, b_at, n_at,
+                                                                 self._workspace(False).data_ptr()))
 
     def calib_accumulate(self, abar: torch.Tensor, bucket_steps: int, stats) -> None:
         """Add this observation to stats = (mass_fx, count, age_sum), int64
@@ -481,29 +467,27 @@ def _ptr(t: torch.Tensor, dtype) -> int:
     return t.data_ptr()
 
 
+
 TYPES = {torch.float32: B.MD_F32, torch.bfloat16: B.MD_BF16, torch.float16: B.MD_F16}
 
 
-def _type(t: torch.Tensor) -> int:
-    if t.dtype not in TYPES:
-        raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}")
-    return TYPES[t.dtype]
+def _rows(t: torch.Tensor, dtype, n: int, heads: int, d: int, device: int):
+    """Address of t, n rows [heads][d] (or [heads d]) each contiguous, and the
+    elements between them."""
+    shape, stride = t.shape, t.stride()
+    if shape == (n, heads, d):
+        rows = stride[2] == 1 and (stride[1] == d or heads == 1)
+    else:
+        rows = shape == (n, heads * d) and stride[1] == 1
+    if not rows or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"expected {dtype} [{n}][{heads}][{d}] with contiguous rows on device {device}, got {t.dtype} "
+                         f"{tuple(shape)} with strides {stride} on {t.device}")
+    return t.data_ptr(), stride[0] if n > 1 else heads * d
 
 
-def _pitch(t: torch.Tensor) -> int:
-    """Elements between the rows of t (its first axis; one row has no next)."""
-    return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
-
-
-def _rows(t: torch.Tensor) -> int:
-    if t.shape[0] and not t[0].is_contiguous():
-        raise ValueError("expected contiguous rows")
+def _flat(t: torch.Tensor, dtype, n: int, device: int) -> int:
+    """Address of t, n contiguous elements."""
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"expected {n} contiguous elements of {dtype} on device {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
-
-
-def _stride(t: torch.Tensor, dtype, n: int, heads: int, d: int) -> int:
-    """Elements between the n rows [heads][d] of t."""
-    if t.dtype != dtype or t.shape[0] != n or t.numel() != n * heads * d:
-        raise ValueError(f"expected {dtype} [{n}][{heads}][{d}], got {t.dtype} {tuple(t.shape)}")
-    _rows(t)
-    return _pitch(t)

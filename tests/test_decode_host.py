@@ -30,6 +30,12 @@ def test_argument_structs_match_the_header(tmp_path):
     out = subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()
     want = [ctypes.sizeof(s) for s in structs] + [getattr(s, f).offset for s in structs for f, _ in s._fields_]
     assert [int(x) for x in out] == want
+    # packed as bytes: the same fields at the same places
+    for st, packed in zip(structs, (B.ROPE_ARGS, B.ATTEND_ARGS, B.SELECT_ARGS)):
+        assert packed.size == ctypes.sizeof(st) and len(st._fields_) == len(packed.unpack(bytes(packed.size)))
+        for i, (name, kind) in enumerate(st._fields_):
+            one = st.from_buffer_copy(packed.pack(*[1 if j == i else 0 for j in range(len(st._fields_))]))
+            assert getattr(one, name) == 1 and [f for f, _ in st._fields_ if getattr(one, f)] == [name]
 
 
 def test_calls_without_a_handle_are_refused():
