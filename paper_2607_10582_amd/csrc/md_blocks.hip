@@ -9,8 +9,10 @@
 // 128 * 127^2 < 2^24): the same pages come out of every way to compute it.
 //
 // What bounds them: the bounds read every key once (and write a sixteenth of
-// that for pages of 16); the scores read 257 bytes per page and KV head; the
-// choice is a chain of a few passes over one row's scores in registers.
+// that for pages of 16); the scores read 257 bytes per page and KV head, at
+// 4.9 TB/s past the first 6 us; the choice is a chain of a few passes over one
+// row's scores in registers (5 - 7 us; with the scores in the same launch,
+// picked by the row's last workgroup, the two took 33 us against 27).
 
 #include "md_decode.h"
 #include "md_device.h"
@@ -208,162 +210,300 @@ __device__ __forceinline__ uint32_t score_key(float x) {
     return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// Scores of 64 pages of one (session, KV head) per workgroup, 16 per wave.
-__global__ void __launch_bounds__(kBlkThreads) k_block_scores(Dims dm, View v, Scratch sc, int layer,
-                                                              const float* __restrict__ q, int64_t q_stride,
-                                                              const int8_t* __restrict__ bounds,
-                                                              const int8_t* __restrict__ bound_exp,
-                                                              uint32_t* __restrict__ keys) {
-    const int s = blockIdx.x / dm.Hkv, kv = blockIdx.x % dm.Hkv;
-    const int np = v.n_pages[s], nt = v.n_tokens[s];
-    const int p0 = (int)blockIdx.y * 64 + (threadIdx.x >> 6) * 16;
-    if (!counters_ok(np, nt, dm) || p0 >= np) return;
-    const int lane = lane_id(), h = lane & 15, g = lane >> 4;
-    // the head's query in 8 bits: elements 64 j + 16 g .. + 15 of it
-    float x[2][16];
-    float amax = 0.0f;
+// Maximum, and sum, over the 16 lanes of a row (each lane gets it): rotations by
+// 8, 4, 2, 1.
+template <int STEP>
+__device__ __forceinline__ float row_rotated(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + STEP, 0xf, 0xf, false));
+}
+
+__device__ __forceinline__ float row_max(float v) {
+    v = fmaxf(v, row_rotated<8>(v));
+    v = fmaxf(v, row_rotated<4>(v));
+    v = fmaxf(v, row_rotated<2>(v));
+    return fmaxf(v, row_rotated<1>(v));
+}
+
+__device__ __forceinline__ float row_sum16(float v) {
+    v += row_rotated<8>(v);
+    v += row_rotated<4>(v);
+    v += row_rotated<2>(v);
+    return v + row_rotated<1>(v);
+}
+
+struct BlockCall {
+    int S, Hkv, G, P, MP, NP, LHkv, layer;
+    const int32_t* page_table;
+    const int32_t* n_pages;
+    const int32_t* n_tokens;
+    int32_t* status;
+    const float* q;
+    int64_t q_stride;
+    const int8_t* bounds;
+    const int8_t* bound_exp;
+    int first, last, max_blocks;
+    int32_t* blocks;
+    int32_t* block_count;
+    uint32_t* keys;      // [S Hkv][MP] scores in an order-preserving form
+};
+
+constexpr int kPickThreads = 1024;
+constexpr int kPickPer = kMaxPages / kPickThreads;   // keys of one thread
+constexpr int kBins = 2048;
+constexpr int kWords = kMaxPages / 32;
+constexpr int kRankAt = kPickThreads / 16;           // candidates ranked directly, 16 threads each
+
+// The row's best keys, a workgroup: the first `first` and the last `last` pages
+// and the best of the others, K in all (first + last <= K < np).  Thread i
+// holds the keys of pages i, i + 1024 ...  A histogram
+// over the range of the keys in question finds the bin that holds the K-th; it
+// becomes the range (scores of one row share their leading bits, so that bins
+// of fixed digits would mostly be a few full ones, whose counts the LDS adds
+// one by one), until few are left in it, which are ranked against each other.
+// Leaves a bit for each taken page in `words` (bins' place).
+__device__ __forceinline__ void pick(const uint32_t (&key)[kPickPer], int np, int first, int last, int K, int* bins,
+                                     int* lds) {
+    __shared__ uint32_t sh_lo, sh_hi;
+    __shared__ int sh_need, sh_count, sh_n;
+    __shared__ uint32_t cand_key[kRankAt];
+    __shared__ int cand_at[kRankAt];
+    const int tid = threadIdx.x, lane = lane_id();
+    const int from = first, to = np - last;   // pages that are chosen from
+    auto chosen_from = [&](int i) { const int page = i * kPickThreads + tid; return page >= from && page < to; };
+    uint32_t lo = 0xFFFFFFFFu, hi = 0;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f32x4 a = {0.f, 0.f, 0.f, 0.f};
-            if (h < dm.G)
-                a = *reinterpret_cast<const f32x4*>(q + (int64_t)s * q_stride + (kv * dm.G + h) * kHeadDim + 64 * j + 16 * g +
-                                                    4 * i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[j][4 * i + k] = a[k] == a[k] ? a[k] : 0.0f;
-                amax = fmaxf(amax, fabsf(x[j][4 * i + k]));
-            }
+    for (int i = 0; i < kPickPer; ++i)
+        if (chosen_from(i)) {
+            lo = min(lo, key[i]);
+            hi = max(hi, key[i]);
         }
-    amax = fmaxf(amax, __shfl_xor(amax, 16));
-    amax = fmaxf(amax, __shfl_xor(amax, 32));
-    const int f = step_exp(amax);
-    const float unit = power2(-f);
-    i32x4 bq[4];   // against lo (0, 1) and hi (2, 3)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t lo = 0, hi = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int c = (int)fminf(fmaxf(rintf(x[j][4 * i + k] * unit), -127.0f), 127.0f);
-                lo |= ((uint32_t)min(c, 0) & 0xFFu) << (8 * k);
-                hi |= ((uint32_t)max(c, 0) & 0xFFu) << (8 * k);
-            }
-            bq[j][i] = (int)lo;
-            bq[2 + j][i] = (int)hi;
-        }
-    const int page = min(p0 + h, np - 1);
-    int p = v.page_table[(size_t)s * dm.MP + page];
-    if ((unsigned)p >= (unsigned)dm.NP) {
-        atomicOr(sc.status, kDevCorrupt);
-        p = 0;
+    if (tid == 0) {
+        sh_lo = 0xFFFFFFFFu;
+        sh_hi = 0;
     }
-    const size_t at = (size_t)p * dm.LHkv + layer * dm.Hkv + kv;
-    const i32x4* b = reinterpret_cast<const i32x4*>(bounds + at * kBoundBytes) + g;
-    i32x4 acc = {0, 0, 0, 0};
+    __syncthreads();
+    lo = wave_min_u32(lo);
+    hi = ~wave_min_u32(~hi);
+    if (lane == 0) {
+        atomicMin(&sh_lo, lo);
+        atomicMax(&sh_hi, hi);
+    }
+    int need = K - first - last, count = to - from;   // keys to take from the range [lo, hi], and how many are in it
+    for (;;) {
+        bins[tid] = bins[tid + kPickThreads] = 0;
+        __syncthreads();
+        lo = sh_lo;
+        hi = sh_hi;
+        if (lo == hi || count <= kRankAt || need == 0) break;
+        const int shift = max(0, 21 - __clz((int)(hi - lo)));   // (hi - lo) >> shift < 2^11
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[4 * j], bq[j], acc, 0, 0, 0);
-    const int e = bound_exp[at];   // of page p0 + h
+        for (int i = 0; i < kPickPer; ++i)
+            if (chosen_from(i) && key[i] >= lo && key[i] <= hi) atomicAdd(&bins[(key[i] - lo) >> shift], 1);
+        __syncthreads();
+        // from the top bin down: thread i has bins 2047 - 2 i and the one below
+        const int c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid];
+        int total;
+        const int before = block_exclusive_scan(c0 + c1, lds, &total);
+        if (before < need && before + c0 + c1 >= need) {
+            const bool upper = before + c0 >= need;
+            const uint32_t bin = kBins - 1 - 2 * tid - (upper ? 0 : 1);
+            sh_lo = lo + (bin << shift);
+            sh_hi = lo + min(hi - lo, (bin << shift) + ((1u << shift) - 1));
+            sh_need = need - before - (upper ? 0 : c0);
+            sh_count = upper ? c0 : c1;
+        }
+        __syncthreads();
+        need = sh_need;
+        count = sh_count;
+    }
+    // Keys above the range are taken; of those in it, `need`: the largest, or
+    // of equal ones the first.
+    if (tid == 0) sh_n = 0;
+    __syncthreads();
+    const bool rank_them = need > 0 && count <= kRankAt;
+    int taken = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // page p0 + 4 g + i, head h
-        const int ep = __shfl(e, 4 * g + i);
-        float y = h < dm.G ? ldexpf((float)acc[i], ep + f) : -INFINITY;
-        y = fmaxf(y, __shfl_xor(y, 8));
-        y = fmaxf(y, __shfl_xor(y, 4));
-        y = fmaxf(y, __shfl_xor(y, 2));
-        y = fmaxf(y, __shfl_xor(y, 1));
-        if (h == 0 && p0 + 4 * g + i < np) keys[(size_t)blockIdx.x * dm.MP + p0 + 4 * g + i] = score_key(y + 0.0f);
+    for (int i = 0; i < kPickPer; ++i) {
+        if (i * kPickThreads >= np) break;
+        const int page = i * kPickThreads + tid;
+        const bool free = chosen_from(i), in = free && need > 0 && key[i] >= lo && key[i] <= hi;
+        bool take = page < np && (!free || (need > 0 && key[i] > hi));
+        if (rank_them) {
+            if (in) {
+                const int at = atomicAdd(&sh_n, 1);
+                cand_key[at] = key[i];
+                cand_at[at] = page;
+            }
+        } else if (need > 0) {   // more equal keys than can be ranked: in page order
+            int total;
+            const int ex = block_exclusive_scan(in ? 1 : 0, lds, &total);
+            take = take || (in && taken + ex < need);
+            taken += total;
+        }
+        const uint64_t m = __ballot(take);
+        if (lane < 2) bins[(i * kPickThreads + (tid & ~63)) / 32 + lane] = (int)(uint32_t)(m >> (32 * lane));
+    }
+    __syncthreads();
+    if (rank_them) {   // thread 16 i + j counts candidates 4 j .. 4 j + 3 that go before the i-th
+        const int i = tid >> 4;
+        const uint32_t k = cand_key[i];
+        const int at = cand_at[i];
+        float rank = 0.0f;
+#pragma unroll
+        for (int x = 0; x < kRankAt / 16; ++x) {
+            const int o = (tid & 15) * (kRankAt / 16) + x;
+            rank += o < count && (cand_key[o] > k || (cand_key[o] == k && cand_at[o] < at)) ? 1.0f : 0.0f;
+        }
+        rank = row_sum16(rank);
+        if ((tid & 15) == 0 && i < count && rank < (float)need) atomicOr(&bins[at >> 5], 1 << (at & 31));
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ bool counts_ok(const BlockCall& c, int np, int nt) {
+    return np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
+}
+
+// Scores of 32 pages of one (session, KV head) per wave, in two groups of 16,
+// requested at once.  The waves of a workgroup take the KV heads of the same
+// pages, whose bounds and exponents lie next to each other.  A load covers
+// four pages' bounds whole (16 pages' 64-byte quarters, the operand's own
+// order, took 25 us where this takes 21: 64 sessions of up to 4,096 pages, two
+// KV heads, 72 MB), so the operands are put together through LDS.
+constexpr int kScoreAt = 2;
+constexpr int kScorePages = 16 * kScoreAt;
+
+__global__ void __launch_bounds__(kBlkThreads) k_block_scores(BlockCall c) {
+    __shared__ i32x4 lds[kBlkThreads / 64][16][17];
+    i32x4 (&turned)[16][17] = lds[threadIdx.x >> 6];
+    const int s = blockIdx.y;
+    const int lane = lane_id(), h = lane & 15, g = lane >> 4;
+    const int task = (int)blockIdx.x * (kBlkThreads / 64) + uni(threadIdx.x >> 6);
+    const int kv = task % c.Hkv, p0 = task / c.Hkv * kScorePages, row = s * c.Hkv + kv;
+    const int np = c.n_pages[s];
+    if (p0 >= np || np <= c.max_blocks || !counts_ok(c, np, c.n_tokens[s])) return;
+    // (the query first: it is turned into codes while the bounds are under way)
+    f32x4 qv[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            qv[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (h < c.G)
+                qv[j][i] = *reinterpret_cast<const f32x4*>(c.q + (int64_t)s * c.q_stride + (kv * c.G + h) * kHeadDim + 64 * j +
+                                                           16 * g + 4 * i);
+        }
+    const int32_t* table = c.page_table + (size_t)s * c.MP;
+    const int head = c.layer * c.Hkv + kv;
+    bool bad = false;
+    auto page_of = [&](int page) {
+        int p = table[min(page, np - 1)];
+        if ((unsigned)p >= (unsigned)c.NP) {
+            bad = true;
+            p = 0;
+        }
+        return (size_t)p * c.LHkv + head;
+    };
+    size_t at[kScoreAt][4], own[kScoreAt];
+#pragma unroll
+    for (int k = 0; k < kScoreAt; ++k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) at[k][j] = page_of(p0 + 16 * k + 4 * j + g);
+        own[k] = page_of(p0 + 16 * k + 4 * g + (h & 3));   // the page whose score this lane writes
+    }
+    i32x4 b[kScoreAt][4];
+    int e[kScoreAt];
+#pragma unroll
+    for (int k = 0; k < kScoreAt; ++k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[k][j] = reinterpret_cast<const i32x4*>(c.bounds + at[k][j] * kBoundBytes)[h];
+        e[k] = c.bound_exp[own[k]];
+    }
+    if (__any(bad) && lane == 0) atomicOr(c.status, kDevCorrupt);
+    // ---- the head's query in 8 bits: elements 64 j + 16 g .. + 15 of it
+    i32x4 bq[4];   // against lo (0, 1) and hi (2, 3)
+    int f;
+    {
+        float x[2][16];
+        float amax = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float a = qv[j][i / 4][i % 4];
+                x[j][i] = a == a ? a : 0.0f;
+                amax = fmaxf(amax, fabsf(x[j][i]));
+            }
+        amax = fmaxf(amax, __shfl_xor(amax, 16));
+        amax = fmaxf(amax, __shfl_xor(amax, 32));
+        f = step_exp(amax);
+        const float unit = power2(-f);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t lo = 0, hi = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int code = (int)fminf(fmaxf(rintf(x[j][4 * i + k] * unit), -127.0f), 127.0f);
+                    lo |= ((uint32_t)min(code, 0) & 0xFFu) << (8 * k);
+                    hi |= ((uint32_t)max(code, 0) & 0xFFu) << (8 * k);
+                }
+                bq[j][i] = (int)lo;
+                bq[2 + j][i] = (int)hi;
+            }
+    }
+    uint32_t* keys = c.keys + (size_t)row * c.MP;
+#pragma unroll
+    for (int k = 0; k < kScoreAt; ++k) {
+        i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) turned[4 * j + g][h] = b[k][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(turned[h][4 * j + g], bq[j], acc, 0, 0, 0);
+        __builtin_amdgcn_wave_barrier();
+        float y[4];   // page 4 g + i: the best head's, short of the page's exponent
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = row_max(h < c.G ? ldexpf((float)acc[i], f) : -INFINITY);
+        const float z = ldexpf((h & 2) ? ((h & 1) ? y[3] : y[2]) : ((h & 1) ? y[1] : y[0]), e[k]);
+        const int page = p0 + 16 * k + 4 * g + h;
+        if (h < 4 && page < np) keys[page] = score_key(z + 0.0f);
     }
 }
 
-// One workgroup per (session, KV head): thread i holds the scores of eight
-// pages 8 i .. 8 i + 7.  A radix select, eight bits at a time, finds the key
-// of the last page to be taken and how many of those with that key are (the
-// oldest); the taken pages' places come from prefix sums in page order.
-__global__ void __launch_bounds__(kSelThreads) k_block_pick(Dims dm, View v, Scratch sc, md_select_args a,
-                                                            const uint32_t* __restrict__ keys) {
-    __shared__ int hist[256];
-    __shared__ int lds[2 * 17];
-    __shared__ int sh_bin, sh_need;
-    const int s = blockIdx.x / dm.Hkv, tid = threadIdx.x;
-    int np = v.n_pages[s];
-    const int nt = v.n_tokens[s];
-    if (!counters_ok(np, nt, dm)) {
-        if (tid == 0) atomicOr(sc.status, kDevCorrupt);
+// One workgroup per (session, KV head).
+__global__ void __launch_bounds__(kPickThreads) k_block_pick(BlockCall c) {
+    __shared__ int bins[kBins];
+    __shared__ int lds[17];
+    const int row = blockIdx.x, s = row / c.Hkv, tid = threadIdx.x;
+    int np = c.n_pages[s];
+    if (!counts_ok(c, np, c.n_tokens[s])) {
+        if (tid == 0) atomicOr(c.status, kDevCorrupt);
         np = 0;
     }
-    const int K = min(a.max_blocks, np);
-    uint32_t key[kPerThread];
+    const int K = min(c.max_blocks, np);
+    int32_t* out = c.blocks + (size_t)row * c.max_blocks;
+    if (K == np) {   // every page: nothing to choose
+        for (int i = tid; i < c.max_blocks; i += kPickThreads) out[i] = i < np ? i : -1;
+        if (tid == 0) c.block_count[row] = K;
+        return;
+    }
+    const uint32_t* keys = c.keys + (size_t)row * c.MP;
+    uint32_t key[kPickPer];
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-        const int page = tid * kPerThread + i;
+    for (int i = 0; i < kPickPer; ++i) {
         key[i] = 0;
-        if (page < np) {
-            key[i] = keys[(size_t)blockIdx.x * dm.MP + page];
-            if (page < a.first || page >= np - a.last) key[i] = 0xFFFFFFFFu;
-        }
+        if (i * kPickThreads < np) key[i] = keys[min(i * kPickThreads + tid, np - 1)];
     }
-    uint32_t prefix = 0;
-    int need = K;   // pages still to be found among those that share the prefix
-    if (K < np) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kPerThread; ++i)
-                if (tid * kPerThread + i < np && (shift == 24 || (key[i] >> (shift + 8)) == (prefix >> (shift + 8))))
-                    atomicAdd(&hist[(key[i] >> shift) & 0xFFu], 1);
-            __syncthreads();
-            if (tid < 64) {   // from the top bin down: lane i has bins 255 - 4 i ..
-                int c[4], sum = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    c[k] = hist[255 - (4 * tid + k)];
-                    sum += c[k];
-                }
-                int before = wave_incl_sum(sum) - sum;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (before < need && before + c[k] >= need) {
-                        sh_bin = 255 - (4 * tid + k);
-                        sh_need = need - before;
-                    }
-                    before += c[k];
-                }
-            }
-            __syncthreads();
-            prefix |= (uint32_t)sh_bin << shift;
-            need = sh_need;
-            __syncthreads();
-        }
-    }
-    // of the pages with the last key the first `need`
-    int ties = 0, above = 0;
-#pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-        const bool in = tid * kPerThread + i < np;
-        ties += in && K < np && key[i] == prefix;
-        above += in && (K == np || key[i] > prefix);
-    }
-    const int cnt[2] = {ties, above};
-    int ex[2], tot[2];
-    block_exclusive_scan_n<2>(cnt, lds, ex, tot);
-    int tie = ex[0];
-    int at = ex[1] + (K < np ? min(ex[0], need) : 0);
-    int32_t* out = a.blocks + (size_t)blockIdx.x * a.max_blocks;
-#pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-        const int page = tid * kPerThread + i;
-        if (page >= np) break;
-        bool take = K == np || key[i] > prefix;
-        if (!take && key[i] == prefix) take = tie++ < need;
-        if (take) out[at++] = page;
-    }
-    for (int i = K + tid; i < a.max_blocks; i += kSelThreads) out[i] = -1;
-    if (tid == 0) a.block_count[blockIdx.x] = K;
+    pick(key, np, c.first, c.last, K, bins, lds);
+    // ---- the taken pages in order, their places from the words' counts
+    const uint32_t word = tid < kWords ? (uint32_t)bins[tid] : 0u;
+    int total;
+    int at = block_exclusive_scan(__popc(word), lds, &total);
+    for (uint32_t w = word; w != 0; w &= w - 1) out[at++] = 32 * tid + __ffs((int)w) - 1;
+    for (int i = K + tid; i < c.max_blocks; i += kPickThreads) out[i] = -1;
+    if (tid == 0) c.block_count[row] = K;
 }
 
 }  // namespace
@@ -384,18 +524,39 @@ uint64_t select_workspace(const Dims& dm) { return (uint64_t)dm.S * dm.Hkv * dm.
 
 hipError_t launch_blocks(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_select_args& a,
                          hipStream_t st) {
-    Dims d = dm;
-    View vv = v;
-    Scratch ss = sc;
-    md_select_args aa = a;
-    uint32_t* keys = static_cast<uint32_t*>(a.workspace);
-    void* sargs[] = {&d, &vv, &ss, &layer, &aa.q, &aa.q_stride, &aa.bounds, &aa.bound_exp, &keys};
+    BlockCall c{};
+    c.S = dm.S;
+    c.Hkv = dm.Hkv;
+    c.G = dm.G;
+    c.P = dm.P;
+    c.MP = dm.MP;
+    c.NP = dm.NP;
+    c.LHkv = dm.LHkv;
+    c.layer = layer;
+    c.page_table = v.page_table;
+    c.n_pages = v.n_pages;
+    c.n_tokens = v.n_tokens;
+    c.status = sc.status;
+    c.q = a.q;
+    c.q_stride = a.q_stride;
+    c.bounds = a.bounds;
+    c.bound_exp = a.bound_exp;
+    c.first = a.first;
+    c.last = a.last;
+    c.max_blocks = a.max_blocks;
+    c.blocks = a.blocks;
+    c.block_count = a.block_count;
+    c.keys = static_cast<uint32_t*>(a.workspace);
+    void* args[] = {&c};
     const unsigned rows = (unsigned)(dm.S * dm.Hkv);
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&k_block_scores), dim3(rows, (unsigned)((dm.MP + 63) / 64)),
-                                         dim3(kBlkThreads), sargs, 0, st);
-    if (e != hipSuccess) return e;
-    void* pargs[] = {&d, &vv, &ss, &aa, &keys};
-    return hipLaunchKernel(reinterpret_cast<const void*>(&k_block_pick), dim3(rows), dim3(kSelThreads), pargs, 0, st);
+    if (dm.MP > a.max_blocks) {   // else every page is taken
+        const int tasks = (dm.MP + kScorePages - 1) / kScorePages * dm.Hkv, waves = kBlkThreads / 64;
+        const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&k_block_scores),
+                                             dim3((unsigned)((tasks + waves - 1) / waves), (unsigned)dm.S), dim3(kBlkThreads),
+                                             args, 0, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipLaunchKernel(reinterpret_cast<const void*>(&k_block_pick), dim3(rows), dim3(kPickThreads), args, 0, st);
 }
 
 }  // namespace md
