@@ -6,6 +6,7 @@
 // operations in between, so a long prompt is bound by HBM and a decode step
 // (a row per session) by the launch and one chain of loads.
 
+#include <algorithm>
 #include <type_traits>
 
 #include "md_decode.h"
@@ -97,6 +98,12 @@ __global__ void __launch_bounds__(64 * kRopeWaves) k_norm_rope(RopeCall c, const
     if (row >= c.n_rows) return;
     float2* turn = turn_lds[wv];
     const int half = c.rot / 2;
+    const int m = lane & 15;
+    float x[8];
+    auto load_head = [&](int h) {
+        load8<TYPE>(c.qkv, (int64_t)row * c.qkv_stride + (int64_t)min(h, c.heads - 1) * kHeadDim + 8 * m, x);
+    };
+    load_head(4 * part + (lane >> 4));   // under way while the angles are worked out
     if (lane < half) {
         const int pos = c.position != nullptr ? c.position[row] : clock[row];
         const double t = (double)pos * (c.inv_freq[lane] * 0.15915494309189533577);   // turns
@@ -106,7 +113,6 @@ __global__ void __launch_bounds__(64 * kRopeWaves) k_norm_rope(RopeCall c, const
         turn[lane] = make_float2(cs, sn);
     }
     __builtin_amdgcn_wave_barrier();
-    const int m = lane & 15;
     // frequencies of this lane's elements: dims 8 m + e, or pairs 4 m + e / 2
     const bool turns = 8 * m < c.rot;
     const bool upper = 8 * m >= half;
@@ -123,8 +129,7 @@ __global__ void __launch_bounds__(64 * kRopeWaves) k_norm_rope(RopeCall c, const
     for (int h0 = 4 * part; h0 < c.heads; h0 += 4 * c.parts) {
         const int h = h0 + (lane >> 4);
         const bool ok = h < c.heads;
-        float x[8];
-        load8<TYPE>(c.qkv, (int64_t)row * c.qkv_stride + (int64_t)min(h, c.heads - 1) * kHeadDim + 8 * m, x);
+        if (h0 != 4 * part) load_head(h);
         const bool value = h >= c.Hq + c.Hkv;
         const float* w = h < c.Hq ? c.q_weight : c.k_weight;
         if (!value && w != nullptr) {
@@ -203,8 +208,10 @@ hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a
     c.Hq = dm.Hq;
     c.Hkv = dm.Hkv;
     c.heads = dm.Hq + dm.Hkv * (a.v_out != nullptr ? 2 : 1);
-    (void)n_cu;
-    c.parts = 1;
+    // Few rows: a wave per four heads, so that the chain of loads is walked
+    // once; many: a wave per row, which works the angles out once.
+    const int64_t most = (c.heads + 3) / 4;
+    c.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, 16 * (int64_t)n_cu / a.n_rows));
     const void* fn = a.qkv_type == MD_F32    ? rope_kernel<MD_F32>(a.interleaved != 0)
                      : a.qkv_type == MD_BF16 ? rope_kernel<MD_BF16>(a.interleaved != 0)
                                              : rope_kernel<MD_F16>(a.interleaved != 0);
