@@ -529,8 +529,9 @@ md_status md_calib_fit(const uint64_t* mass_fx, const uint64_t* count, const uin
  *
  * They follow the conventions above: device pointers, the handle's stream, no
  * synchronisation, no allocation (work space is the caller's), and they can
- * be captured into a graph.  They leave the current device as it was.  None
- * of them changes the retention state.  The values of the cache sit in a pool
+ * be captured into a graph.  They leave the current device as it was.  What a
+ * call writes must not overlap what it reads.  None of them changes the
+ * retention state.  The values of the cache sit in a pool
  * of the caller's,
  *  v_pool       uint16 bf16 bits [NP][L][Hkv][P/16][d/32][4][16][2][4]: for each
  *               (layer, KV head) of a page, blocks of 16 tokens; element
@@ -593,9 +594,11 @@ md_status md_append_values(md_handle h, const uint16_t* new_v, uint16_t* v_pool)
  * Query head h reads KV head h / (Hq / Hkv).  Logits, statistics and sums are
  * float32 or exact (queries as three bf16 terms); softmax weights enter the
  * products with the values as two bf16 terms (relative error 2^-17).  A
- * session without any token gets zeros and lse = -infinity.  Handles of every
- * page size, layout and of the quantised tier; MD_E_UNSUPPORTED with an
- * offload tier.
+ * session without any token gets zeros and lse = -infinity; a NaN in a query
+ * stays in its head, and an infinite value makes its dimension NaN.  The same
+ * inputs give the same bits.  Every page size, layout and the quantised tier;
+ * MD_E_UNSUPPORTED with an offload tier, and where the rows of full page tables
+ * come to 2^31 steps of 32 tokens (S Hkv MP P / 32).
  */
 typedef struct md_attend_args {
     const float* q;           /* [S][Hq d], sessions q_stride elements apart (a multiple of  */

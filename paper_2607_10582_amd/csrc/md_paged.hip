@@ -34,8 +34,9 @@ namespace {
 // A step is two tiles of 16 tokens, whose values meet in one product of 32;
 // a cell is two steps per wave or more.
 constexpr int kMinWaveSteps = 2;
+constexpr int kWideSteps = 64;       // even shares below this may be doubled for whole rows
 constexpr int kStreamSteps = 8192;   // a line this long (128 MiB) is read past the caches
-constexpr int kJoin = 16;            // partial results that one workgroup joins
+constexpr int kJoin = 8;             // partial results that one thread joins
 
 __device__ __forceinline__ bool counts_ok(const TokenCall& c, int np, int nt) {
     return np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
@@ -195,11 +196,13 @@ __device__ __forceinline__ void write_out(const TokenCall& c, const Row& r, int 
 // The rows lie end to end on a line of steps of 32 tokens (sessions in order,
 // each session's KV heads one after another), which is cut into cells, one
 // for each workgroup, whatever the sessions' lengths.  Where cells of the
-// line's even share each (or of kMinCellSteps) leave room for it, every row
-// is cut by itself, into the fewest cells of at most that length (rows of
-// equal length, mostly); else the line is, and a cell holds the whole of some
+// line's even share each (or of the shortest length) leave room for it, every
+// row is cut by itself, into the fewest cells of at most that length (rows of
+// equal length, mostly); short ones also where cells of twice that do (400
+// rows of 300 - 700 tokens: 27 us whole against 31 cut evenly, 512 of about
+// 1,000: 51 against 61); else the line is, and a cell holds the whole of some
 // rows and parts of at most two.  A row in several cells is joined by the
-// workgroup that finishes last: in groups of kJoin cells by the last of each
+// workgroup that finishes last: in groups of cells by the last of each
 // group, then the groups by the last of those (arrivals, no waits).
 //
 // Within a cell's stretch of one row the waves take steps in turn.  The keys
@@ -208,10 +211,11 @@ __device__ __forceinline__ void write_out(const TokenCall& c, const Row& r, int 
 // step before this one's results are put together: 12 KiB per wave under way,
 // with which the CU's eight waves fill HBM (64 sessions of 32k tokens, two KV
 // heads: 2.15 GB in 335 us, 6.4 TB/s; a second step in registers, or twelve
-// waves, read no faster).  Two things cost a sixth each: a load behind a branch
-// turns the wait for the values into one for the next keys too, and cached
-// loads of a long line are 6 % slower than ones past the caches (short lines
-// the other way round: 54 MB that the cache still holds, 19 against 22 us).
+// waves, read no faster).  A load behind a branch would turn the wait for the
+// values into one for the next keys too (421 against 407 us when it was
+// taken out, 64 sessions of 2k - 64k tokens), and long lines are read past the
+// caches (364 against 391 us; short ones the other way round: 54 MB that the
+// cache still holds, 19 against 22 us).
 // Small cells at the end of the line, claimed from a queue by whichever
 // workgroup reads faster, cost more than they gave (390 us).
 //
@@ -229,12 +233,13 @@ k_token(TokenCall c) {
     __shared__ __align__(16) u32x4 q_lds[3][4][64];
     __shared__ __align__(16) f32x4 acc_lds[W][8][64];
     __shared__ float2 stat_lds[W][16];
-    __shared__ int scan_lds[17];
+    __shared__ int scan_lds[2 * 17];
     __shared__ int sh_last;
     extern __shared__ int2 session_lds[];
     int2* held = session_lds;                             // [S] pages (-1: counters inconsistent) and slots in use
     int* pref = reinterpret_cast<int*>(held + c.S);       // [S + 1] steps of one row of the sessions before
     int* cpref = pref + c.S + 1;                          // [S + 1] cells of one row of the sessions before
+    int* wpref = cpref + c.S + 1;                         // [S + 1] the same, of cells twice as long
     const int tid = threadIdx.x, lane = lane_id(), wv = uni(tid >> 6);
     const int h = lane & 15, g = lane >> 4;
     const int per = c.P >> 4;
@@ -262,21 +267,33 @@ k_token(TokenCall c) {
     }
     const int T = uni(before) * c.Hkv;
     const int big = max(kMinWaveSteps * W, (int)(((unsigned)T + c.units - 1) / (unsigned)c.units));
-    int cells = 0;
+    // (cells of the even share and of twice that, by rows)
+    int cells = 0, wide = 0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
         const int s = k * kThreads + tid;
         if (k * kThreads >= c.S) break;
-        int total;
-        const int ex = block_exclusive_scan((int)((unsigned)(n[k] + big - 1) / (unsigned)big), scan_lds, &total);
-        if (s < c.S) cpref[s] = cells + ex;
-        cells += total;
+        const int of[2] = {(int)((unsigned)(n[k] + big - 1) / (unsigned)big),
+                           (int)((unsigned)(n[k] + 2 * big - 1) / (unsigned)(2 * big))};
+        int ex[2], total[2];
+        block_exclusive_scan_n<2>(of, scan_lds, ex, total);
+        if (s < c.S) {
+            cpref[s] = cells + ex[0];
+            wpref[s] = wide + ex[1];
+        }
+        cells += total[0];
+        wide += total[1];
     }
     if (tid == 0) {
         pref[c.S] = before;
         cpref[c.S] = cells;
+        wpref[c.S] = wide;
     }
     __syncthreads();
+    if (uni(cells) * c.Hkv > c.units && big < kWideSteps) {
+        cells = wide;
+        cpref = wpref;
+    }
     cells = uni(cells) * c.Hkv;
     const bool by_row = cells <= c.units;   // every row cut by itself
     const int cell = blockIdx.x;
@@ -604,15 +621,16 @@ k_token(TokenCall c) {
                 }
                 return sum;
             };
-            const int i0 = i / kJoin * kJoin, members = min(kJoin, n - i0);
+            const int join = kJoin * 16 / heads;
+            const int i0 = i / join * join, members = min(join, n - i0);
             bool go = arrived_last(c.count + 2 * (first + i0) + slot_of(i0), members);
             if (go) {
                 Mine sum = sum_parts(first + i0, i0, 1, members);
-                const int groups = (n + kJoin - 1) / kJoin;
+                const int groups = (n + join - 1) / join;
                 if (groups > 1) {
                     if (hh < c.G) part_store(part_at(c, first + i0, slot_of(i0), hh), ep, sum);
                     go = arrived_last(c.count + 2 * c.units + first, groups);
-                    if (go) sum = sum_parts(first, 0, kJoin, groups);
+                    if (go) sum = sum_parts(first, 0, join, groups);
                 }
                 if (go && hh < c.G) write_out(c, done.r, hh, ep, sum);
             }
@@ -708,7 +726,7 @@ hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_
     const bool sparse = a.blocks != nullptr, codes = dm.quant != 0;
     const void* fn = W == 8 ? token_kernel<8>(sparse, codes) : W == 4 ? token_kernel<4>(sparse, codes)
                                                              : token_kernel<2>(sparse, codes);
-    const unsigned lds = (unsigned)(dm.S * sizeof(int2) + 2 * (dm.S + 1) * sizeof(int));
+    const unsigned lds = (unsigned)(dm.S * sizeof(int2) + 3 * (dm.S + 1) * sizeof(int));
     return hipLaunchKernel(fn, dim3((unsigned)c.units), dim3(64 * W), args, lds, st);
 }
 

@@ -230,6 +230,47 @@ def test_many_sessions():
     run_attend(w)
 
 
+@pytest.mark.parametrize("shape,lens", [((1, 1, 1), [(7 * i) % 40 for i in range(1024)]),
+                                        ((1, 6, 2), [(11 * i) % 70 for i in range(1024)]),
+                                        ((1, 16, 16), [(5 * i) % 33 for i in range(140)]),
+                                        ((1, 2, 1), [131072 - 5]), ((1, 12, 2), [65536, 9000])],
+                         ids=["1024x1", "1024x2", "140x16", "131k", "66k+9k"])
+def test_widest_and_longest(shape, lens):
+    # every width of the kernel's workgroups, the longest rows, the most sessions
+    say("[attend]", shape, len(lens))
+    w = World(*shape, 16, lens, seed=26, extra=0)
+    run_attend(w)
+    run_attend(w, new=False, out_type=BF16)
+
+
+def test_the_same_bits_every_time():
+    # rows cut and joined by whichever workgroup is last: the order of adding is fixed
+    w = World(1, 12, 2, 16, [9000, 700, 31, 4096], seed=27)
+    q = w.normal(4, 12, D)
+    outs = [torch.zeros((4, 12, D), device=w.dev) for _ in range(6)]
+    for o in outs:
+        w.md.attend(0, q, o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, outs[0]) for o in outs[1:])
+
+
+def test_two_handles_of_one_cache():
+    # each with a work space of its own, on streams of their own at the same time
+    w = World(1, 12, 2, 16, [9000, 700], seed=28)
+    w.out = torch.float32
+    ones = torch.ones((2, 7))
+    other = MemDecay(w.cache, ones, ones, rho=0.9, alpha=1.0, tau_scale=2.0, pinned_mask=0, stream=torch.cuda.Stream())
+    q = w.normal(2, 12, D)
+    outs = [(torch.zeros((2, 12, D), device=w.dev), torch.zeros((2, 12), device=w.dev)) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for md, (o, l) in zip((w.md, other), outs):
+            md.attend(0, q, o, lse=l)
+    torch.cuda.synchronize()
+    for o, l in outs:
+        check_attend(w, 0, q, o, l)
+
+
 def test_large_logits():
     # logits in the hundreds: weights underflow, the maximum moves late
     w = World(1, 12, 2, 16, [900], seed=9, scale=8.0)
