@@ -593,7 +593,7 @@ md_status md_append_values(md_handle h, const uint16_t* new_v, uint16_t* v_pool)
  * new_k and new_v, the token itself, whose key md_observe_step appends later.
  * Query head h reads KV head h / (Hq / Hkv).  Logits, statistics and sums are
  * float32 or exact (queries as three bf16 terms); softmax weights enter the
- * products with the values as two bf16 terms (relative error 2^-17).  A
+ * products with the values as three bf16 terms (relative error 2^-26).  A
  * session without any token gets zeros and lse = -infinity; a NaN in a query
  * stays in its head, and an infinite value makes its dimension NaN.  The same
  * inputs give the same bits.  Every page size, layout and the quantised tier;

@@ -504,7 +504,7 @@ k_token(TokenCall c) {
                     m = mn;
                 }
                 const float ms = m == -INFINITY ? 0.0f : m;
-                uint32_t ph[4], pl[4];   // weights as two bf16 terms
+                uint32_t ph[4], pm[4], pl[4];   // weights as three bf16 terms
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float p[4];
@@ -515,11 +515,14 @@ k_token(TokenCall c) {
                     }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const uint32_t w = pack_bf16(p[2 * k], p[2 * k + 1]);
-                        ph[2 * u + k] = w;
-                        pl[2 * u + k] = pack_bf16(p[2 * k] - bf16_lo(w), p[2 * k + 1] - bf16_hi(w));
+                        float a = p[2 * k], b = p[2 * k + 1];
+                        uint32_t w = ph[2 * u + k] = pack_bf16(a, b);
+                        a -= bf16_lo(w);
+                        b -= bf16_hi(w);
+                        w = pm[2 * u + k] = pack_bf16(a, b);
+                        pl[2 * u + k] = pack_bf16(a - bf16_lo(w), b - bf16_hi(w));
                     }
-                    // a slot that does not count may hold anything, and 0 times
+                // a slot that does not count may hold anything, and 0 times
                     // an infinity or NaN is NaN: its values become 0
                     if (live[u] < 16) {
                         const int k4 = live[u] - 4 * g;   // tokens of this lane's four that count
@@ -530,6 +533,7 @@ k_token(TokenCall c) {
                     }
                 }
                 const bf16x8 bh = __builtin_bit_cast(bf16x8, u32x4{ph[0], ph[1], ph[2], ph[3]});
+                const bf16x8 bm = __builtin_bit_cast(bf16x8, u32x4{pm[0], pm[1], pm[2], pm[3]});
                 const bf16x8 bl = __builtin_bit_cast(bf16x8, u32x4{pl[0], pl[1], pl[2], pl[3]});
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -538,6 +542,7 @@ k_token(TokenCall c) {
                         const bf16x8 a = __builtin_bit_cast(
                             bf16x8, u32x4{vt[0][j][2 * e], vt[0][j][2 * e + 1], vt[1][j][2 * e], vt[1][j][2 * e + 1]});
                         o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bh, o[2 * j + e], 0, 0, 0);
+                        o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bm, o[2 * j + e], 0, 0, 0);
                         o[2 * j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bl, o[2 * j + e], 0, 0, 0);
                     }
                 load_v(t, nx);

@@ -10,8 +10,8 @@ Tolerances, before any run.  A bf16 result is off by at most half a step,
   turned pair's length.
 * attention: a logit is 3 * 128 exact products summed in float32, at most
   2^-24 * 384 * sum |q_e k_e| / sqrt(d) off; weights follow it twice over
-  (their own and the sum's), and take two bf16 terms (2^-17), the exponential
-  and the sums 2^-20.  An output is off by at most that times the largest
+  (their own and the sum's), and take three bf16 terms (2^-26), the
+  exponential and the sums 2^-20.  An output is off by at most that times the largest
   value, the log-sum by the logit's error and 2^-20 relative.
 * bounds and selections are whole numbers: equal.
 """
@@ -148,7 +148,7 @@ def check_attend(w, layer, q, out, lse, new_k=None, new_v=None, lists=None, seen
                 assert torch.equal(got, ref) and torch.equal(gl, rl), (seen, s, kv)
                 continue
             off = float((qq.double().abs() @ k.double().abs().T).max()) / math.sqrt(D) * 384 * 2.0 ** -24
-            tol = (2 * off + 2.0 ** -17 + 2.0 ** -20) * float(v.abs().max())
+            tol = (2 * off + 2.0 ** -26 + 2.0 ** -20) * float(v.abs().max())
             step = 2.0 ** -8 * ref.abs() if w.out == BF16 else 0.0
             err = (got - ref).abs()
             assert torch.isfinite(got).all() and bool((err <= tol + step).all()), (seen, s, kv, float(err.max()), tol)
