@@ -86,8 +86,8 @@ __device__ __forceinline__ float row_sum(float v) {
 // A wave takes one row, or one of `parts` of its heads, four heads at a time:
 // 16 lanes a head, eight consecutive elements each (16-byte loads of 16-bit
 // types).  Lane i works out the cosine and sine of frequency i once (in
-// turns, reduced in float64: a float32 product of a position in the millions
-// would be off by a radian), and the row's heads share them through LDS.  The
+// turns, reduced in float64: a float32 product of a position of a million is
+// off by up to 0.03 radian, of ten millions by up to 0.5), and the row's heads share them through LDS.  The
 // halves that turn together sit rot / 16 lanes apart.
 template <int TYPE, bool PAIRS>
 __global__ void __launch_bounds__(64 * kRopeWaves) k_norm_rope(RopeCall c, const int32_t* __restrict__ clock) {
