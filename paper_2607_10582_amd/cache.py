@@ -188,13 +188,20 @@ class PagedCache:
 
     def load_values(self, s: int, values: torch.Tensor, region=None):
         """Place the values bf16 [n][L][Hkv][d] of a session's prompt next to
-        the keys that ``load_session`` placed; region: the same codes, with
-        region-aligned pages only."""
+        the keys that ``load_session`` placed, one for each of its tokens;
+        region: the same codes, with region-aligned pages only."""
         n, P = int(values.shape[0]), self.P
+        if self.v_pool is None:
+            raise ValueError("the cache has no values (PagedCache(values=True))")
+        if region is not None and len(region) != n:
+            raise ValueError("need one region code per token")
+        pos = self.positions(np.zeros(n) if region is None else region, P, region is not None)
+        slots = int(pos[-1]) + 1 if n else 0
+        if slots != int(self.n_tokens[s]) or (region is not None and n != int(self.n_live[s])):
+            raise ValueError(f"{n} values in {slots} slots for session {s} with {int(self.n_tokens[s])} slots in use")
         if n == 0:
             return
-        pos = self.positions(np.zeros(n) if region is None else region, P, region is not None)
-        m = int(pos[-1]) // P + 1
+        m = (slots + P - 1) // P
         full = torch.zeros((m * P,) + tuple(values.shape[1:]), dtype=torch.bfloat16, device=self.device)
         full[torch.as_tensor(pos, device=self.device)] = values.to(self.device, torch.bfloat16)
         ids = self.page_table[s, :m].long()
@@ -385,6 +392,8 @@ class MemDecay:
             v_at, v_pitch = _rows(new_v, torch.bfloat16, S, c.Hkv, c.d, dev)
             if new_k is not None and v_pitch != kv_pitch:
                 raise ValueError("new_k and new_v have sessions the same distance apart")
+        if blocks is None and block_count is not None:
+            raise ValueError("counts without their blocks")
         b_at, n_at, most = (0, 0, 0) if blocks is None else self._lists(blocks, block_count)
         B.md_attend_token(self.handle, layer, B.ATTEND_ARGS.pack(
             q_at, q_pitch, k_at, v_at, kv_pitch, self._values(), b_at, n_at, most, TYPES[out.dtype], out_at, out_pitch,

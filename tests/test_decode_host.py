@@ -136,3 +136,26 @@ def test_oracle_selection():
     assert O.select([1.0, 5.0, 5.0, 2.0, 9.0], 3, 1, 1) == [0, 1, 4]
     assert O.select([1.0, 5.0], 2, 0, 0) == [0, 1] and O.select([], 3, 1, 1) == []
     assert O.select([0.0, -math.inf, -1.0], 2, 0, 0) == [0, 2]
+
+
+def test_values_go_where_the_sessions_keys_are():
+    # more or fewer tokens than the session holds would reach pages that it
+    # lacks (or leave some without values): refused before anything is written
+    c = PagedCache(L=1, Hq=2, Hkv=1, d=128, P=16, S=2, max_pages=4, n_phys=6, device="cpu", values=True)
+    keys = torch.zeros((20, 1, 1, 128), dtype=torch.bfloat16)
+    c.load_session(0, keys, [1] * 20, [4, 2], budget=20, clock=20)
+    c.v_pool.zero_()
+    for n in (1, 19, 21, 33, 64, 100):
+        with pytest.raises(ValueError):
+            c.load_values(0, torch.ones((n, 1, 1, 128), dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        c.load_values(1, keys)                 # a session without pages
+    with pytest.raises(ValueError):
+        c.load_values(0, keys, [1] * 10 + [2] * 10)   # its keys lie without holes
+    assert int(torch.count_nonzero(c.v_pool)) == 0
+    values = torch.arange(20 * 128).to(torch.bfloat16).view(20, 1, 1, 128)
+    c.load_values(0, values)
+    got = c.from_value_layout(c.v_pool[torch.tensor([4, 2])]).reshape(32, 1, 1, 128)
+    assert torch.equal(got[:20], values) and int(torch.count_nonzero(got[20:])) == 0
+    with pytest.raises(ValueError):
+        PagedCache(L=1, Hq=2, Hkv=1, d=128, P=16, S=1, max_pages=4, n_phys=4, device="cpu").load_values(0, keys)

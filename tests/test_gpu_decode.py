@@ -770,3 +770,12 @@ def test_captured_calls_replay():
         for name in a:
             assert torch.equal(a[name], e[name]), (i, name)
     assert md.device_status() == 0
+
+
+def test_counts_need_their_blocks():
+    w = World(1, 4, 2, 16, [40, 7], seed=5)
+    q, out = torch.zeros((2, 4, 128), device="cuda"), torch.full((2, 4, 128), 3.0, device="cuda")
+    with pytest.raises(ValueError):
+        w.md.attend(0, q, out, block_count=torch.ones((2, 2), dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert torch.all(out == 3.0)
