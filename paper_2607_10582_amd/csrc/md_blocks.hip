@@ -286,7 +286,7 @@ constexpr int kRankAt = kPickThreads / 16;           // candidates ranked direct
 // becomes the range (scores of one row share their leading bits, so that bins
 // of fixed digits would mostly be a few full ones, whose counts the LDS adds
 // one by one), until few are left in it, which are ranked against each other.
-// Leaves a bit for each taken page in `words` (bins' place).
+// Leaves a bit for each taken page in the first words of `bins`.
 __device__ __forceinline__ void pick(const uint32_t (&key)[kPickPer], int np, int first, int last, int K, int* bins,
                                      int* lds) {
     __shared__ uint32_t sh_lo, sh_hi;

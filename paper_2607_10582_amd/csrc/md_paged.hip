@@ -522,7 +522,7 @@ k_token(TokenCall c) {
                         w = pm[2 * u + k] = pack_bf16(a, b);
                         pl[2 * u + k] = pack_bf16(a - bf16_lo(w), b - bf16_hi(w));
                     }
-                // a slot that does not count may hold anything, and 0 times
+                    // a slot that does not count may hold anything, and 0 times
                     // an infinity or NaN is NaN: its values become 0
                     if (live[u] < 16) {
                         const int k4 = live[u] - 4 * g;   // tokens of this lane's four that count

