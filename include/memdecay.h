@@ -607,8 +607,9 @@ typedef struct md_attend_args {
     const uint16_t* new_v;    /* multiple of 8); both or neither NULL                        */
     int64_t kv_stride;
     const uint16_t* v_pool;
-    const int32_t* blocks;    /* NULL, or [S][Hkv][max_blocks]: the first block_count[s][kv] */
-    const int32_t* block_count; /* entries of a row are logical pages, strictly ascending    */
+    const int32_t* blocks;    /* [S][Hkv][max_blocks]: the first block_count[s][kv] entries  */
+    const int32_t* block_count; /* of a row are logical pages, strictly ascending; both or   */
+                              /* neither NULL                                                */
     int32_t max_blocks;       /* >= 1 with blocks                                            */
     int32_t out_type;         /* MD_F32 or MD_BF16                                           */
     void* out;                /* [S][Hq d], sessions out_stride elements apart (a multiple   */

@@ -401,8 +401,9 @@ class MemDecay:
 
     def _lists(self, blocks: torch.Tensor, count: torch.Tensor):
         c, dev = self.cache, self._device
-        if count is None or blocks.dim() != 3 or blocks.shape[0] != c.S or blocks.shape[1] != c.Hkv:
-            raise ValueError("blocks hold [S][Hkv][max_blocks], their counts [S][Hkv]")
+        # (an empty tensor's address is 0, which the library takes for no list: every page)
+        if count is None or blocks.dim() != 3 or blocks.shape[0] != c.S or blocks.shape[1] != c.Hkv or blocks.shape[2] < 1:
+            raise ValueError("blocks hold [S][Hkv][max_blocks], max_blocks >= 1, their counts [S][Hkv]")
         return _flat(blocks, torch.int32, blocks.numel(), dev), _flat(count, torch.int32, c.S * c.Hkv, dev), blocks.shape[2]
 
     def _bounds(self):

@@ -1016,8 +1016,9 @@ md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a) {
                                 a->kv_stride % 8 != 0))
         return MD_E_INVALID;
     if (a->v_pool == nullptr || !aligned(a->v_pool, 16)) return MD_E_INVALID;
-    if (a->blocks != nullptr && (a->block_count == nullptr || !aligned(a->blocks, 4) || !aligned(a->block_count, 4) ||
-                                 a->max_blocks < 1 || a->max_blocks > md::kMaxPages))
+    if ((a->blocks == nullptr) != (a->block_count == nullptr)) return MD_E_INVALID;
+    if (a->blocks != nullptr && (!aligned(a->blocks, 4) || !aligned(a->block_count, 4) || a->max_blocks < 1 ||
+                                 a->max_blocks > md::kMaxPages))
         return MD_E_INVALID;
     if (a->out == nullptr || !aligned(a->out, 16) || a->out_stride < hq || a->out_stride % 8 != 0 ||
         (a->out_type != MD_F32 && a->out_type != MD_BF16) || !aligned(a->lse, 4))
