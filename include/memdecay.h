@@ -525,7 +525,7 @@ md_status md_calib_fit(const uint64_t* mass_fx, const uint64_t* count, const uin
  *
  * and once per step, with the queries and keys that md_norm_rope left,
  *
- *     md_observe_step -> md_append_values [-> md_key_bounds] -> md_select_compact
+ *     md_observe_step -> md_append_values -> md_select_compact [-> md_key_bounds]
  *
  * They follow the conventions above: device pointers, the handle's stream, no
  * synchronisation, no allocation (work space is the caller's), and they can
@@ -631,10 +631,17 @@ md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a);
  * bounds:    int8 [NP][L][Hkv][2][d], lo then hi; 16-byte aligned.
  * bound_exp: int8 [NP][L][Hkv], the exponents e.
  * all_pages: 1 for every page of every session (after the prompts are
- *   loaded, or when pages have turned into codes), 0 for each session's last
- *   page (after md_observe_step, the page that took the token).
+ *   loaded), 0 once per step: for each session's last page (the page that took
+ *   the token) and, with the quantised tier, the pages that this handle's
+ *   md_compact or md_select_compact has turned into codes since its last
+ *   md_key_bounds.  Behind the compaction it finds them at once; before it,
+ *   at the next step's call.  A session's pages are taken one after another:
+ *   where a compaction converts most of a cache, 1 is faster.  A handle keeps
+ *   one pair of arrays up to date (another pair: 1 first).
  * The keys of a page that holds 8-bit codes are the float32 products of scale
- * and code.  MD_E_UNSUPPORTED with an offload tier.
+ * and code: a key moves by up to 2^-4 of itself when it becomes one, so the
+ * bounds of bf16 keys do not hold for their codes.  MD_E_UNSUPPORTED with an
+ * offload tier.
  */
 md_status md_key_bounds(md_handle h, int32_t all_pages, int8_t* bounds, int8_t* bound_exp);
 

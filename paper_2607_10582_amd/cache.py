@@ -414,8 +414,10 @@ class MemDecay:
         return _flat(c.key_bounds, torch.int8, 2 * n * c.d, dev), _flat(c.bound_exp, torch.int8, n, dev)
 
     def update_bounds(self, all_pages: bool = False):
-        """Bounds of the keys of each session's last page (after an append),
-        or of every page (after the prompts are loaded)."""
+        """Bounds of the keys, once per step behind its compaction: of each
+        session's last page and, with the quantised tier, of the pages that
+        became codes since the last call; or of every page (after the prompts
+        are loaded; also faster where most of a cache has become codes)."""
         B.md_key_bounds(self.handle, int(all_pages), *self._bounds())
 
     def select_blocks(self, layer: int, q: torch.Tensor, blocks: torch.Tensor, block_count: torch.Tensor, *,

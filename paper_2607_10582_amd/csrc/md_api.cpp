@@ -287,6 +287,7 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
     dm.aligned = (cfg->flags & MD_FLAG_REGION_ALIGNED) ? 1 : 0;
     dm.quant = cfg->quant_threshold > 0.0f ? 1 : 0;
     dm.quant_thr = cfg->quant_threshold;
+    dm.stamps = dm.quant && cfg->offload_pages == 0 ? 1 : 0;   // (md_key_bounds has no offload tier)
     dm.H = cfg->offload_pages;
     dm.drop_thr = cfg->drop_threshold;
     dm.page_bytes = (size_t)dm.LHkv * dm.P * md::kHeadDim * sizeof(uint16_t);
@@ -547,6 +548,10 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
     if (dm.tail > 1) dm.U_cap += dm.n_wg; else dm.tail = 1;
     size_t bytes = md::scratch_bytes(dm);
     const auto too_large = [&] { return use_static && bytes > md::kStaticScratchBytes + md::row_group_words(dm.S); };
+    if (too_large() && dm.stamps) {   // md_key_bounds then looks at every page of codes again
+        dm.stamps = 0;
+        bytes = md::scratch_bytes(dm);
+    }
     if (too_large() && dm.rows_rg > 0) {   // no room for another path: no observe changes to it later
         limit_first = limit_steady = INT64_MAX;
         if (fused_first && rows_first == 0) rows_first = rows_steady;

@@ -1714,6 +1714,7 @@ __global__ void __launch_bounds__(256) k_quant(Dims dm, View v, Scratch sc, cons
     const int s = blockIdx.y;
     const int np = v.n_pages[s];
     if (!sc.valid[s] || np < 2) return;
+    if (sc.coded_at != nullptr && blockIdx.x == 0 && threadIdx.x == 0) sc.last_coded[2 * s + 1] = code_time(sc);
     const int cnt = min(max(ev_count[s], 0), dm.MP);
     const int32_t* evs = ev_serial + (size_t)s * dm.MP;
     const int32_t* ptab = v.page_table + (size_t)s * dm.MP;
@@ -1776,7 +1777,14 @@ __global__ void __launch_bounds__(256) k_quant(Dims dm, View v, Scratch sc, cons
             }
         }
         __syncthreads();
-        if (threadIdx.x == 0) v.page_format[phys] = 1;
+        if (threadIdx.x == 0) {
+            v.page_format[phys] = 1;
+            if (sc.coded_at != nullptr) {   // the bounds of its keys are no longer theirs (k_bounds)
+                const uint32_t now = code_time(sc);
+                sc.coded_at[phys] = now;
+                sc.last_coded[2 * s] = now;
+            }
+        }
     }
 }
 
@@ -1884,6 +1892,11 @@ size_t scratch_bytes(const Dims& dm) {
         n += align256((size_t)(dm.S + 1) * sizeof(int32_t));
         n += align256((size_t)dm.S * dm.rows_rg * rows_capacity(dm.rows_nc) * sizeof(float));
     }
+    if (dm.stamps) {
+        n += align256((size_t)dm.NP * sizeof(uint32_t));
+        n += align256((size_t)dm.S * 2 * sizeof(uint32_t));
+        n += align256((size_t)dm.S * bound_groups(dm) * sizeof(uint32_t));
+    }
     return n;
 }
 
@@ -1935,6 +1948,12 @@ void scratch_carve(const Dims& dm, void* base, Scratch* sc) {
         sc->rows_read = sc->rows_done + dm.S;
         sc->rows_part = reinterpret_cast<float*>(
             take((size_t)dm.S * dm.rows_rg * rows_capacity(dm.rows_nc) * sizeof(float)));
+    }
+    sc->coded_at = sc->last_coded = sc->looked = nullptr;
+    if (dm.stamps) {
+        sc->coded_at = reinterpret_cast<uint32_t*>(take((size_t)dm.NP * sizeof(uint32_t)));
+        sc->last_coded = reinterpret_cast<uint32_t*>(take((size_t)dm.S * 2 * sizeof(uint32_t)));
+        sc->looked = reinterpret_cast<uint32_t*>(take((size_t)dm.S * bound_groups(dm) * sizeof(uint32_t)));
     }
 }
 
