@@ -42,6 +42,9 @@ __device__ __forceinline__ bool counts_ok(const TokenCall& c, int np, int nt) {
     return np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
 }
 
+// The kernel's LDS that grows with the sessions.
+constexpr size_t session_bytes(int S) { return (size_t)(2 * S + 1) * sizeof(int); }
+
 struct Desc {       // one 16-token tile, per lane
     int phys;       // page
     int live;       // tokens of it that count, 0 .. 16; -1: the new token
@@ -235,11 +238,16 @@ k_token(TokenCall c) {
     __shared__ float2 stat_lds[W][16];
     __shared__ int scan_lds[2 * 17];
     __shared__ int sh_last;
-    extern __shared__ int2 session_lds[];
-    int2* held = session_lds;                             // [S] pages (-1: counters inconsistent) and slots in use
-    int* pref = reinterpret_cast<int*>(held + c.S);       // [S + 1] steps of one row of the sessions before
-    int* cpref = pref + c.S + 1;                          // [S + 1] cells of one row of the sessions before
-    int* wpref = cpref + c.S + 1;                         // [S + 1] the same, of cells twice as long
+    extern __shared__ int session_lds[];
+    int* held = session_lds;              // [S] slots in use (-1: counters inconsistent), which give the pages
+    int* pref = held + c.S;               // [S + 1] steps of one row of the sessions before
+    // (of rows cut by themselves only, whose one stretch begins before any result is there)
+    int* cpref = reinterpret_cast<int*>(acc_lds);   // [S + 1] cells of one row of the sessions before
+    int* wpref = cpref + c.S + 1;                   // [S + 1] the same, of cells twice as long
+    static_assert(sizeof(acc_lds) >= 2 * (kMaxSessions + 1) * sizeof(int));
+    static_assert(8 / W * (sizeof(q_lds) + sizeof(acc_lds) + sizeof(stat_lds) + sizeof(scan_lds) + sizeof(sh_last) +
+                           session_bytes(kMaxSessions) + 1280) <= 160 * 1024,
+                  "eight waves a CU, whatever the sessions (1,280: the LDS is given out in such pieces)");
     const int tid = threadIdx.x, lane = lane_id(), wv = uni(tid >> 6);
     const int h = lane & 15, g = lane >> 4;
     const int per = c.P >> 4;
@@ -256,7 +264,7 @@ k_token(TokenCall c) {
             const int np = c.n_pages[s], nt = c.n_tokens[s];
             const bool ok = counts_ok(c, np, nt);
             if (!ok && blockIdx.x == 0) status = kDevCorrupt;
-            held[s] = ok ? make_int2(np, nt) : make_int2(-1, 0);
+            held[s] = ok ? nt : -1;
             const int tiles = !ok ? 0 : SPARSE ? min(c.max_blocks, np) * per : (nt + 15) >> 4;
             n[k] = max(1, ((tiles + 1) >> 1) + (c.new_k != nullptr && ok ? 1 : 0));
         }
@@ -374,9 +382,10 @@ k_token(TokenCall c) {
                 t.count = (int)((unsigned)(row0 + length - 1) / (unsigned)big) - t.first + 1;
                 t.next = row0 + t.hi;
             }
-            r.np = uni(max(0, held[r.s].x));
-            r.nt = uni(held[r.s].y);
-            r.ok = uni(held[r.s].x) >= 0;
+            r.nt = uni(held[r.s]);
+            r.ok = r.nt >= 0;
+            r.nt = max(0, r.nt);
+            r.np = (r.nt + c.P - 1) >> c.Pshift;   // (what counts_ok says of consistent ones)
             r.tiles = (r.nt + 15) >> 4;
             if constexpr (SPARSE) {
                 const int most = min(c.max_blocks, r.np);
@@ -660,7 +669,9 @@ const void* token_kernel(bool sparse, bool codes) {
 // page tables' capacity leaves the workgroups less than the shortest cell.
 // Four, as a rule.  Two where each CU has eight rows or more, most of them
 // whole in one cell (4,096 rows of 5 - 60 tokens: 44 against 61 us, of about
-// 1,000: 359 against 373).  Eight where a few long rows are cut into half as
+// 1,000: 359 against 373); four of these workgroups fit a CU's LDS with any
+// number of sessions (1,024 of 300 - 700 tokens, two KV heads: 123 us; 142
+// where their words left room for three).  Eight where a few long rows are cut into half as
 // many parts to join (two rows of 131k tokens: 37 against 41 us; 32 rows of
 // 32k: 82 either way).
 static int attend_waves(const Dims& dm, int n_cu) {
@@ -731,8 +742,7 @@ hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_
     const bool sparse = a.blocks != nullptr, codes = dm.quant != 0;
     const void* fn = W == 8 ? token_kernel<8>(sparse, codes) : W == 4 ? token_kernel<4>(sparse, codes)
                                                              : token_kernel<2>(sparse, codes);
-    const unsigned lds = (unsigned)(dm.S * sizeof(int2) + 3 * (dm.S + 1) * sizeof(int));
-    return hipLaunchKernel(fn, dim3((unsigned)c.units), dim3(64 * W), args, lds, st);
+    return hipLaunchKernel(fn, dim3((unsigned)c.units), dim3(64 * W), args, session_bytes(dm.S), st);
 }
 
 }  // namespace md
