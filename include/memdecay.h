@@ -107,8 +107,11 @@ enum {
                                 /* skipped for the step                         */
 #define MD_DEV_BAD_BLOCK  0x20  /* md_attend_token got a list of blocks that    */
                                 /* does not ascend, names a page the session    */
-                                /* lacks or counts more entries than a row has; */
-                                /* those entries are left out                   */
+                                /* lacks or counts more entries than a row has: */
+                                /* an entry counts where it names a page of the */
+                                /* session and is above the entry before it,    */
+                                /* which need not count itself (of 5 3 4 5: 5,  */
+                                /* 4 and 5 again; of 0 2^30 1: 0)               */
 #define MD_DEV_TIMEOUT    0x10  /* a bounded wait between the workgroups of the */
                                 /* fused observation kernel ran out; the step's */
                                 /* attention mass is not valid (the session     */

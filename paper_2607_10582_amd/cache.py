@@ -378,7 +378,8 @@ class MemDecay:
         cached tokens (or the listed pages) and, with new_k and new_v bf16
         [S][Hkv][d], itself.  q float32 and out (float32 or bfloat16)
         [S][Hq][d], lse float32 [S][Hq]; sessions of q, out and of the new
-        keys and values may be any distance apart."""
+        keys and values may be any distance apart.  A row's listed pages
+        ascend (device_status() tells of one that does not)."""
         c, dev = self.cache, self._device
         S = c.S
         q_at, q_pitch = _rows(q, torch.float32, S, c.Hq, c.d, dev)

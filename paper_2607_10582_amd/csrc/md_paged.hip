@@ -89,6 +89,8 @@ __device__ __forceinline__ Desc tile_desc(const TokenCall& c, const Row& r, int 
         const int32_t* list = c.blocks + ((size_t)r.s * c.Hkv + r.kv) * c.max_blocks;
         const int o = page;
         page = list[o];
+        // (by the entry before alone: the entries that count before a broken
+        // one would take a pass over the list)
         if (page < 0 || page >= r.np || (o > 0 && page <= list[o - 1])) {
             status |= MD_DEV_BAD_BLOCK;
             return d;

@@ -5,6 +5,7 @@ import types
 import pytest
 import torch
 
+import decode_oracle as O
 from paper_2607_10582_amd import binding as B
 from paper_2607_10582_amd.cache import MemDecay, PagedCache
 
@@ -62,3 +63,32 @@ def test_attention_refuses_empty_and_half_given_lists():
     raw(blocks.data_ptr(), count.data_ptr(), 3)                       # lists without entries: nothing is attended to
     torch.cuda.synchronize()
     assert not out.any() and md.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_what_counts_in_a_broken_list():
+    # An entry counts where it names a page of the session and is above the
+    # entry before it, whatever became of that one.  Equal keys, values that
+    # tell the pages apart: the result is the mean over the tokens that count,
+    # in whole numbers over their number (reciprocal and product, 2^-23); the
+    # log-sum takes a logarithm of two units, a product and its constant (2^-22).
+    c = PagedCache(L=1, Hq=4, Hkv=2, d=D, P=16, S=1, max_pages=8, n_phys=9, values=True)
+    md = MemDecay(c, torch.ones((1, 7)), torch.ones((1, 7)), rho=0.9, alpha=1.0, tau_scale=2.0, pinned_mask=0)
+    n = 7 * 16 - 5
+    page = torch.arange(n) // 16
+    values = (2.0 ** page)[:, None, None, None].expand(n, 1, 2, D)
+    c.load_session(0, torch.zeros((n, 1, 2, D)), [1] * n, [3, 8, 1, 0, 7, 2, 5], budget=n, clock=n)
+    c.load_values(0, values)
+    for rows, counted in (([[5, 3, 4, 5], [0, 1 << 30, 1, 2]], [[5, 4, 5], [0, 2]]), ([[6, 6, 6, 6], [-1, 0, 7, 1]], [[6], [0]]),
+                          ([[3, 2, 1, 0], [-5, -4, -3, 6]], [[3], [6]])):
+        blocks = torch.tensor([rows], dtype=torch.int32, device="cuda")
+        count = torch.full((1, 2), 4, dtype=torch.int32, device="cuda")
+        out, lse = torch.zeros((1, 4, D), device="cuda"), torch.zeros((1, 4), device="cuda")
+        md.attend(0, torch.ones((1, 4, D), device="cuda"), out, lse=lse, blocks=blocks, block_count=count)
+        torch.cuda.synchronize()
+        assert md.device_status() == B.MD_DEV_BAD_BLOCK
+        for kv in range(2):
+            v = torch.cat([values[page == o, 0, kv] for o in counted[kv]])
+            ref, rl = O.attend(torch.ones((2, D)), torch.zeros_like(v), v)
+            assert bool(((out[0, 2 * kv:2 * kv + 2].cpu() - ref).abs() <= 2.0 ** -23 * ref).all()), (rows, kv)
+            assert bool(((lse[0, 2 * kv:2 * kv + 2].cpu() - rl).abs() <= 2.0 ** -22 * rl).all()), (rows, kv)
