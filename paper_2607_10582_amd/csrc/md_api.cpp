@@ -31,6 +31,7 @@ struct md_handle_s {
     md::Dims dm;
     md::View v;
     md::Scratch sc;
+    md::CodeTimes ct;    // the quantised tier's conversions (NULLs: not noted)
     hipStream_t stream;
     int device;
     void* scratch;
@@ -287,7 +288,6 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
     dm.aligned = (cfg->flags & MD_FLAG_REGION_ALIGNED) ? 1 : 0;
     dm.quant = cfg->quant_threshold > 0.0f ? 1 : 0;
     dm.quant_thr = cfg->quant_threshold;
-    dm.stamps = dm.quant && cfg->offload_pages == 0 ? 1 : 0;   // (md_key_bounds has no offload tier)
     dm.H = cfg->offload_pages;
     dm.drop_thr = cfg->drop_threshold;
     dm.page_bytes = (size_t)dm.LHkv * dm.P * md::kHeadDim * sizeof(uint16_t);
@@ -548,10 +548,6 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
     if (dm.tail > 1) dm.U_cap += dm.n_wg; else dm.tail = 1;
     size_t bytes = md::scratch_bytes(dm);
     const auto too_large = [&] { return use_static && bytes > md::kStaticScratchBytes + md::row_group_words(dm.S); };
-    if (too_large() && dm.stamps) {   // md_key_bounds then looks at every page of codes again
-        dm.stamps = 0;
-        bytes = md::scratch_bytes(dm);
-    }
     if (too_large() && dm.rows_rg > 0) {   // no room for another path: no observe changes to it later
         limit_first = limit_steady = INT64_MAX;
         if (fused_first && rows_first == 0) rows_first = rows_steady;
@@ -571,6 +567,13 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
         bytes = md::scratch_bytes(dm);
     }
     if (too_large()) return MD_E_TOO_LARGE;
+    // The quantised tier's conversions, for md_key_bounds (which has no offload
+    // tier); where the static scratch has no room for their times it looks at
+    // every page of codes.
+    const size_t times_at = bytes;
+    const bool times = dm.quant && dm.H == 0 &&
+                       (!use_static || bytes + md::code_times_bytes(dm) <= md::kStaticScratchBytes + md::row_group_words(dm.S));
+    if (times) bytes += md::code_times_bytes(dm);
     md_handle_s* h = use_static ? take_static_handle() : new (std::nothrow) md_handle_s();
     if (h == nullptr) return use_static ? MD_E_TOO_LARGE : MD_E_NOMEM;
     if (!use_static) h->static_slot = -1;
@@ -624,6 +627,7 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
         return MD_E_NOMEM;
     }
     md::scratch_carve(dm, h->scratch, &h->sc);
+    h->ct = times ? md::code_times_carve(dm, static_cast<char*>(h->scratch) + times_at) : md::CodeTimes{};
     // counters, status, epoch and the tagged unit statistics start at zero
     // (no step's tag is zero); work lists are empty until the first append.
     // The static scratch keeps what its last handle left there: cleared too.
@@ -794,9 +798,12 @@ md_status md_compact(md_handle h, const int32_t* evict_serial, const int32_t* ev
     if (h->dm.H > 0 &&
         md::launch_offload(h->dm, h->v, h->sc, evict_serial, evict_count, h->stream) != hipSuccess)
         return MD_E_HIP;
-    if (h->dm.quant &&
-        md::launch_quant(h->dm, h->v, h->sc, evict_serial, evict_count, h->stream) != hipSuccess)
-        return MD_E_HIP;
+    if (h->dm.quant) {
+        const hipError_t e = h->ct.coded_at != nullptr
+                                 ? md::launch_quant(h->dm, h->v, h->sc, h->ct, evict_serial, evict_count, h->stream)
+                                 : md::launch_quant(h->dm, h->v, h->sc, evict_serial, evict_count, h->stream);
+        if (e != hipSuccess) return MD_E_HIP;
+    }
     if (timed_launch(h, MD_K_COMPACT, [&] {
             return md::launch_compact(h->dm, h->v, h->sc, evict_serial, evict_count, trusted, h->stream); }) !=
         hipSuccess)
@@ -1041,7 +1048,7 @@ md_status md_key_bounds(md_handle h, int32_t all_pages, int8_t* bounds, int8_t* 
     if (h->dm.H > 0) return MD_E_UNSUPPORTED;
     const OnDevice on(h->device);
     if (!on.ok) return MD_E_HIP;
-    return md::launch_bounds(h->dm, h->v, h->sc, all_pages, bounds, bound_exp, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+    return md::launch_bounds(h->dm, h->v, h->sc, h->ct, all_pages, bounds, bound_exp, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
 }
 
 md_status md_select_blocks(md_handle h, int32_t layer, const md_select_args* a) {

@@ -84,7 +84,7 @@ static_assert(kBoundGroup == kBlkThreads / 64 && kBoundSpan % kBoundGroup == 0, 
 // dims 8 b .. 8 b + 7 of tokens i, i + 4, i + 8, i + 12 of a block (its four
 // loads), so that most of the search over the tokens needs no other lane.
 template <bool QT>
-__global__ void __launch_bounds__(kBlkThreads) k_bounds(Dims dm, View v, Scratch sc, int all, int span,
+__global__ void __launch_bounds__(kBlkThreads) k_bounds(Dims dm, View v, Scratch sc, CodeTimes ct, int all, int span,
                                                         int8_t* __restrict__ bounds, int8_t* __restrict__ bound_exp) {
     __shared__ __align__(16) uint32_t staged[kBoundSpan * kBoundBytes / 4];
     __shared__ int8_t staged_exp[kBoundSpan];
@@ -106,9 +106,9 @@ __global__ void __launch_bounds__(kBlkThreads) k_bounds(Dims dm, View v, Scratch
     uint32_t now = 0, seen = 0;
     uint32_t* looked = nullptr;
     if constexpr (QT) {
-        if (sc.coded_at != nullptr) {
-            looked = sc.looked + (size_t)s * bound_groups(dm) + row0 / kBoundGroup;
-            const uint32_t last = sc.last_coded[2 * s], pass = sc.last_coded[2 * s + 1];
+        if (ct.coded_at != nullptr) {
+            looked = ct.looked + (size_t)s * bound_groups(dm) + row0 / kBoundGroup;
+            const uint32_t last = ct.last[2 * s], pass = ct.last[2 * s + 1];
             now = code_time(sc);
             now -= pass == now ? 0u : 1u;
             if (all) {
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kBlkThreads) k_bounds(Dims dm, View v, Scratch
             const int i = at + (int)threadIdx.x;
             if (i < np - 1) {
                 const int p = table[i];
-                if ((unsigned)p < (unsigned)dm.NP && v.page_format[p] != 0 && (looked == nullptr || sc.coded_at[p] > seen))
+                if ((unsigned)p < (unsigned)dm.NP && v.page_format[p] != 0 && (looked == nullptr || ct.coded_at[p] > seen))
                     found[atomicAdd(&sh_found, 1)] = i;
             }
             __syncthreads();
@@ -588,14 +588,15 @@ __global__ void __launch_bounds__(kPickThreads) k_block_pick(BlockCall c) {
 
 }  // namespace
 
-hipError_t launch_bounds(const Dims& dm, const View& v, const Scratch& sc, int all, int8_t* bounds, int8_t* bound_exp,
-                         hipStream_t st) {
+hipError_t launch_bounds(const Dims& dm, const View& v, const Scratch& sc, const CodeTimes& ct, int all, int8_t* bounds,
+                         int8_t* bound_exp, hipStream_t st) {
     Dims d = dm;
     View vv = v;
     Scratch ss = sc;
+    CodeTimes tt = ct;
     // every page: a workgroup walks all of one, or 64 tiles; the last pages: a tile per wave
     int span = all ? std::min(dm.LHkv, kBoundSpan) : kBoundGroup;
-    void* args[] = {&d, &vv, &ss, &all, &span, &bounds, &bound_exp};
+    void* args[] = {&d, &vv, &ss, &tt, &all, &span, &bounds, &bound_exp};
     const dim3 grid((unsigned)((dm.LHkv + span - 1) / span * (all ? dm.MP : 1)), (unsigned)dm.S);
     const void* fn = dm.quant ? reinterpret_cast<const void*>(&k_bounds<true>) : reinterpret_cast<const void*>(&k_bounds<false>);
     return hipLaunchKernel(fn, grid, dim3(kBlkThreads), args, 0, st);

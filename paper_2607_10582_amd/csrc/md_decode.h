@@ -55,8 +55,29 @@ hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a
 hipError_t launch_append_values(const Dims& dm, const View& v, const uint16_t* new_v, uint16_t* v_pool,
                                 hipStream_t st);
 
-hipError_t launch_bounds(const Dims& dm, const View& v, const Scratch& sc, int all, int8_t* bounds, int8_t* bound_exp,
-                         hipStream_t st);
+// md_key_bounds after a step: tiles (layer, KV head) of one workgroup.
+constexpr int kBoundGroup = 4;
+inline __host__ __device__ int bound_groups(const Dims& dm) { return (dm.LHkv + kBoundGroup - 1) / kBoundGroup; }
+
+// Quantised tier: when pages became codes, and when the bounds of their keys
+// were last looked after.  Behind the handle's scratch, zero at first; NULL
+// where there is no room or no md_key_bounds (offload tier).
+struct CodeTimes {
+    uint32_t* coded_at;   // [NP] each page's conversion (0: none)
+    uint32_t* last;       // [S][2] each session's last conversion, and its last tier pass
+    uint32_t* looked;     // [S][bound_groups] md_key_bounds' last look at the session, by its workgroup
+};
+size_t code_times_bytes(const Dims& dm);
+CodeTimes code_times_carve(const Dims& dm, void* base);
+// Time in half steps: twice the steps observed before the step's conversions,
+// one more from then on.  This is the conversions'.
+__device__ __forceinline__ uint32_t code_time(const Scratch& sc) { return 2u * (uint32_t)sc.counters[1] + 1u; }
+// The quantised tier's pass that notes its conversions.
+hipError_t launch_quant(const Dims& dm, const View& v, const Scratch& sc, const CodeTimes& ct, const int32_t* ev_serial,
+                        const int32_t* ev_count, hipStream_t st);
+
+hipError_t launch_bounds(const Dims& dm, const View& v, const Scratch& sc, const CodeTimes& ct, int all, int8_t* bounds,
+                         int8_t* bound_exp, hipStream_t st);
 uint64_t select_workspace(const Dims& dm);
 hipError_t launch_blocks(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_select_args& a,
                          hipStream_t st);

@@ -160,10 +160,6 @@ __device__ inline bool opens_page(const Dims& dm, const View& v, int s2, const u
     return v.region[(size_t)p * dm.P + slot - 1] != new_region[s2];
 }
 
-// Time of the quantised tier, in half steps: twice the steps observed before
-// the step's conversions, one more from then on.  This is the conversions'.
-__device__ __forceinline__ uint32_t code_time(const Scratch& sc) { return 2u * (uint32_t)sc.counters[1] + 1u; }
-
 // Split a float32 into three bfloat16 terms with x == hi + mid + lo exactly:
 // hi and mid truncate (the differences are exact by Sterbenz's lemma), and
 // what is left has at most 8 significant bits, so lo holds it exactly.

@@ -60,7 +60,6 @@ struct Dims {
     int norm_attn; // 1: the attention term of Eq. 4 is alpha * |K_t| * a_i
     int aligned;   // 1: region-aligned pages (hole slots; n_live counts the tokens)
     int quant;     // 1: quantised tier on (pages may hold 8-bit codes)
-    int stamps;    // 1: the scratch says when pages became codes (the bounds of their keys are then due)
     float quant_thr;  // quantised tier: pages scoring below it are quantised
     int H;         // offload tier: host-memory pages per session (0: off)
     float drop_thr;   // offload tier: pages scoring below it are dropped
@@ -149,14 +148,7 @@ struct Scratch {
     int32_t* rows_done;    // [S] session kernel: row ranges done (low half), void ranges (high half)
     int32_t* rows_read;    // [1] session kernel: workgroups that have read the step's counters (0 between launches)
     float* rows_part;      // [S][ranges][rows_capacity] session kernel: partial masses
-    uint32_t* coded_at;    // [NP] quantised tier: time of each page's conversion (0: none; NULL without stamps)
-    uint32_t* last_coded;  // [S][2] time of each session's last conversion, and of its last tier pass
-    uint32_t* looked;      // [S][bound_groups] time of md_key_bounds' last look at the session, by its workgroup
 };
-
-// md_key_bounds after a step: tiles (layer, KV head) of one workgroup.
-constexpr int kBoundGroup = 4;
-inline __host__ __device__ int bound_groups(const Dims& dm) { return (dm.LHkv + kBoundGroup - 1) / kBoundGroup; }
 
 size_t scratch_bytes(const Dims& dm);
 void scratch_carve(const Dims& dm, void* base, Scratch* sc);

@@ -23,6 +23,7 @@
 
 #include <mutex>
 
+#include "md_decode.h"
 #include "md_device.h"
 
 namespace md {
@@ -1709,12 +1710,13 @@ __global__ void __launch_bounds__(kSelThreads) k_compact(Dims dm, View v, Scratc
 // the block's first 2 KiB (lane l: 16 bytes at 16 l + 1024 j', the codes of
 // its chunks 2 j' and 2 j' + 1) and the scale (four copies) at byte 2048,
 // once every lane has read (the reduction needs them all).
-__global__ void __launch_bounds__(256) k_quant(Dims dm, View v, Scratch sc, const int32_t* __restrict__ ev_serial,
+__global__ void __launch_bounds__(256) k_quant(Dims dm, View v, Scratch sc, CodeTimes ct,
+                                               const int32_t* __restrict__ ev_serial,
                                                const int32_t* __restrict__ ev_count) {
     const int s = blockIdx.y;
     const int np = v.n_pages[s];
     if (!sc.valid[s] || np < 2) return;
-    if (sc.coded_at != nullptr && blockIdx.x == 0 && threadIdx.x == 0) sc.last_coded[2 * s + 1] = code_time(sc);
+    if (ct.coded_at != nullptr && blockIdx.x == 0 && threadIdx.x == 0) ct.last[2 * s + 1] = code_time(sc);
     const int cnt = min(max(ev_count[s], 0), dm.MP);
     const int32_t* evs = ev_serial + (size_t)s * dm.MP;
     const int32_t* ptab = v.page_table + (size_t)s * dm.MP;
@@ -1779,19 +1781,24 @@ __global__ void __launch_bounds__(256) k_quant(Dims dm, View v, Scratch sc, cons
         __syncthreads();
         if (threadIdx.x == 0) {
             v.page_format[phys] = 1;
-            if (sc.coded_at != nullptr) {   // the bounds of its keys are no longer theirs (k_bounds)
+            if (ct.coded_at != nullptr) {   // the bounds of its keys are no longer theirs (k_bounds)
                 const uint32_t now = code_time(sc);
-                sc.coded_at[phys] = now;
-                sc.last_coded[2 * s] = now;
+                ct.coded_at[phys] = now;
+                ct.last[2 * s] = now;
             }
         }
     }
 }
 
+hipError_t launch_quant(const Dims& dm, const View& v, const Scratch& sc, const CodeTimes& ct, const int32_t* ev_serial,
+                        const int32_t* ev_count, hipStream_t st) {
+    hipLaunchKernelGGL(k_quant, dim3(64, dm.S), dim3(256), 0, st, dm, v, sc, ct, ev_serial, ev_count);
+    return hipGetLastError();
+}
+
 hipError_t launch_quant(const Dims& dm, const View& v, const Scratch& sc, const int32_t* ev_serial,
                         const int32_t* ev_count, hipStream_t st) {
-    hipLaunchKernelGGL(k_quant, dim3(64, dm.S), dim3(256), 0, st, dm, v, sc, ev_serial, ev_count);
-    return hipGetLastError();
+    return launch_quant(dm, v, sc, CodeTimes{}, ev_serial, ev_count, st);
 }
 
 hipError_t launch_compact(const Dims& dm, const View& v, const Scratch& sc,
@@ -1892,11 +1899,6 @@ size_t scratch_bytes(const Dims& dm) {
         n += align256((size_t)(dm.S + 1) * sizeof(int32_t));
         n += align256((size_t)dm.S * dm.rows_rg * rows_capacity(dm.rows_nc) * sizeof(float));
     }
-    if (dm.stamps) {
-        n += align256((size_t)dm.NP * sizeof(uint32_t));
-        n += align256((size_t)dm.S * 2 * sizeof(uint32_t));
-        n += align256((size_t)dm.S * bound_groups(dm) * sizeof(uint32_t));
-    }
     return n;
 }
 
@@ -1949,12 +1951,22 @@ void scratch_carve(const Dims& dm, void* base, Scratch* sc) {
         sc->rows_part = reinterpret_cast<float*>(
             take((size_t)dm.S * dm.rows_rg * rows_capacity(dm.rows_nc) * sizeof(float)));
     }
-    sc->coded_at = sc->last_coded = sc->looked = nullptr;
-    if (dm.stamps) {
-        sc->coded_at = reinterpret_cast<uint32_t*>(take((size_t)dm.NP * sizeof(uint32_t)));
-        sc->last_coded = reinterpret_cast<uint32_t*>(take((size_t)dm.S * 2 * sizeof(uint32_t)));
-        sc->looked = reinterpret_cast<uint32_t*>(take((size_t)dm.S * bound_groups(dm) * sizeof(uint32_t)));
-    }
+}
+
+size_t code_times_bytes(const Dims& dm) {
+    return align256((size_t)dm.NP * sizeof(uint32_t)) + align256((size_t)dm.S * 2 * sizeof(uint32_t)) +
+           align256((size_t)dm.S * bound_groups(dm) * sizeof(uint32_t));
+}
+
+CodeTimes code_times_carve(const Dims& dm, void* base) {
+    char* p = static_cast<char*>(base);
+    CodeTimes ct{};
+    ct.coded_at = reinterpret_cast<uint32_t*>(p);
+    p += align256((size_t)dm.NP * sizeof(uint32_t));
+    ct.last = reinterpret_cast<uint32_t*>(p);
+    p += align256((size_t)dm.S * 2 * sizeof(uint32_t));
+    ct.looked = reinterpret_cast<uint32_t*>(p);
+    return ct;
 }
 
 }  // namespace md

@@ -29,7 +29,9 @@ hipError_t launch_append_values(const Dims&, const View&, const uint16_t*, uint1
 hipError_t launch_token(const Dims&, const View&, const Scratch&, int, int, const md_attend_args&, hipStream_t) {
     return ++launched, hipSuccess;
 }
-hipError_t launch_bounds(const Dims&, const View&, const Scratch&, int, int8_t*, int8_t*, hipStream_t) { return ++launched, hipSuccess; }
+hipError_t launch_bounds(const Dims&, const View&, const Scratch&, const CodeTimes&, int, int8_t*, int8_t*, hipStream_t) {
+    return ++launched, hipSuccess;
+}
 hipError_t launch_blocks(const Dims&, const View&, const Scratch&, int, const md_select_args&, hipStream_t) {
     return ++launched, hipSuccess;
 }
