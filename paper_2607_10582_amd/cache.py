@@ -322,6 +322,9 @@ class MemDecay:
     # ---- what a decode engine runs around the step (memdecay.h).  A call of
     # a few sessions takes the device less than 10 us, so the checks keep to
     # comparisons of the tensors' shapes, strides, types and devices.
+    # Like the step's calls they run on the stream that the handle was made
+    # with (``MemDecay(stream=...)``), whatever stream is current: tensors made
+    # or read on another one need a wait in between.
     def norm_rope(self, qkv: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor,
                   v_out: Optional[torch.Tensor] = None, *, q_weight: Optional[torch.Tensor] = None,
                   k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -334,7 +337,8 @@ class MemDecay:
         any distance apart (a layer of the step's q and new_k buffers).
         q_weight, k_weight [d]: None leaves those heads as they are.
         inv_freq float64 [r / 2]: the first r elements of each head turn (None:
-        none).  position int32 [n]; None: each session's clock (n = S)."""
+        none).  position int32 [n]; None: each session's clock (n = S).  Runs
+        on the handle's stream, whatever stream is current."""
         c, dev = self.cache, self._device
         n = qkv.shape[0]
         if qkv.dtype not in TYPES:
@@ -360,7 +364,8 @@ class MemDecay:
 
     def append_values(self, new_v: torch.Tensor):
         """The values bf16 [S][L][Hkv][d] of the tokens that the last observe
-        appended (before anything is compacted)."""
+        appended (before anything is compacted).  Runs on the handle's stream,
+        whatever stream is current."""
         c = self.cache
         B.md_append_values(self.handle, _flat(new_v, torch.bfloat16, c.S * c.L * c.Hkv * c.d, self._device),
                            self._values())
@@ -379,7 +384,9 @@ class MemDecay:
         [S][Hkv][d], itself.  q float32 and out (float32 or bfloat16)
         [S][Hq][d], lse float32 [S][Hq]; sessions of q, out and of the new
         keys and values may be any distance apart.  A row's listed pages
-        ascend (device_status() tells of one that does not)."""
+        ascend (device_status() tells of one that does not).  Runs on the
+        handle's stream, whatever stream is current; the handle has one work
+        space, so captured calls of it are not replayed at the same time."""
         c, dev = self.cache, self._device
         S = c.S
         q_at, q_pitch = _rows(q, torch.float32, S, c.Hq, c.d, dev)
@@ -418,14 +425,17 @@ class MemDecay:
         """Bounds of the keys, once per step behind its compaction: of each
         session's last page and, with the quantised tier, of the pages that
         became codes since the last call; or of every page (after the prompts
-        are loaded; also faster where most of a cache has become codes)."""
+        are loaded; also faster where most of a cache has become codes).
+        Runs on the handle's stream, whatever stream is current."""
         B.md_key_bounds(self.handle, int(all_pages), *self._bounds())
 
     def select_blocks(self, layer: int, q: torch.Tensor, blocks: torch.Tensor, block_count: torch.Tensor, *,
                       first: int = 1, last: int = 1):
         """The pages each session's query q float32 [S][Hq][d] attends to in
         one layer: blocks int32 [S][Hkv][max_blocks], block_count int32
-        [S][Hkv]; always the ``first`` and ``last`` pages of the session."""
+        [S][Hkv]; always the ``first`` and ``last`` pages of the session.  Runs
+        on the handle's stream, whatever stream is current, in the handle's
+        one work space."""
         c = self.cache
         q_at, q_pitch = _rows(q, torch.float32, c.S, c.Hq, c.d, self._device)
         b_at, n_at, most = self._lists(blocks, block_count)

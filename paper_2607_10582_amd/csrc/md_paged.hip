@@ -675,7 +675,10 @@ const void* token_kernel(bool sparse, bool codes) {
 // number of sessions (1,024 of 300 - 700 tokens, two KV heads: 123 us; 142
 // where their words left room for three).  Eight where a few long rows are cut into half as
 // many parts to join (two rows of 131k tokens: 37 against 41 us; 32 rows of
-// 32k: 82 either way).
+// 32k: 82 either way).  The length that the host knows is the page tables':
+// short rows in a table for long ones pay for it (one session of 450 tokens,
+// two KV heads: one cell of eight waves a row, 10.4 us, against two of four and
+// their join, 9.9; of 1,700: 12.9 against 11.1).
 static int attend_waves(const Dims& dm, int n_cu) {
     const int rows = dm.S * dm.Hkv;
     if (rows >= 8 * n_cu) return 2;
