@@ -94,8 +94,8 @@ def test_bounds_follow_pages_into_codes(kw):
     assert md.device_status() == 0
 
 
-def test_bounds_of_codes_without_room_for_stamps():
-    # a static handle whose pages' stamps would not fit the static scratch
+def test_bounds_of_codes_without_room_for_their_times():
+    # a static handle whose pages' times of conversion would not fit the static scratch
     # (only the handle is told of that many pages; none of them is used)
     w = make(seed=32, shape=(1, 1, 1))
     c, ones = w.cache, torch.ones((4, 7))
