@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kBlkThreads) k_bounds(Dims dm, View v, Scratch
         if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(sc.status, kDevCorrupt);
         return;
     }
-    const int page = all ? (int)blockIdx.x / spans : np - 1;
+    int page = all ? (int)blockIdx.x / spans : np - 1;
     const int row0 = ((int)blockIdx.x % spans) * span, row1 = min(dm.LHkv, row0 + span);
     if (page < 0 || page >= np) return;
     // ---- quantised tier: the pages that became codes since this workgroup
@@ -124,164 +124,168 @@ __global__ void __launch_bounds__(kBlkThreads) k_bounds(Dims dm, View v, Scratch
     }
     constexpr int kWaves = kBlkThreads / 64;
     const int lane = lane_id(), b = lane >> 2, i4 = lane & 3;
-    const int32_t* table = v.page_table + (size_t)s * dm.MP;
-    auto tiles_of = [&](int page) {
-        const int p = table[page];
-        if ((unsigned)p >= (unsigned)dm.NP) {
-            if (threadIdx.x == 0) atomicOr(sc.status, kDevCorrupt);
-            return;
-        }
-        int row = row0 + uni(threadIdx.x >> 6);
-        const int slots = min(dm.P, nt - page * dm.P), blocks = (slots + 15) >> 4;
-        const bool codes = QT && v.page_format[p] != 0;
-        // tokens of this lane that count: bit 4 k + j for token 16 k + 4 j + i4
-        uint32_t live = 0;
-        for (int k = 0; k < blocks; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int slot = 16 * k + 4 * j + i4;
-                if (slot < slots && (!dm.aligned || v.region[(size_t)p * dm.P + slot] != (uint8_t)kHole)) live |= 1u << (4 * k + j);
-            }
-        const bool whole = __all(live == (1u << (4 * blocks)) - 1u);
-        const bool upper = i4 >= 2;   // after the search: lanes 2, 3 of four have the upper bounds
-        const size_t tile = (size_t)dm.P * kHeadDim;
-        const uint16_t* keys = v.k_pool + ((size_t)p * dm.LHkv + row) * tile;
-        auto load = [&](const uint16_t* block, u32x4 (&w)[4]) {
-            if (!codes) {
-                const u32x4* kp = reinterpret_cast<const u32x4*>(block) + 16 * b + i4;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = kp[4 * j];
-            } else {   // dims 8 b ..: 8 bytes of each token
-                const uint2* kp = reinterpret_cast<const uint2*>(block) + 128 * (b >> 3) + 2 * (i4 + 16 * (b & 3)) + ((b >> 2) & 1);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint2 c = kp[8 * j];
-                    w[j] = codes_to_bf16<0>(u32x4{c.x, c.y, 0u, 0u});
-                }
-            }
-        };
-        const s16x2 least = {-0x8000, -0x8000}, most = {0x7FFF, 0x7FFF};
-        u32x4 w[4];
-        if (row < row1) load(keys, w);
-        for (; row < row1; row += kWaves) {
-            s16x2 lo[4], hi[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                lo[x] = most;
-                hi[x] = least;
-            }
-            // The four lanes' ends meet, the largest complemented, so that both are
-            // minima: lane i4 ends with the lower bounds (i4 < 2) or the negated
-            // upper ones of dims 8 b + 4 (i4 & 1) .. + 3, infinities and NaNs as the
-            // largest number of their sign.
-            auto meet = [&](float (&z)[4]) {
-                s16x2 half[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) half[x] = min2(upper ? ~hi[x] : lo[x], from_pair<1>(upper ? lo[x] : ~hi[x]));
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const s16x2 all4 = min2(i4 & 1 ? half[2 + x] : half[x], from_pair<0>(i4 & 1 ? half[x] : half[2 + x]));
-                    // (the complement of an ordered number is, but for a last bit that its
-                    // own complement makes up for, its negative's: -1 - n)
-                    const s16x2 c = max2(min2(all4, s16x2{0x7F7F, 0x7F7F}), s16x2{-0x7F80, -0x7F80});
-                    const uint32_t u = __builtin_bit_cast(uint32_t, ordered(upper ? ~c : c)) ^ (upper ? 0x80008000u : 0u);
-                    z[2 * x] = __uint_as_float(u << 16);
-                    z[2 * x + 1] = __uint_as_float(u & 0xFFFF0000u);
-                }
-            };
-            float y[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
-            for (int k = 0; k < blocks; ++k) {
-                u32x4 now[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) now[j] = w[j];
-                const uint16_t* block = keys + (size_t)k * 16 * kHeadDim;
-                // (unconditional, like the attention's: behind the last block it reads that block again, out of the cache)
-                load(k + 1 < blocks ? block + 16 * kHeadDim : row + kWaves < row1 ? keys + kWaves * tile : block, w);
-                if (whole) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        s16x2 o[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) o[j] = ordered(now[j][x]);
-                        lo[x] = min2(lo[x], min2(min2(o[0], o[1]), min2(o[2], o[3])));
-                        hi[x] = max2(hi[x], max2(max2(o[0], o[1]), max2(o[2], o[3])));
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const bool count = (live >> (4 * k + j)) & 1u;
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const s16x2 o = ordered(now[j][x]);
-                            lo[x] = min2(lo[x], count ? o : most);
-                            hi[x] = max2(hi[x], count ? o : least);
-                        }
-                    }
-                }
-                if (codes) {   // each block of codes has its own scale
-                    const float scale = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(block) + 2048);
-                    const bool any = __any(((live >> (4 * k)) & 15u) != 0);
-                    float z[4];
-                    meet(z);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (any) y[x] = fminf(y[x], z[x] * scale);
-                        lo[x] = most;
-                        hi[x] = least;
-                    }
-                }
-            }
-            if (!codes) meet(y);
-            const int e = step_exp(wave_max_dpp(fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3])))));
-            const float unit = power2(-e);
-            uint32_t word = 0;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                // (a number so small that the product becomes 0 still rounds outward)
-                float c = __builtin_amdgcn_fmed3f(floorf(y[x] * unit), -127.0f, y[x] < 0.0f ? -1.0f : 127.0f);
-                c = upper ? -c : c;
-                word |= ((uint32_t)(int)c & 0xFFu) << (8 * x);
-            }
-            staged[(row - row0) * (kBoundBytes / 4) + (upper ? kHeadDim / 4 : 0) + 2 * b + (i4 & 1)] = word;
-            if (lane == 0) staged_exp[row - row0] = (int8_t)e;
-            keys += kWaves * tile;
-        }
-        // The span's bounds go out at once, consecutive in memory (tile by tile as
-        // they are found: 1,446 us against 1,412 for 7.5 GB of keys in pages of 64).
-        // Few as they are, they cost HBM much: the same keys without them take
-        // 1,225 us, 6.1 TB/s, and with them 1,603 in pages of 16, however they are
-        // written (past the caches, or written through).
-        __syncthreads();
-        const size_t at = (size_t)p * dm.LHkv + row0;
-        u32x4* out = reinterpret_cast<u32x4*>(bounds + at * kBoundBytes);
-        for (int i = threadIdx.x; i < (row1 - row0) * (kBoundBytes / 16); i += kBlkThreads)
-            out[i] = reinterpret_cast<const u32x4*>(staged)[i];
-        if ((int)threadIdx.x < row1 - row0) bound_exp[at + threadIdx.x] = staged_exp[threadIdx.x];
-    };
-    tiles_of(page);
-    if constexpr (QT) {
-        if (!due) return;
+    int from = 0, k = 0, n = 0;   // of the pages before `from` the n found due, k of which are taken
+    auto next_due = [&] {
         __shared__ int found[kBlkThreads];
         __shared__ int sh_found;
-        for (int at = 0; at < np - 1; at += kBlkThreads) {
-            __syncthreads();   // the pages found before are done, and what they staged is out
+        while (k == n) {
+            if (from >= np - 1) return -1;
+            __syncthreads();   // the pages found before are taken
             if (threadIdx.x == 0) sh_found = 0;
             __syncthreads();
-            const int i = at + (int)threadIdx.x;
+            const int i = from + (int)threadIdx.x;
             if (i < np - 1) {
-                const int p = table[i];
+                const int p = v.page_table[(size_t)s * dm.MP + i];
                 if ((unsigned)p < (unsigned)dm.NP && v.page_format[p] != 0 && (looked == nullptr || ct.coded_at[p] > seen))
                     found[atomicAdd(&sh_found, 1)] = i;
             }
             __syncthreads();
-            const int n = sh_found;
-            for (int k = 0; k < n; ++k) {
-                tiles_of(found[k]);
-                __syncthreads();
-            }
+            from += kBlkThreads;
+            k = 0;
+            n = sh_found;
         }
-        if (looked != nullptr && threadIdx.x == 0) *looked = now;
+        __syncthreads();   // what the page before staged is out
+        return uni(found[k++]);
+    };
+    for (;;) {   // one page, or the last and each that is due
+        const int p = v.page_table[(size_t)s * dm.MP + page];
+        if ((unsigned)p >= (unsigned)dm.NP) {
+            if (threadIdx.x == 0) atomicOr(sc.status, kDevCorrupt);
+        } else {
+            int row = row0 + uni(threadIdx.x >> 6);
+            const int slots = min(dm.P, nt - page * dm.P), blocks = (slots + 15) >> 4;
+            const bool codes = QT && v.page_format[p] != 0;
+            // tokens of this lane that count: bit 4 k + j for token 16 k + 4 j + i4
+            uint32_t live = 0;
+            for (int k = 0; k < blocks; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int slot = 16 * k + 4 * j + i4;
+                    if (slot < slots && (!dm.aligned || v.region[(size_t)p * dm.P + slot] != (uint8_t)kHole)) live |= 1u << (4 * k + j);
+                }
+            const bool whole = __all(live == (1u << (4 * blocks)) - 1u);
+            const bool upper = i4 >= 2;   // after the search: lanes 2, 3 of four have the upper bounds
+            const size_t tile = (size_t)dm.P * kHeadDim;
+            const uint16_t* keys = v.k_pool + ((size_t)p * dm.LHkv + row) * tile;
+            auto load = [&](const uint16_t* block, u32x4 (&w)[4]) {
+                if (!codes) {
+                    const u32x4* kp = reinterpret_cast<const u32x4*>(block) + 16 * b + i4;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = kp[4 * j];
+                } else {   // dims 8 b ..: 8 bytes of each token
+                    const uint2* kp = reinterpret_cast<const uint2*>(block) + 128 * (b >> 3) + 2 * (i4 + 16 * (b & 3)) + ((b >> 2) & 1);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint2 c = kp[8 * j];
+                        w[j] = codes_to_bf16<0>(u32x4{c.x, c.y, 0u, 0u});
+                    }
+                }
+            };
+            const s16x2 least = {-0x8000, -0x8000}, most = {0x7FFF, 0x7FFF};
+            u32x4 w[4];
+            if (row < row1) load(keys, w);
+            for (; row < row1; row += kWaves) {
+                s16x2 lo[4], hi[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    lo[x] = most;
+                    hi[x] = least;
+                }
+                // The four lanes' ends meet, the largest complemented, so that both are
+                // minima: lane i4 ends with the lower bounds (i4 < 2) or the negated
+                // upper ones of dims 8 b + 4 (i4 & 1) .. + 3, infinities and NaNs as the
+                // largest number of their sign.
+                auto meet = [&](float (&z)[4]) {
+                    s16x2 half[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) half[x] = min2(upper ? ~hi[x] : lo[x], from_pair<1>(upper ? lo[x] : ~hi[x]));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const s16x2 all4 = min2(i4 & 1 ? half[2 + x] : half[x], from_pair<0>(i4 & 1 ? half[x] : half[2 + x]));
+                        // (the complement of an ordered number is, but for a last bit that its
+                        // own complement makes up for, its negative's: -1 - n)
+                        const s16x2 c = max2(min2(all4, s16x2{0x7F7F, 0x7F7F}), s16x2{-0x7F80, -0x7F80});
+                        const uint32_t u = __builtin_bit_cast(uint32_t, ordered(upper ? ~c : c)) ^ (upper ? 0x80008000u : 0u);
+                        z[2 * x] = __uint_as_float(u << 16);
+                        z[2 * x + 1] = __uint_as_float(u & 0xFFFF0000u);
+                    }
+                };
+                float y[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
+                for (int k = 0; k < blocks; ++k) {
+                    u32x4 now[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) now[j] = w[j];
+                    const uint16_t* block = keys + (size_t)k * 16 * kHeadDim;
+                    // (unconditional, like the attention's: behind the last block it reads that block again, out of the cache)
+                    load(k + 1 < blocks ? block + 16 * kHeadDim : row + kWaves < row1 ? keys + kWaves * tile : block, w);
+                    if (whole) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            s16x2 o[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[j] = ordered(now[j][x]);
+                            lo[x] = min2(lo[x], min2(min2(o[0], o[1]), min2(o[2], o[3])));
+                            hi[x] = max2(hi[x], max2(max2(o[0], o[1]), max2(o[2], o[3])));
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const bool count = (live >> (4 * k + j)) & 1u;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const s16x2 o = ordered(now[j][x]);
+                                lo[x] = min2(lo[x], count ? o : most);
+                                hi[x] = max2(hi[x], count ? o : least);
+                            }
+                        }
+                    }
+                    if (codes) {   // each block of codes has its own scale
+                        const float scale = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(block) + 2048);
+                        const bool any = __any(((live >> (4 * k)) & 15u) != 0);
+                        float z[4];
+                        meet(z);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            if (any) y[x] = fminf(y[x], z[x] * scale);
+                            lo[x] = most;
+                            hi[x] = least;
+                        }
+                    }
+                }
+                if (!codes) meet(y);
+                const int e = step_exp(wave_max_dpp(fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3])))));
+                const float unit = power2(-e);
+                uint32_t word = 0;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    // (a number so small that the product becomes 0 still rounds outward)
+                    float c = __builtin_amdgcn_fmed3f(floorf(y[x] * unit), -127.0f, y[x] < 0.0f ? -1.0f : 127.0f);
+                    c = upper ? -c : c;
+                    word |= ((uint32_t)(int)c & 0xFFu) << (8 * x);
+                }
+                staged[(row - row0) * (kBoundBytes / 4) + (upper ? kHeadDim / 4 : 0) + 2 * b + (i4 & 1)] = word;
+                if (lane == 0) staged_exp[row - row0] = (int8_t)e;
+                keys += kWaves * tile;
+            }
+            // The span's bounds go out at once, consecutive in memory (tile by tile as
+            // they are found: 1,446 us against 1,412 for 7.5 GB of keys in pages of 64).
+            // Few as they are, they cost HBM much: the same keys without them take
+            // 1,225 us, 6.1 TB/s, and with them 1,603 in pages of 16, however they are
+            // written (past the caches, or written through).
+            __syncthreads();
+            const size_t at = (size_t)p * dm.LHkv + row0;
+            u32x4* out = reinterpret_cast<u32x4*>(bounds + at * kBoundBytes);
+            for (int i = threadIdx.x; i < (row1 - row0) * (kBoundBytes / 16); i += kBlkThreads)
+                out[i] = reinterpret_cast<const u32x4*>(staged)[i];
+            if ((int)threadIdx.x < row1 - row0) bound_exp[at + threadIdx.x] = staged_exp[threadIdx.x];
+        }
+        if constexpr (QT) {
+            if (due) page = next_due();
+            if (due && page >= 0) continue;
+        }
+        break;
     }
+    if (QT && due && looked != nullptr && threadIdx.x == 0) *looked = now;
 }
 
 // Order-preserving uint32 of a score.
