@@ -583,9 +583,10 @@ md_status md_norm_rope(md_handle h, const md_rope_args* a);
  * md_append_values — the values of the tokens that the last md_observe_step
  * appended: new_v bf16 bits [S][L][Hkv][d] to the slots of v_pool that the
  * keys took.  Sessions that took no token (MD_DEV_CAPACITY, MD_DEV_CORRUPT;
- * the insertion step of their last one is not their clock) are left alone.  MD_E_STATE unless the last md_observe_step had keys and no
- * compaction has followed; MD_E_UNSUPPORTED with an offload tier (its pages
- * come and go without values).
+ * the insertion step of their last one is not their clock) are left alone.
+ * MD_E_STATE unless the last md_observe_step had keys and no compaction has
+ * followed; MD_E_UNSUPPORTED with an offload tier (its pages come and go
+ * without values).
  */
 md_status md_append_values(md_handle h, const uint16_t* new_v, uint16_t* v_pool);
 
