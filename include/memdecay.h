@@ -112,6 +112,10 @@ enum {
                                 /* session and is above the entry before it,    */
                                 /* which need not count itself (of 5 3 4 5: 5,  */
                                 /* 4 and 5 again; of 0 2^30 1: 0)               */
+#define MD_DEV_BAD_ROW    0x40  /* md_write_rows, md_read_rows or md_attend_rows */
+                                /* got a row whose slot its session does not    */
+                                /* hold, or (md_write_rows) that is not above   */
+                                /* the row before it or sits in a page of codes */
 #define MD_DEV_TIMEOUT    0x10  /* a bounded wait between the workgroups of the */
                                 /* fused observation kernel ran out; the step's */
                                 /* attention mass is not valid (the session     */
@@ -678,6 +682,140 @@ md_status md_select_blocks(md_handle h, int32_t layer, const md_select_args* a);
 /* Bytes of the work space of md_attend_token and of md_select_blocks for this
  * handle.  Host-only, no device work. */
 md_status md_decode_workspace(md_handle h, uint64_t* attend_bytes, uint64_t* select_bytes);
+
+/*
+ * Rows of the cache.  A prompt, a chunk of one or a few tokens to verify
+ * enter the cache, attend over it and leave it as ragged rows, one layer at a
+ * time:
+ *
+ *     md_norm_rope -> md_write_rows -> md_attend_rows        (per layer)
+ *
+ * md_row_list says which: rows row_start[s] .. row_start[s + 1] - 1 of a call's
+ * arrays are session s's (row_start ascends from 0; rows behind row_start[S]
+ * belong to nobody and are left as they were), and row_slot tells each row's
+ * slot among the session's (page * P + offset, pages in logical order; NULL:
+ * the session's last ones, in order).  The page tables, counts and region
+ * codes of these slots are there before the call: the caller has placed the
+ * tokens, as with the keys of a prompt.  A row whose slot is not one of the
+ * session's n_tokens counts as not there (MD_DEV_BAD_ROW).
+ *
+ * md_values says where the cache's values are: in v_pool (as above), or in
+ * 8 bits,
+ *  v_codes      uint8 FP8 E4M3 codes [NP][L][Hkv][P/16][d/64][4][16][4][4]:
+ *               element (t, e) of a (page, l, kv) tile sits at (t & ~15) * d
+ *               + (e / 64) * 1024 + ((t / 4) % 4) * 256 + (e % 16) * 16
+ *               + ((e / 16) % 4) * 4 + t % 4
+ *  v_scale      float [NP][L][Hkv][P/16]: value = scale * code, for each block
+ *               of 16 tokens and KV head: scale = max|v| / 448 over the block's
+ *               tokens, code = the E4M3 value nearest to v / scale (ties to
+ *               even; 0 where the scale is 0).  A block with a value that is
+ *               not finite has a NaN scale: all of it reads as NaN.
+ *  v_open       uint16 bf16 bits [S][L][Hkv][16][d]: the values of the block
+ *               that each session wrote last (zeros behind its last token).
+ * A block's codes are those of its bf16 values, whichever calls wrote them:
+ * rows that go on inside a block take its earlier values from v_open, which
+ * holds them when a session's rows are written in order.  Half the bytes of a
+ * bf16 pool, each value off by at most 2^-4 of itself or 2^-10 scale.
+ */
+typedef struct md_row_list {
+    const int32_t* row_start; /* [S + 1]                                                     */
+    const int32_t* row_slot;  /* [n_rows], or NULL                                           */
+    int32_t n_rows;           /* rows of the call's arrays, >= 0                             */
+    int32_t reserved;         /* 0                                                           */
+} md_row_list;
+
+typedef struct md_values {
+    uint16_t* v_pool;         /* bf16 values; or NULL and                                    */
+    uint8_t* v_codes;         /* 8-bit values,                                               */
+    float* v_scale;           /* their scales,                                               */
+    uint16_t* v_open;         /* and the open blocks (for the calls that write)              */
+} md_values;                  /* all 16-byte aligned                                         */
+
+/*
+ * md_append_codes — md_append_values into 8-bit values: the values of the
+ * tokens that the last md_observe_step appended, new_v bf16 bits
+ * [S][L][Hkv][d].  A block whose scale does not change has its new codes
+ * written; one whose scale grows, all of them.  Refusals as for
+ * md_append_values.
+ */
+md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v);
+
+/*
+ * md_write_rows — keys and values of ragged rows of one layer into the pools.
+ * The slots of a session's rows ascend; a row that is not above the one
+ * before it, or whose page holds 8-bit keys, does not count (MD_DEV_BAD_ROW).
+ * In the 8-bit pool a session's rows go on in one block after another: the
+ * slots of a block behind the last row written to it get the code 0.
+ * MD_E_UNSUPPORTED with an offload tier.
+ */
+typedef struct md_write_args {
+    md_row_list rows;
+    const uint16_t* k;        /* bf16 [n_rows][Hkv d], rows stride elements apart (a multiple */
+    const uint16_t* v;        /* of 8); either may be NULL, and is then not written          */
+    int64_t stride;
+    md_values values;
+} md_write_args;
+md_status md_write_rows(md_handle h, int32_t layer, const md_write_args* a);
+
+/*
+ * md_read_rows — keys and values of ragged rows of one layer out of the pools,
+ * in any order of slots: bf16 ones as they are, codes as the float32 product
+ * of scale and code, rounded once for bf16 outputs.  A row that does not count
+ * gets zeros.  MD_E_UNSUPPORTED with an offload tier.
+ */
+typedef struct md_read_args {
+    md_row_list rows;
+    void* k;                  /* [n_rows][Hkv d], rows stride elements apart (a multiple of  */
+    void* v;                  /* 8); either may be NULL                                      */
+    int64_t stride;
+    int32_t type;             /* MD_F32 or MD_BF16                                           */
+    md_values values;
+} md_read_args;
+md_status md_read_rows(md_handle h, int32_t layer, const md_read_args* a);
+
+/*
+ * md_attend_values — md_attend_token over values in either form, all of the
+ * cache or a window of it: with window > 0 the token at slot p (the slot
+ * behind the session's last, or without new_k the last one) sees the slots
+ * j <= p with p - j < window or j < sinks.  a's own v_pool is not looked at;
+ * everything else as for md_attend_token.  MD_E_UNSUPPORTED for a window
+ * with lists of blocks.
+ */
+md_status md_attend_values(md_handle h, int32_t layer, const md_attend_args* a, const md_values* v, int32_t window,
+                           int32_t sinks);
+
+/*
+ * md_attend_rows — attention of ragged rows in one layer over their sessions'
+ * cached tokens, their own among them (md_write_rows comes first): the row at
+ * slot p sees the tokens at slots j <= p, with window > 0 those of them with
+ * p - j < window or j < sinks.
+ *   out_h = sum_i softmax_i(q_h . k_i / sqrt(d)) v_i,  lse_h = ln sum_i exp(q_h . k_i / sqrt(d))
+ * Logits, statistics and sums are float32.  bf16 queries with bf16 outputs:
+ * products of bf16 queries, and softmax weights rounded to bf16 once, whose
+ * sum is that of the rounded ones.  Else queries and weights enter the
+ * products as three bf16 terms, as in md_attend_token.  A row without any
+ * token gets zeros and lse = -infinity.  The same inputs give the same bits.
+ * MD_E_UNSUPPORTED with an offload tier, and where n_rows Hq / Hkv + 256 S
+ * comes to 2^31.
+ */
+typedef struct md_rows_args {
+    md_row_list rows;
+    const void* q;            /* [n_rows][Hq d], rows q_stride elements apart (a multiple    */
+    int64_t q_stride;         /* of 8)                                                       */
+    int32_t q_type;           /* MD_F32 or MD_BF16                                           */
+    int32_t out_type;         /* MD_F32 or MD_BF16                                           */
+    void* out;                /* [n_rows][Hq d], rows out_stride elements apart (a multiple  */
+    int64_t out_stride;       /* of 8)                                                       */
+    float* lse;               /* [n_rows][Hq] or NULL                                        */
+    int32_t window, sinks;    /* >= 0; window 0: every token up to the row's own             */
+    md_values values;
+    void* workspace;          /* md_rows_workspace's bytes; as in md_attend_args             */
+} md_rows_args;
+md_status md_attend_rows(md_handle h, int32_t layer, const md_rows_args* a);
+
+/* Bytes of the work space of md_attend_rows for this handle (any number of
+ * rows).  Host-only, no device work. */
+md_status md_rows_workspace(md_handle h, uint64_t* bytes);
 
 /* Release the scratch and the handle (synchronises the stream first). */
 md_status md_destroy(md_handle h);

@@ -28,6 +28,7 @@ MD_DEV_BAD_EVICT = 0x4
 MD_DEV_CORRUPT = 0x8
 MD_DEV_TIMEOUT = 0x10
 MD_DEV_BAD_BLOCK = 0x20
+MD_DEV_BAD_ROW = 0x40
 
 MD_F32, MD_BF16, MD_F16 = range(3)   # types of a call's arrays
 
@@ -44,7 +45,8 @@ EXPORTS = ("md_abi_version", "md_status_str", "md_init", "md_init_static", "md_o
            "md_profile_enable", "md_profile_read", "md_read_counters", "md_kernel_config", "md_observe_path",
            "md_calib_accumulate", "md_calib_fit",
            "md_norm_rope", "md_append_values", "md_attend_token", "md_key_bounds", "md_select_blocks",
-           "md_decode_workspace", "md_destroy")
+           "md_decode_workspace", "md_append_codes", "md_write_rows", "md_read_rows", "md_attend_values",
+           "md_attend_rows", "md_rows_workspace", "md_destroy")
 
 # paths of md_observe_path
 PATHS = ("multi-kernel", "fused", "session")
@@ -104,11 +106,41 @@ class md_select_args(ctypes.Structure):
                 ("workspace", ctypes.c_void_p)]
 
 
-# The same three as bytes, packed in one step: what a call of a few
+class md_row_list(ctypes.Structure):
+    _fields_ = [("row_start", ctypes.c_void_p), ("row_slot", ctypes.c_void_p), ("n_rows", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class md_values(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("v_pool", "v_codes", "v_scale", "v_open")]
+
+
+class md_write_args(ctypes.Structure):
+    _fields_ = [("rows", md_row_list), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride", ctypes.c_int64),
+                ("values", md_values)]
+
+
+class md_read_args(ctypes.Structure):
+    _fields_ = [("rows", md_row_list), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("values", md_values)]
+
+
+class md_rows_args(ctypes.Structure):
+    _fields_ = [("rows", md_row_list), ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("q_type", ctypes.c_int32),
+                ("out_type", ctypes.c_int32), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("values", md_values),
+                ("workspace", ctypes.c_void_p)]
+
+
+# The argument structs as bytes, packed in one step: what a call of a few
 # microseconds passes (a ctypes.Structure takes longer to fill than the call).
 ROPE_ARGS = struct.Struct("@PqiiPPfiPPiPqPPq")
 ATTEND_ARGS = struct.Struct("@PqPPqPPPiiPqPP")
 SELECT_ARGS = struct.Struct("@PqPPiiiPPP")
+VALUES = struct.Struct("@PPPP")
+WRITE_ARGS = struct.Struct("@PPiiPPqPPPP")
+READ_ARGS = struct.Struct("@PPiiPPqi4xPPPP")
+ROWS_ARGS = struct.Struct("@PPiiPqiiPqPiiPPPPP")
 
 
 class MemDecayError(RuntimeError):
@@ -203,6 +235,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.md_select_blocks.argtypes = [vp, i32, vp]
     lib.md_decode_workspace.restype = i32
     lib.md_decode_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
+    lib.md_append_codes.restype = i32
+    lib.md_append_codes.argtypes = [vp, vp, vp]
+    lib.md_write_rows.restype = i32
+    lib.md_write_rows.argtypes = [vp, i32, vp]
+    lib.md_read_rows.restype = i32
+    lib.md_read_rows.argtypes = [vp, i32, vp]
+    lib.md_attend_values.restype = i32
+    lib.md_attend_values.argtypes = [vp, i32, vp, vp, i32, i32]
+    lib.md_attend_rows.restype = i32
+    lib.md_attend_rows.argtypes = [vp, i32, vp]
+    lib.md_rows_workspace.restype = i32
+    lib.md_rows_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.md_destroy.restype = i32
     lib.md_destroy.argtypes = [vp]
     _lib = lib
@@ -374,6 +418,35 @@ def md_decode_workspace(h: int):
     out = (ctypes.c_uint64(0), ctypes.c_uint64(0))
     _check("md_decode_workspace", load_library().md_decode_workspace(h, ctypes.byref(out[0]), ctypes.byref(out[1])))
     return int(out[0].value), int(out[1].value)
+
+
+def md_append_codes(h: int, new_v: int, values) -> int:
+    """values: md_values, or its fields packed by VALUES (so for the structs of
+    the calls below)."""
+    return _check("md_append_codes", load_library().md_append_codes(h, new_v, _arg(values)))
+
+
+def md_write_rows(h: int, layer: int, args) -> int:
+    return _check("md_write_rows", load_library().md_write_rows(h, layer, _arg(args)))
+
+
+def md_read_rows(h: int, layer: int, args) -> int:
+    return _check("md_read_rows", load_library().md_read_rows(h, layer, _arg(args)))
+
+
+def md_attend_values(h: int, layer: int, args, values, window: int = 0, sinks: int = 0) -> int:
+    return _check("md_attend_values", load_library().md_attend_values(h, layer, _arg(args), _arg(values), window, sinks))
+
+
+def md_attend_rows(h: int, layer: int, args) -> int:
+    return _check("md_attend_rows", load_library().md_attend_rows(h, layer, _arg(args)))
+
+
+def md_rows_workspace(h: int) -> int:
+    """Bytes of the work space of md_attend_rows."""
+    out = ctypes.c_uint64(0)
+    _check("md_rows_workspace", load_library().md_rows_workspace(h, ctypes.byref(out)))
+    return int(out.value)
 
 
 def md_destroy(h: int) -> int:

@@ -24,10 +24,13 @@ class PagedCache:
     """Device buffers of one batch of sessions (layouts as in memdecay.h)."""
 
     def __init__(self, *, L: int, Hq: int, Hkv: int, d: int, P: int, S: int,
-                 max_pages: int, n_phys: int, device="cuda", offload_pages: int = 0, values: bool = False,
+                 max_pages: int, n_phys: int, device="cuda", offload_pages: int = 0, values=False,
                  bounds: bool = False):
-        # values: a pool of values beside the keys (MemDecay.attend);
-        # bounds: 8-bit bounds of each page's keys (MemDecay.select_blocks)
+        # values: a pool of values beside the keys (MemDecay.attend), True for
+        # bf16 ones, "e4m3" for 8-bit codes with a scale per 16 tokens and KV
+        # head; bounds: 8-bit bounds of each page's keys (MemDecay.select_blocks)
+        if values not in (False, True, "e4m3"):
+            raise ValueError('values are True (bf16), "e4m3" or False')
         self.L, self.Hq, self.Hkv, self.d, self.P = L, Hq, Hkv, d, P
         self.S, self.max_pages, self.n_phys = S, max_pages, n_phys
         self.device = torch.device(device)
@@ -54,7 +57,13 @@ class PagedCache:
         # pages past a session's table are never read, so the pools are left
         # uninitialised
         self.v_pool = torch.empty((n_phys, L, Hkv, P // 16, d // 32, 4, 16, 2, 4), dtype=torch.bfloat16,
-                                  device=dev) if values else None
+                                  device=dev) if values is True else None
+        coded = values == "e4m3"
+        self.v_codes = torch.empty((n_phys, L, Hkv, P // 16, d // 64, 4, 16, 4, 4), dtype=torch.uint8,
+                                   device=dev) if coded else None
+        self.v_scale = torch.empty((n_phys, L, Hkv, P // 16), dtype=torch.float32, device=dev) if coded else None
+        # the block that each session wrote last, in bf16
+        self.v_open = torch.zeros((S, L, Hkv, 16, d), dtype=torch.bfloat16, device=dev) if coded else None
         self.key_bounds = torch.empty((n_phys, L, Hkv, 2, d), dtype=torch.int8, device=dev) if bounds else None
         self.bound_exp = torch.empty((n_phys, L, Hkv), dtype=torch.int8, device=dev) if bounds else None
         # offload tier: offload_pages host-memory pages per session, their
@@ -116,6 +125,29 @@ class PagedCache:
         return pages.permute(0, 3, 5, 8, 1, 2, 4, 7, 6).reshape(m, nb * 16, L, Hkv, db * 32)
 
     @staticmethod
+    def to_code_layout(v: torch.Tensor):
+        """Values [m][P][L][Hkv][d] of m pages -> their codes
+        [m][L][Hkv][P/16][d/64][4][16][4][4] (uint8) and scales
+        [m][L][Hkv][P/16] (memdecay.h)."""
+        m, P, L, Hkv, d = v.shape
+        x = v.float().view(m, P // 16, 16, L, Hkv, d)
+        top = x.abs().amax((2, 5))
+        # (by a tensor: a number's division may become a product with its reciprocal)
+        scale = torch.where(torch.isfinite(top), top / torch.full_like(top, 448.0), math.nan)
+        q = x / torch.where(scale > 0, scale, 1.0)[:, :, None, :, :, None]
+        q = torch.where((scale > 0)[:, :, None, :, :, None], q, 0.0)
+        codes = q.to(torch.float8_e4m3fn).view(torch.uint8).view(m, P // 16, 4, 4, L, Hkv, d // 64, 4, 16)
+        return codes.permute(0, 4, 5, 1, 6, 2, 8, 7, 3).contiguous(), scale.permute(0, 2, 3, 1).contiguous()
+
+    @staticmethod
+    def from_code_layout(codes: torch.Tensor, scale: torch.Tensor) -> torch.Tensor:
+        """The inverse but for the rounding: pages of codes and their scales ->
+        float32 values [m][P][L][Hkv][d]."""
+        m, L, Hkv, nb, half = codes.shape[:5]
+        x = codes.contiguous().view(torch.float8_e4m3fn).float() * scale[..., None, None, None, None, None]
+        return x.permute(0, 3, 5, 8, 1, 2, 4, 7, 6).reshape(m, nb * 16, L, Hkv, half * 64)
+
+    @staticmethod
     def positions(region, P: int, region_aligned: bool) -> np.ndarray:
         """Slot position (page * P + offset) of each prompt token in the
         session's page sequence: consecutive, or with region-aligned pages a
@@ -148,6 +180,23 @@ class PagedCache:
         t_ins[i] (default i) and importance 0; holes get the hole code."""
         P = self.P
         n = int(keys.shape[0])
+        if len(region) != n:
+            raise ValueError("need one region code per token")
+        ids, posd, m = self.place_session(s, region, page_ids, budget, clock, t_ins, region_aligned)
+        k = keys.to(self.device, torch.bfloat16)
+        full = torch.zeros((m * P,) + tuple(k.shape[1:]), dtype=k.dtype, device=k.device)
+        full[posd] = k
+        # [m][P][L][Hkv][d] -> [m][L][Hkv][P][d]
+        self.k_pool.index_copy_(0, ids, self.to_pool_layout(full.view(m, P, self.L, self.Hkv, self.d)))
+
+    def place_session(self, s: int, region, page_ids: Sequence[int], budget: int, clock: int, t_ins=None,
+                      region_aligned: bool = False):
+        """load_session without its keys, for a prompt whose rows come through
+        MemDecay.write_rows: the page table, the counts and every token's
+        region and times.  Returns the page ids, the slot of each token
+        (``positions``) and the number of pages."""
+        P = self.P
+        n = len(region)
         pos = self.positions(region, P, region_aligned)
         n_pos = int(pos[-1]) + 1 if n else 0
         m = (n_pos + P - 1) // P
@@ -155,11 +204,6 @@ class PagedCache:
             raise ValueError("need one page id per page of the layout, within max_pages")
         ids = torch.as_tensor(np.asarray(page_ids, dtype=np.int64), device=self.device)
         posd = torch.as_tensor(pos, device=self.device)
-        k = keys.to(self.device, torch.bfloat16)
-        full = torch.zeros((m * P,) + tuple(k.shape[1:]), dtype=k.dtype, device=k.device)
-        full[posd] = k
-        # [m][P][L][Hkv][d] -> [m][L][Hkv][P][d]
-        self.k_pool.index_copy_(0, ids, self.to_pool_layout(full.view(m, P, self.L, self.Hkv, self.d)))
         reg = torch.as_tensor(np.asarray(region, dtype=np.uint8), device=self.device)
         t0 = torch.arange(n, dtype=torch.int32, device=self.device) if t_ins is None else \
             torch.as_tensor(np.asarray(t_ins, dtype=np.int32), device=self.device)
@@ -185,13 +229,14 @@ class PagedCache:
         self.clock[s] = clock
         self.next_serial[s] = m
         self.budget[s] = budget
+        return ids, posd, m
 
     def load_values(self, s: int, values: torch.Tensor, region=None):
         """Place the values bf16 [n][L][Hkv][d] of a session's prompt next to
         the keys that ``load_session`` placed, one for each of its tokens;
         region: the same codes, with region-aligned pages only."""
         n, P = int(values.shape[0]), self.P
-        if self.v_pool is None:
+        if self.v_pool is None and self.v_codes is None:
             raise ValueError("the cache has no values (PagedCache(values=True))")
         if region is not None and len(region) != n:
             raise ValueError("need one region code per token")
@@ -205,7 +250,15 @@ class PagedCache:
         full = torch.zeros((m * P,) + tuple(values.shape[1:]), dtype=torch.bfloat16, device=self.device)
         full[torch.as_tensor(pos, device=self.device)] = values.to(self.device, torch.bfloat16)
         ids = self.page_table[s, :m].long()
-        self.v_pool.index_copy_(0, ids, self.to_value_layout(full.view(m, P, self.L, self.Hkv, self.d)))
+        full = full.view(m, P, self.L, self.Hkv, self.d)
+        if self.v_pool is not None:
+            self.v_pool.index_copy_(0, ids, self.to_value_layout(full))
+            return
+        codes, scale = self.to_code_layout(full)
+        self.v_codes.index_copy_(0, ids, codes)
+        self.v_scale.index_copy_(0, ids, scale)
+        at = (slots - 1) % P // 16 * 16
+        self.v_open[s] = full[-1, at:at + 16].permute(1, 2, 0, 3)
 
     def set_free_pages(self, ids: Sequence[int]):
         """The free list: ids pop from the end."""
@@ -260,9 +313,9 @@ class MemDecay:
 
         # work space of the decode operators (one per handle: calls on its
         # stream run one after another)
-        self._attend_ws = self._select_ws = None
+        self._attend_ws = self._select_ws = self._rows_ws = None
         self._device = cache.k_pool.get_device()
-        if cache.v_pool is not None:   # now, so that a captured call allocates nothing
+        if cache.v_pool is not None or cache.v_codes is not None:   # now, so that a captured call allocates nothing
             self._workspace(True)
         if cache.key_bounds is not None:
             self._workspace(False)
@@ -364,11 +417,15 @@ class MemDecay:
 
     def append_values(self, new_v: torch.Tensor):
         """The values bf16 [S][L][Hkv][d] of the tokens that the last observe
-        appended (before anything is compacted).  Runs on the handle's stream,
-        whatever stream is current."""
+        appended (before anything is compacted); in a cache of 8-bit values
+        they become codes.  Runs on the handle's stream, whatever stream is
+        current."""
         c = self.cache
-        B.md_append_values(self.handle, _flat(new_v, torch.bfloat16, c.S * c.L * c.Hkv * c.d, self._device),
-                           self._values())
+        new_at = _flat(new_v, torch.bfloat16, c.S * c.L * c.Hkv * c.d, self._device)
+        if c.v_codes is not None:
+            B.md_append_codes(self.handle, new_at, B.VALUES.pack(*self._value_pools(True)))
+        else:
+            B.md_append_values(self.handle, new_at, self._values())
 
     def _values(self) -> int:
         v = self.cache.v_pool
@@ -376,9 +433,111 @@ class MemDecay:
             raise ValueError("the cache has no values (PagedCache(values=True))")
         return _flat(v, torch.bfloat16, self.cache.k_pool.numel(), self._device)
 
+    def _value_pools(self, written: bool):
+        """The fields of md_values."""
+        c, dev = self.cache, self._device
+        if c.v_codes is None:
+            return self._values(), 0, 0, 0
+        n = c.k_pool.numel()
+        return (0, _flat(c.v_codes, torch.uint8, n, dev), _flat(c.v_scale, torch.float32, n // (16 * c.d), dev),
+                _flat(c.v_open, torch.bfloat16, c.S * c.L * c.Hkv * 16 * c.d, dev) if written else 0)
+
+    # ---- rows of the cache: prompts, chunks of them, tokens to verify.  The
+    # rows of a call are ragged: row_start int32 [S + 1] tells where each
+    # session's begin, row_slot int32 [n] their slots (None: each session's
+    # last ones), which PagedCache.place_session has set up.  The tensors stay
+    # on the device; a row that is not in its session's slots counts as not
+    # there (device_status() tells of it).
+    def _row_list(self, n: int, row_start: torch.Tensor, row_slot: Optional[torch.Tensor]):
+        dev = self._device
+        return (_flat(row_start, torch.int32, self.cache.S + 1, dev),
+                0 if row_slot is None else _flat(row_slot, torch.int32, n, dev), n, 0)
+
+    def _kv_rows(self, k, v, dtypes):
+        """Rows, addresses, distance and type of keys and values [n][Hkv][d], either of which may be left out."""
+        c, dev = self.cache, self._device
+        one = k if k is not None else v
+        if one is None:
+            raise ValueError("rows of keys, of values, or both")
+        n, dtype = one.shape[0], one.dtype
+        if dtype not in dtypes:
+            raise ValueError(f"expected {' or '.join(map(str, dtypes))} rows, got {dtype}")
+        k_at = v_at = 0
+        pitches = []
+        for x in (k, v):
+            if x is not None:
+                at, pitch = _rows(x, dtype, n, c.Hkv, c.d, dev)
+                pitches.append(pitch)
+                if x is k:
+                    k_at = at
+                if x is v:
+                    v_at = at
+        if len(set(pitches)) > 1:
+            raise ValueError("keys and values have rows the same distance apart")
+        return n, k_at, v_at, pitches[0], dtype
+
+    def write_rows(self, layer: int, row_start: torch.Tensor, k: Optional[torch.Tensor] = None,
+                   v: Optional[torch.Tensor] = None, *, row_slot: Optional[torch.Tensor] = None):
+        """Keys and values bf16 [n][Hkv][d] (rows any distance apart) of one
+        layer into the pools, values as codes in a cache of 8-bit values.  A
+        session's slots ascend, and its rows are written in order.  Keys of
+        pages that hold 8-bit keys are left alone.  Runs on the handle's
+        stream, whatever stream is current."""
+        n, k_at, v_at, pitch, _ = self._kv_rows(k, v, (torch.bfloat16,))
+        rows = self._row_list(n, row_start, row_slot)
+        if n == 0:
+            return
+        B.md_write_rows(self.handle, layer, B.WRITE_ARGS.pack(
+            *rows, k_at, v_at, pitch, *((0, 0, 0, 0) if v is None else self._value_pools(True))))
+
+    def read_rows(self, layer: int, row_start: torch.Tensor, k_out: Optional[torch.Tensor] = None,
+                  v_out: Optional[torch.Tensor] = None, *, row_slot: Optional[torch.Tensor] = None):
+        """Keys and values of one layer out of the pools into k_out and v_out
+        [n][Hkv][d], bfloat16 or float32, rows any distance apart: what 8-bit
+        codes stand for, bf16 ones as they are.  Runs on the handle's stream,
+        whatever stream is current."""
+        n, k_at, v_at, pitch, dtype = self._kv_rows(k_out, v_out, (torch.bfloat16, torch.float32))
+        rows = self._row_list(n, row_start, row_slot)
+        if n == 0:
+            return
+        B.md_read_rows(self.handle, layer, B.READ_ARGS.pack(
+            *rows, k_at, v_at, pitch, TYPES[dtype], *((0, 0, 0, 0) if v_out is None else self._value_pools(False))))
+
+    def attend_rows(self, layer: int, q: torch.Tensor, out: torch.Tensor, row_start: torch.Tensor, *,
+                    row_slot: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                    lse: Optional[torch.Tensor] = None):
+        """Attention of rows [n][Hq][d] over their sessions' cached tokens up to
+        their own (write_rows comes first); with window > 0 over those less
+        than ``window`` slots back and the first ``sinks``.  q and out float32
+        or bfloat16, rows any distance apart, lse float32 [n][Hq].  bf16 q and
+        out take the faster products; float32 on either side the exact ones.
+        Runs on the handle's stream, whatever stream is current, in a work
+        space of the handle's, so that captured calls of it are not replayed
+        at the same time; the first call allocates it and is not captured."""
+        c, dev = self.cache, self._device
+        n = q.shape[0]
+        if q.dtype not in (torch.float32, torch.bfloat16) or out.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"expected float32 or bfloat16 queries and outputs, got {q.dtype} and {out.dtype}")
+        q_at, q_pitch = _rows(q, q.dtype, n, c.Hq, c.d, dev)
+        out_at, out_pitch = _rows(out, out.dtype, n, c.Hq, c.d, dev)
+        rows = self._row_list(n, row_start, row_slot)
+        lse_at = 0 if lse is None else _flat(lse, torch.float32, n * c.Hq, dev)
+        pools = self._value_pools(False)
+        if n == 0:
+            return
+        if self._rows_ws is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("attend_rows allocates its work space in its first call: make one before the capture")
+            with torch.cuda.stream(self.stream):
+                self._rows_ws = torch.zeros(max(B.md_rows_workspace(self.handle), 16), dtype=torch.uint8, device=c.device)
+        B.md_attend_rows(self.handle, layer, B.ROWS_ARGS.pack(
+            *rows, q_at, q_pitch, TYPES[q.dtype], TYPES[out.dtype], out_at, out_pitch, lse_at, window, sinks, *pools,
+            self._rows_ws.data_ptr()))
+
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, *, new_k: Optional[torch.Tensor] = None,
                new_v: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
-               blocks: Optional[torch.Tensor] = None, block_count: Optional[torch.Tensor] = None):
+               blocks: Optional[torch.Tensor] = None, block_count: Optional[torch.Tensor] = None, window: int = 0,
+               sinks: int = 0):
         """Attention of one token of every session in one layer over its
         cached tokens (or the listed pages) and, with new_k and new_v bf16
         [S][Hkv][d], itself.  q float32 and out (float32 or bfloat16)
@@ -386,7 +545,10 @@ class MemDecay:
         keys and values may be any distance apart.  A row's listed pages
         ascend (device_status() tells of one that does not).  Runs on the
         handle's stream, whatever stream is current; the handle has one work
-        space, so captured calls of it are not replayed at the same time."""
+        space, so captured calls of it are not replayed at the same time.
+        With window > 0 the token (the slot behind the session's last, or
+        without new_k the last one) sees the slots less than ``window`` back
+        and the first ``sinks`` ones; not together with blocks."""
         c, dev = self.cache, self._device
         S = c.S
         q_at, q_pitch = _rows(q, torch.float32, S, c.Hq, c.d, dev)
@@ -403,9 +565,14 @@ class MemDecay:
         if blocks is None and block_count is not None:
             raise ValueError("counts without their blocks")
         b_at, n_at, most = (0, 0, 0) if blocks is None else self._lists(blocks, block_count)
-        B.md_attend_token(self.handle, layer, B.ATTEND_ARGS.pack(
-            q_at, q_pitch, k_at, v_at, kv_pitch, self._values(), b_at, n_at, most, TYPES[out.dtype], out_at, out_pitch,
-            0 if lse is None else _flat(lse, torch.float32, S * c.Hq, dev), self._workspace(True).data_ptr()))
+        pools = (self._values(),) if c.v_codes is None else self._value_pools(False)
+        args = B.ATTEND_ARGS.pack(
+            q_at, q_pitch, k_at, v_at, kv_pitch, pools[0], b_at, n_at, most, TYPES[out.dtype], out_at, out_pitch,
+            0 if lse is None else _flat(lse, torch.float32, S * c.Hq, dev), self._workspace(True).data_ptr())
+        if window == 0 and len(pools) == 1:
+            B.md_attend_token(self.handle, layer, args)
+        else:
+            B.md_attend_values(self.handle, layer, args, B.VALUES.pack(*pools, *(0,) * (4 - len(pools))), window, sinks)
 
     def _lists(self, blocks: torch.Tensor, count: torch.Tensor):
         c, dev = self.cache, self._device

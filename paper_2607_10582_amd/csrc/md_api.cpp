@@ -1019,29 +1019,6 @@ md_status md_append_values(md_handle h, const uint16_t* new_v, uint16_t* v_pool)
     return md::launch_append_values(h->dm, h->v, new_v, v_pool, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
 }
 
-md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a) {
-    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L) return MD_E_INVALID;
-    const int64_t hq = (int64_t)h->dm.Hq * md::kHeadDim, hkv = (int64_t)h->dm.Hkv * md::kHeadDim;
-    if (a->q == nullptr || !aligned(a->q, 16) || a->q_stride < hq || a->q_stride % 4 != 0) return MD_E_INVALID;
-    if ((a->new_k == nullptr) != (a->new_v == nullptr)) return MD_E_INVALID;
-    if (a->new_k != nullptr && (!aligned(a->new_k, 16) || !aligned(a->new_v, 16) || a->kv_stride < hkv ||
-                                a->kv_stride % 8 != 0))
-        return MD_E_INVALID;
-    if (a->v_pool == nullptr || !aligned(a->v_pool, 16)) return MD_E_INVALID;
-    if ((a->blocks == nullptr) != (a->block_count == nullptr)) return MD_E_INVALID;
-    if (a->blocks != nullptr && (!aligned(a->blocks, 4) || !aligned(a->block_count, 4) || a->max_blocks < 1 ||
-                                 a->max_blocks > md::kMaxPages))
-        return MD_E_INVALID;
-    if (a->out == nullptr || !aligned(a->out, 16) || a->out_stride < hq || a->out_stride % 8 != 0 ||
-        (a->out_type != MD_F32 && a->out_type != MD_BF16) || !aligned(a->lse, 4))
-        return MD_E_INVALID;
-    if (a->workspace == nullptr || !aligned(a->workspace, 16)) return MD_E_INVALID;
-    if (h->dm.H > 0 || !md::attend_fits(h->dm)) return MD_E_UNSUPPORTED;
-    const OnDevice on(h->device);
-    if (!on.ok) return MD_E_HIP;
-    return md::launch_token(h->dm, h->v, h->sc, h->n_cu, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
-}
-
 md_status md_key_bounds(md_handle h, int32_t all_pages, int8_t* bounds, int8_t* bound_exp) {
     if (h == nullptr || (all_pages & ~1) != 0 || bounds == nullptr || bound_exp == nullptr || !aligned(bounds, 16))
         return MD_E_INVALID;
@@ -1072,6 +1049,125 @@ md_status md_decode_workspace(md_handle h, uint64_t* attend_bytes, uint64_t* sel
     if (h == nullptr || attend_bytes == nullptr || select_bytes == nullptr) return MD_E_INVALID;
     *attend_bytes = md::attend_workspace(h->dm, h->n_cu);
     *select_bytes = md::select_workspace(h->dm);
+    return MD_OK;
+}
+
+namespace {
+
+// ---- rows of the cache, and values in either form
+bool rows_ok(const md_row_list& r) {
+    return r.row_start != nullptr && aligned(r.row_start, 4) && aligned(r.row_slot, 4) && r.n_rows >= 0 && r.reserved == 0;
+}
+
+// written: the call writes them, which takes the open blocks of 8-bit ones
+bool values_ok(const md_values& v, bool written) {
+    if (!aligned(v.v_pool, 16) || !aligned(v.v_codes, 16) || !aligned(v.v_scale, 16) || !aligned(v.v_open, 16)) return false;
+    if (v.v_pool != nullptr) return v.v_codes == nullptr && v.v_scale == nullptr && v.v_open == nullptr;
+    return v.v_codes != nullptr && v.v_scale != nullptr && (!written || v.v_open != nullptr);
+}
+
+bool pitch_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0; }
+
+md_status attend_args_ok(md_handle h, int32_t layer, const md_attend_args* a) {
+    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L) return MD_E_INVALID;
+    const int64_t hq = (int64_t)h->dm.Hq * md::kHeadDim, hkv = (int64_t)h->dm.Hkv * md::kHeadDim;
+    if (a->q == nullptr || !aligned(a->q, 16) || a->q_stride < hq || a->q_stride % 4 != 0) return MD_E_INVALID;
+    if ((a->new_k == nullptr) != (a->new_v == nullptr)) return MD_E_INVALID;
+    if (a->new_k != nullptr && (!aligned(a->new_k, 16) || !aligned(a->new_v, 16) || a->kv_stride < hkv ||
+                                a->kv_stride % 8 != 0))
+        return MD_E_INVALID;
+    if ((a->blocks == nullptr) != (a->block_count == nullptr)) return MD_E_INVALID;
+    if (a->blocks != nullptr && (!aligned(a->blocks, 4) || !aligned(a->block_count, 4) || a->max_blocks < 1 ||
+                                 a->max_blocks > md::kMaxPages))
+        return MD_E_INVALID;
+    if (a->out == nullptr || !aligned(a->out, 16) || a->out_stride < hq || a->out_stride % 8 != 0 ||
+        (a->out_type != MD_F32 && a->out_type != MD_BF16) || !aligned(a->lse, 4))
+        return MD_E_INVALID;
+    if (a->workspace == nullptr || !aligned(a->workspace, 16)) return MD_E_INVALID;
+    return MD_OK;
+}
+
+}  // namespace
+
+md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a) {
+    const md_status st = attend_args_ok(h, layer, a);
+    if (st != MD_OK) return st;
+    if (a->v_pool == nullptr || !aligned(a->v_pool, 16)) return MD_E_INVALID;
+    if (h->dm.H > 0 || !md::attend_fits(h->dm)) return MD_E_UNSUPPORTED;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_token(h->dm, h->v, h->sc, h->n_cu, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v) {
+    if (h == nullptr || new_v == nullptr || v == nullptr || !aligned(new_v, 16) || v->v_pool != nullptr ||
+        !values_ok(*v, true))
+        return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    if (!h->fresh) return MD_E_STATE;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_append_codes(h->dm, h->v, new_v, *v, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_write_rows(md_handle h, int32_t layer, const md_write_args* a) {
+    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L || !rows_ok(a->rows)) return MD_E_INVALID;
+    if ((a->k == nullptr && a->v == nullptr) || !aligned(a->k, 16) || !aligned(a->v, 16) ||
+        !pitch_ok(a->stride, (int64_t)h->dm.Hkv * md::kHeadDim))
+        return MD_E_INVALID;
+    if (a->v != nullptr && !values_ok(a->values, true)) return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    if (a->rows.n_rows == 0) return MD_OK;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_write_rows(h->dm, h->v, h->sc, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_read_rows(md_handle h, int32_t layer, const md_read_args* a) {
+    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L || !rows_ok(a->rows)) return MD_E_INVALID;
+    if ((a->k == nullptr && a->v == nullptr) || !aligned(a->k, 16) || !aligned(a->v, 16) ||
+        !pitch_ok(a->stride, (int64_t)h->dm.Hkv * md::kHeadDim) || (a->type != MD_F32 && a->type != MD_BF16))
+        return MD_E_INVALID;
+    if (a->v != nullptr && !values_ok(a->values, false)) return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    if (a->rows.n_rows == 0) return MD_OK;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_read_rows(h->dm, h->v, h->sc, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_attend_values(md_handle h, int32_t layer, const md_attend_args* a, const md_values* v, int32_t window,
+                           int32_t sinks) {
+    const md_status st = attend_args_ok(h, layer, a);
+    if (st != MD_OK) return st;
+    if (v == nullptr || !values_ok(*v, false) || window < 0 || sinks < 0) return MD_E_INVALID;
+    if (h->dm.H > 0 || !md::attend_fits(h->dm) || (window > 0 && a->blocks != nullptr)) return MD_E_UNSUPPORTED;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_token_values(h->dm, h->v, h->sc, h->n_cu, layer, *a, *v, window, sinks, h->stream) == hipSuccess
+               ? MD_OK : MD_E_HIP;
+}
+
+md_status md_attend_rows(md_handle h, int32_t layer, const md_rows_args* a) {
+    if (h == nullptr || a == nullptr || layer < 0 || layer >= h->dm.L || !rows_ok(a->rows)) return MD_E_INVALID;
+    const int64_t hq = (int64_t)h->dm.Hq * md::kHeadDim;
+    if (a->q == nullptr || !aligned(a->q, 16) || !pitch_ok(a->q_stride, hq) || (a->q_type != MD_F32 && a->q_type != MD_BF16))
+        return MD_E_INVALID;
+    if (a->out == nullptr || !aligned(a->out, 16) || !pitch_ok(a->out_stride, hq) ||
+        (a->out_type != MD_F32 && a->out_type != MD_BF16) || !aligned(a->lse, 4))
+        return MD_E_INVALID;
+    if (a->window < 0 || a->sinks < 0 || !values_ok(a->values, false)) return MD_E_INVALID;
+    if (a->workspace == nullptr || !aligned(a->workspace, 16)) return MD_E_INVALID;
+    if (h->dm.H > 0 || (int64_t)a->rows.n_rows * h->dm.G + 256 * (int64_t)h->dm.S >= (int64_t)1 << 31) return MD_E_UNSUPPORTED;
+    if (a->rows.n_rows == 0) return MD_OK;
+    const OnDevice on(h->device);
+    if (!on.ok) return MD_E_HIP;
+    return md::launch_attend_rows(h->dm, h->v, h->sc, h->n_cu, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_rows_workspace(md_handle h, uint64_t* bytes) {
+    if (h == nullptr || bytes == nullptr) return MD_E_INVALID;
+    *bytes = md::rows_workspace(h->dm, h->n_cu);
     return MD_OK;
 }
 

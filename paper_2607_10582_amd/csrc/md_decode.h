@@ -35,6 +35,10 @@ struct TokenCall {
     void* out;
     int64_t out_stride;
     float* lse;
+    // values in 8 bits (v_pool NULL), and a window behind the first tokens
+    const uint8_t* v_codes;
+    const float* v_scale;
+    int L, window, sinks;
     int units;      // workgroups
     int32_t* count; // [3 units] arrivals (zero between launches)
     float* part;    // [units][2][G][kPartWords] partial results
@@ -50,6 +54,19 @@ uint64_t attend_workspace(const Dims& dm, int n_cu);
 bool attend_fits(const Dims& dm);
 hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
                         hipStream_t st);
+
+// The same over either form of the values, with a window (0: none).
+hipError_t launch_token_values(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
+                               const md_values& values, int window, int sinks, hipStream_t st);
+
+// Rows into and out of the pools (md_store.hip), attention of ragged rows (md_prompt.hip).
+hipError_t launch_append_codes(const Dims& dm, const View& v, const uint16_t* new_v, const md_values& values, hipStream_t st);
+hipError_t launch_write_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
+                             hipStream_t st);
+hipError_t launch_read_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_read_args& a, hipStream_t st);
+uint64_t rows_workspace(const Dims& dm, int n_cu);
+hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_rows_args& a,
+                              hipStream_t st);
 
 hipError_t launch_norm_rope(const Dims& dm, const View& v, const md_rope_args& a, int n_cu, hipStream_t st);
 hipError_t launch_append_values(const Dims& dm, const View& v, const uint16_t* new_v, uint16_t* v_pool,

@@ -45,17 +45,34 @@ __device__ __forceinline__ bool counts_ok(const TokenCall& c, int np, int nt) {
 // The kernel's LDS that grows with the sessions.
 constexpr size_t session_bytes(int S) { return (size_t)(2 * S + 1) * sizeof(int); }
 
+// Which of a session's tiles a call walks: all of them, those of listed pages,
+// or the first tokens' and a window's.
+enum Walk { kAll = 0, kListed = 1, kWindow = 2 };
+
 struct Desc {       // one 16-token tile, per lane
     int phys;       // page
-    int live;       // tokens of it that count, 0 .. 16; -1: the new token
+    int live;       // tokens of it that count, 0 .. 16 (kWindow: a bit for each); -1: the new token
     int quant;      // its keys are 8-bit codes
+    float scale;    // of its values' codes
 };
 
 struct Row {
     int s, kv, np, nt;   // session, KV head, pages and slots in use
     int tiles;           // 16-token tiles to walk
     bool ok;             // the session's counters are consistent
+    int low, head, skip; // kWindow: the window's first slot, tiles before it, and how many are left out behind those
 };
+
+// The tiles of a window: those of the first `sinks` tokens, then those from
+// the window's first slot on.
+__device__ __forceinline__ void window_of(const TokenCall& c, Row& r) {
+    const int own = r.nt - (c.new_k != nullptr ? 0 : 1);
+    const int all = (r.nt + 15) >> 4;
+    r.low = max(0, own - c.window + 1);   // (window >= 1, so that own + 1 cannot be passed)
+    r.head = min((min(c.sinks, r.nt) + 15) >> 4, r.low >> 4);
+    r.skip = min(r.low >> 4, all) - r.head;
+    r.tiles = all - r.skip;
+}
 
 // Leading tokens among 16 slots' region codes (holes follow a page's last token).
 __device__ __forceinline__ int tokens_before_holes(const uint8_t* region) {
@@ -73,19 +90,21 @@ __device__ __forceinline__ int tokens_before_holes(const uint8_t* region) {
 
 // Tile u of step t of a row: two tiles of its pages a step, then a step for
 // the new token.
-template <bool SPARSE, bool QT>
+template <int WALK, bool QT, bool V8>
 __device__ __forceinline__ Desc tile_desc(const TokenCall& c, const Row& r, int step, int u,
                                           int& status) {
-    Desc d{0, 0, 0};
-    const int t = 2 * step + u;
+    Desc d{0, 0, 0, 0.0f};
+    int t = 2 * step + u;
     if (t >= r.tiles) {
         if (r.ok && c.new_k != nullptr && u == 0 && step == (r.tiles + 1) >> 1) d.live = -1;
         return d;
     }
+    if constexpr (WALK == kWindow)
+        if (t >= r.head) t += r.skip;
     const int per = c.P >> 4;
     int page = t >> (c.Pshift - 4);
     const int sub = t & (per - 1);
-    if constexpr (SPARSE) {
+    if constexpr (WALK == kListed) {
         const int32_t* list = c.blocks + ((size_t)r.s * c.Hkv + r.kv) * c.max_blocks;
         const int o = page;
         page = list[o];
@@ -105,6 +124,15 @@ __device__ __forceinline__ Desc tile_desc(const TokenCall& c, const Row& r, int 
     d.live = min(16, max(0, r.nt - (page * c.P + 16 * sub)));
     if (c.aligned) d.live = min(d.live, tokens_before_holes(c.region + (size_t)p * c.P + 16 * sub));
     if constexpr (QT) d.quant = c.page_format[p];
+    if constexpr (WALK == kWindow) {   // slots below the sinks or from the window's first on
+        const int first = 16 * t;
+        const uint32_t sinks = (1u << min(16, max(0, c.sinks - first))) - 1u;
+        const uint32_t near = 0xFFFFu << min(16, max(0, r.low - first));
+        d.live = (int)(((1u << d.live) - 1u) & (sinks | near) & 0xFFFFu);
+    }
+    // (a tile without a token keeps the scale 0: its own may be anything)
+    if constexpr (V8)
+        if (d.live != 0) d.scale = c.v_scale[(((size_t)p * c.L + c.layer) * c.Hkv + r.kv) * (size_t)per + sub];
     return d;
 }
 
@@ -227,8 +255,10 @@ __device__ __forceinline__ void write_out(const TokenCall& c, const Row& r, int 
 // What bounds short lines is the chain: counters, scan, page table, keys and
 // values (3 - 6 us), results through LDS, and where a row is cut its parts
 // through memory (4 us).
-// SPARSE: pages from the call's lists; QT: pages may hold 8-bit codes.
-template <int W, bool SPARSE, bool QT>
+// QT: pages may hold 8-bit keys; V8: the values are 8-bit codes, which widen
+// to bf16 exactly and whose scale (one per tile) goes to the weights before
+// these are cut into their terms: half the bytes, the same products.
+template <int W, int WALK, bool QT, bool V8>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2)))
 k_token(TokenCall c) {
     constexpr int kThreads = 64 * W;
@@ -267,7 +297,14 @@ k_token(TokenCall c) {
             const bool ok = counts_ok(c, np, nt);
             if (!ok && blockIdx.x == 0) status = kDevCorrupt;
             held[s] = ok ? nt : -1;
-            const int tiles = !ok ? 0 : SPARSE ? min(c.max_blocks, np) * per : (nt + 15) >> 4;
+            int tiles = !ok ? 0 : WALK == kListed ? min(c.max_blocks, np) * per : (nt + 15) >> 4;
+            if constexpr (WALK == kWindow)
+                if (ok) {
+                    Row w{};
+                    w.nt = nt;
+                    window_of(c, w);
+                    tiles = w.tiles;
+                }
             n[k] = max(1, ((tiles + 1) >> 1) + (c.new_k != nullptr && ok ? 1 : 0));
         }
         int total;
@@ -321,17 +358,21 @@ k_token(TokenCall c) {
     auto run = [&](auto past) {
         Desc d;
         u32x4 kt[2][4], vt[2][4];
+        u32x4 vc[2][2];   // V8: a step's codes, widened into vt when their turn comes
         f32x4 qa[kQ][2];
+        auto counted = [](int live, int k) { return WALK == kWindow ? ((live >> k) & 1) != 0 : k < live; };
         auto steps_of = [&](const Stretch& t) { return max(0, (t.hi - t.lo - wv + W - 1) / W); };
         // descriptors of this wave's steps i .. i + 31 (lo + wv + 4 i ..): lane 2 k + u holds tile u of the k-th
         auto describe = [&](const Stretch& t, int i) {
             const int mine = t.lo + wv + (i + (lane >> 1)) * W;
-            d = Desc{0, 0, 0};
-            if (mine < t.hi) d = tile_desc<SPARSE, QT>(c, t.r, mine, lane & 1, status);
+            d = Desc{0, 0, 0, 0.0f};
+            if (mine < t.hi) d = tile_desc<WALK, QT, V8>(c, t.r, mine, lane & 1, status);
         };
         auto elem_at = [&](const Stretch& t, int i, int u) {
             const int phys = __builtin_amdgcn_readlane(d.phys, 2 * (i & 31) + u);
-            const int tile = 2 * (t.lo + wv + i * W) + u;
+            int tile = 2 * (t.lo + wv + i * W) + u;
+            if constexpr (WALK == kWindow)
+                if (tile >= t.r.head) tile += t.r.skip;
             return (size_t)phys * c.page_elems +
                    ((size_t)c.layer * c.Hkv + t.r.kv) * c.P * kHeadDim + (size_t)(tile & (per - 1)) * 16 * kHeadDim;
         };
@@ -350,11 +391,14 @@ k_token(TokenCall c) {
         auto load_v = [&](const Stretch& t, int i) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const gbytes vp = uni_ptr(c.v_pool + elem_at(t, i, u));
+                gbytes vp;
+                if constexpr (V8) vp = uni_ptr(c.v_codes + elem_at(t, i, u));
+                else vp = uni_ptr(c.v_pool + elem_at(t, i, u));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < (V8 ? 2 : 4); ++j) {
                     const gvec at = reinterpret_cast<gvec>(vp + (uint32_t)(1024 * j + 16 * lane));
-                    vt[u][j] = past.value ? __builtin_nontemporal_load(at) : *at;
+                    u32x4& to = V8 ? vc[u][j & 1] : vt[u][j];
+                    to = past.value ? __builtin_nontemporal_load(at) : *at;
                 }
             }
         };
@@ -389,7 +433,11 @@ k_token(TokenCall c) {
             r.nt = max(0, r.nt);
             r.np = (r.nt + c.P - 1) >> c.Pshift;   // (what counts_ok says of consistent ones)
             r.tiles = (r.nt + 15) >> 4;
-            if constexpr (SPARSE) {
+            if constexpr (WALK == kWindow) {
+                r.low = r.head = r.skip = 0;
+                if (r.ok) window_of(c, r);
+            }
+            if constexpr (WALK == kListed) {
                 const int most = min(c.max_blocks, r.np);
                 int n = c.block_count[(size_t)r.s * c.Hkv + r.kv];
                 if (n < 0 || n > most) {
@@ -447,6 +495,7 @@ k_token(TokenCall c) {
             for (int i = 0; i < nw; ++i) {
                 int live[2];
                 float qsc[2] = {1.0f, 1.0f};
+                u32x4 fv[4];   // V8: the new token's values
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     live[u] = __builtin_amdgcn_readlane(d.live, 2 * (i & 31) + u);
@@ -460,13 +509,15 @@ k_token(TokenCall c) {
                         }
                     }
                 }
-                if (live[0] < 0) {   // the new token: every lane reads its dims, the other tokens count nothing
+                const bool fresh = live[0] < 0;
+                if (fresh) {   // the new token: every lane reads its dims, the other tokens count nothing
                     const uint16_t* nk = c.new_k + (int64_t)t.r.s * c.kv_stride + t.r.kv * kHeadDim;
                     const uint16_t* nv = c.new_v + (int64_t)t.r.s * c.kv_stride + t.r.kv * kHeadDim;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         kt[0][j] = *reinterpret_cast<const u32x4*>(nk + 32 * j + 8 * g);
-                        vt[0][j] = u32x4{nv[32 * j + h], 0u, nv[32 * j + 16 + h], 0u};
+                        const u32x4 own{nv[32 * j + h], 0u, nv[32 * j + 16 + h], 0u};
+                        (V8 ? fv[j] : vt[0][j]) = own;
                     }
                     live[0] = 1;
                 }
@@ -493,6 +544,7 @@ k_token(TokenCall c) {
                 // (unconditional: loads behind a branch would make the wait for the
                 // values one for these keys too; behind the last step it reads
                 // that step's tiles again, out of the cache)
+                const float d_scale = d.scale;   // (of this step: describe may replace d)
                 const int nx = min(i + 1, nw - 1);
                 if ((nx & 31) == 0 && nx > i) describe(t, nx);
                 load_k(t, nx);
@@ -501,7 +553,7 @@ k_token(TokenCall c) {
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        x[u][k] = 4 * g + k < live[u] ? x[u][k] * (QT ? kLogitScale * qsc[u] : kLogitScale) : -INFINITY;
+                        x[u][k] = counted(live[u], 4 * g + k) ? x[u][k] * (QT ? kLogitScale * qsc[u] : kLogitScale) : -INFINITY;
                         mx = fmaxf(mx, x[u][k]);
                     }
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -524,6 +576,19 @@ k_token(TokenCall c) {
                         p[k] = hw_exp2(x[u][k] - ms);
                         l += p[k];
                     }
+                    if constexpr (V8) {
+                        const float vs = fresh && u == 0 ? 1.0f
+                            : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d_scale), 2 * (i & 31) + u));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) p[k] *= vs;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {   // dims 32 j + m and 32 j + 16 + m: words 2 (j & 1) .. of codes j / 2
+                            const uint32_t a = vc[u][j >> 1][2 * (j & 1)], b = vc[u][j >> 1][2 * (j & 1) + 1];
+                            vt[u][j] = u32x4{codes_pair_to_bf16<false>(a), codes_pair_to_bf16<true>(a),
+                                             codes_pair_to_bf16<false>(b), codes_pair_to_bf16<true>(b)};
+                            if (u == 0 && fresh) vt[0][j] = fv[j];
+                        }
+                    }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         float a = p[2 * k], b = p[2 * k + 1];
@@ -535,10 +600,17 @@ k_token(TokenCall c) {
                     }
                     // a slot that does not count may hold anything, and 0 times
                     // an infinity or NaN is NaN: its values become 0
-                    if (live[u] < 16) {
-                        const int k4 = live[u] - 4 * g;   // tokens of this lane's four that count
-                        const uint32_t m0 = k4 >= 2 ? 0xFFFFFFFFu : k4 == 1 ? 0x0000FFFFu : 0u;
-                        const uint32_t m1 = k4 >= 4 ? 0xFFFFFFFFu : k4 == 3 ? 0x0000FFFFu : 0u;
+                    if (WALK == kWindow ? live[u] != 0xFFFF : live[u] < 16) {
+                        uint32_t m0, m1;
+                        if constexpr (WALK == kWindow) {
+                            const uint32_t b = (uint32_t)live[u] >> (4 * g);
+                            m0 = (b & 1u) * 0x0000FFFFu | ((b >> 1) & 1u) * 0xFFFF0000u;
+                            m1 = ((b >> 2) & 1u) * 0x0000FFFFu | ((b >> 3) & 1u) * 0xFFFF0000u;
+                        } else {
+                            const int k4 = live[u] - 4 * g;   // tokens of this lane's four that count
+                            m0 = k4 >= 2 ? 0xFFFFFFFFu : k4 == 1 ? 0x0000FFFFu : 0u;
+                            m1 = k4 >= 4 ? 0xFFFFFFFFu : k4 == 3 ? 0x0000FFFFu : 0u;
+                        }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) vt[u][j] = vt[u][j] & u32x4{m0, m1, m0, m1};
                     }
@@ -657,12 +729,19 @@ k_token(TokenCall c) {
     if (status != 0) atomicOr(c.status, status);
 }
 
+template <int W, int WALK>
+const void* token_kernel(bool keys8, bool values8) {
+    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_token<W, WALK, true, true>)
+                            : reinterpret_cast<const void*>(&k_token<W, WALK, true, false>))
+                 : (values8 ? reinterpret_cast<const void*>(&k_token<W, WALK, false, true>)
+                            : reinterpret_cast<const void*>(&k_token<W, WALK, false, false>));
+}
+
 template <int W>
-const void* token_kernel(bool sparse, bool codes) {
-    return sparse ? (codes ? reinterpret_cast<const void*>(&k_token<W, true, true>)
-                           : reinterpret_cast<const void*>(&k_token<W, true, false>))
-                  : (codes ? reinterpret_cast<const void*>(&k_token<W, false, true>)
-                           : reinterpret_cast<const void*>(&k_token<W, false, false>));
+const void* token_kernel(int walk, bool keys8, bool values8) {
+    return walk == kListed   ? token_kernel<W, kListed>(keys8, values8)
+           : walk == kWindow ? token_kernel<W, kWindow>(keys8, values8)
+                             : token_kernel<W, kAll>(keys8, values8);
 }
 
 }  // namespace
@@ -707,6 +786,12 @@ bool attend_fits(const Dims& dm) {
 
 hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
                         hipStream_t st) {
+    return launch_token_values(dm, v, sc, n_cu, layer, a, md_values{const_cast<uint16_t*>(a.v_pool), nullptr, nullptr, nullptr},
+                               0, 0, st);
+}
+
+hipError_t launch_token_values(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
+                               const md_values& values, int window, int sinks, hipStream_t st) {
     TokenCall c{};
     c.S = dm.S;
     c.Hq = dm.Hq;
@@ -731,7 +816,12 @@ hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_
     c.new_k = a.new_k;
     c.new_v = a.new_v;
     c.kv_stride = a.kv_stride;
-    c.v_pool = a.v_pool;
+    c.v_pool = values.v_pool;
+    c.v_codes = values.v_codes;
+    c.v_scale = values.v_scale;
+    c.L = dm.L;
+    c.window = window;
+    c.sinks = sinks;
     c.blocks = a.blocks;
     c.block_count = a.block_count;
     c.max_blocks = a.max_blocks;
@@ -744,9 +834,10 @@ hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_
     c.part = static_cast<float*>(a.workspace) + count_words(c.units);
     void* args[] = {&c};
     const int W = attend_waves(dm, n_cu);
-    const bool sparse = a.blocks != nullptr, codes = dm.quant != 0;
-    const void* fn = W == 8 ? token_kernel<8>(sparse, codes) : W == 4 ? token_kernel<4>(sparse, codes)
-                                                             : token_kernel<2>(sparse, codes);
+    const int walk = a.blocks != nullptr ? kListed : window > 0 ? kWindow : kAll;
+    const bool keys8 = dm.quant != 0, values8 = values.v_pool == nullptr;
+    const void* fn = W == 8 ? token_kernel<8>(walk, keys8, values8) : W == 4 ? token_kernel<4>(walk, keys8, values8)
+                                                                 : token_kernel<2>(walk, keys8, values8);
     return hipLaunchKernel(fn, dim3((unsigned)c.units), dim3(64 * W), args, session_bytes(dm.S), st);
 }
 

@@ -1,0 +1,532 @@
+// gfx950 kernels that move rows between a caller's arrays and the pools: keys
+// and values of ragged rows in and out, and a step's values in 8 bits.
+//
+//   scale = max |v| / 448 over a block of 16 tokens and KV head,  code = e4m3(v / scale)
+//
+// Each moves a value once and turns it by a few operations, so long calls are
+// bound by HBM, and a decode step's by the launch and its chain of loads.
+
+#include "md_decode.h"
+#include "md_device.h"
+
+namespace md {
+
+namespace {
+
+constexpr int kWaves = 4;          // waves per workgroup
+constexpr float kTopCode = 448.0f; // the largest E4M3 value
+constexpr int kPitch = kHeadDim + 8;   // elements between the tokens of a block in LDS
+
+struct RowCall {
+    int S, L, Hkv, P, Pshift, MP, NP, layer, quant;
+    size_t page_elems;
+    uint16_t* k_pool;
+    const int32_t* page_table;
+    const int32_t* n_pages;
+    const int32_t* n_tokens;
+    const uint8_t* page_format;
+    int32_t* status;
+    const int32_t* row_start;
+    const int32_t* row_slot;
+    int n_rows;
+    md_values values;
+    void* k;   // the caller's rows
+    void* v;
+    int64_t stride;
+};
+
+// Eight E4M3 codes of 8 floats (already divided by their scale).
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// v / scale, 0 where the scale is 0 or not a number.
+__device__ __forceinline__ float in_scale(float v, float scale) { return scale > 0.0f ? v / scale : 0.0f; }
+
+// The scale of a block whose largest magnitude has these bf16 bits (NaN for
+// a value that is not finite: those have the largest bits).
+__device__ __forceinline__ float scale_of(uint32_t top_bits) {
+    return top_bits >= 0x7F80u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top_bits << 16) / kTopCode;
+}
+
+__device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) { return ~wave_min_u32(~v); }
+
+// Largest magnitude bits among the two bf16 values of a word.
+__device__ __forceinline__ uint32_t top_of(uint32_t w) { return max(w & 0x7FFFu, (w >> 16) & 0x7FFFu); }
+
+// A block's codes out of LDS ([16 tokens][kPitch] bf16), lane (m, g): tokens
+// 4g .. 4g+3 of dims 64 a + 16 i + m, in the pool's order.
+__device__ __forceinline__ u32x4 block_codes(const uint16_t* x, int a, float scale) {
+    const int m = lane_id() & 15, g = lane_id() >> 4;
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float q[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) q[t] = in_scale(bf16_value(x[(4 * g + t) * kPitch + 64 * a + 16 * i + m]), scale);
+        w[i] = four_codes(q[0], q[1], q[2], q[3]);
+    }
+    return w;
+}
+
+// Orders a wave's LDS accesses before and behind it (the hardware takes them
+// in order; this keeps the compiler from moving them).
+__device__ __forceinline__ void wave_lds() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// What the wave's row `lane & 31` of rows r0 .. r0 + 31 is.
+struct Span {
+    int s, lo, hi, nt; // its session, that session's rows and slots in use
+    int slot, prev;    // its slot, and that of the session's row before it
+    int phys, sub, t;  // page, block of it and token of the block
+    bool mine;         // it is some session's row
+    bool in;           // and its slot holds a token's place
+};
+
+__device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
+    const int lane = lane_id(), r = r0 + (lane & 31);
+    Span x{};
+    // the sessions that end at or before a row, for 32 rows at once
+    int s = 0;
+    for (int base = 0; base < c.S; base += 64) {
+        const int end = base + lane < c.S ? c.row_start[base + lane + 1] : 0x7FFFFFFF;
+#pragma unroll 8
+        for (int i = 0; i < 32; ++i) {
+            const int n = __popcll(__ballot(end <= r0 + i));
+            if (i == (lane & 31)) s += n;
+        }
+    }
+    x.s = min(s, c.S - 1);
+    x.lo = c.row_start[x.s];
+    x.hi = c.row_start[x.s + 1];
+    x.mine = s < c.S && x.lo >= 0 && x.lo <= r && r < x.hi && x.hi <= c.n_rows;
+    x.prev = -1;
+    if (!x.mine) return x;
+    const int np = c.n_pages[x.s], nt = c.n_tokens[x.s];
+    const bool ok = np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
+    if (!ok) {
+        status |= kDevCorrupt;
+        return x;
+    }
+    x.nt = nt;
+    x.slot = c.row_slot != nullptr ? c.row_slot[r] : nt - (x.hi - r);
+    if (r > x.lo) x.prev = c.row_slot != nullptr ? c.row_slot[r - 1] : x.slot - 1;
+    x.in = x.slot >= 0 && x.slot < nt;
+    if (!x.in) {
+        status |= MD_DEV_BAD_ROW;
+        return x;
+    }
+    x.phys = c.page_table[(size_t)x.s * c.MP + (x.slot >> c.Pshift)];
+    if ((unsigned)x.phys >= (unsigned)c.NP) {
+        status |= kDevCorrupt;
+        x.in = false;
+        x.phys = 0;
+    }
+    x.sub = (x.slot & (c.P - 1)) >> 4;
+    x.t = x.slot & 15;
+    return x;
+}
+
+__device__ __forceinline__ size_t tile_of(const RowCall& c, int phys, int sub, int kv) {
+    return (size_t)phys * c.page_elems + ((size_t)c.layer * c.Hkv + kv) * c.P * kHeadDim + (size_t)sub * 16 * kHeadDim;
+}
+__device__ __forceinline__ size_t scale_at(const RowCall& c, int phys, int sub, int kv) {
+    return (((size_t)phys * c.L + c.layer) * c.Hkv + kv) * (size_t)(c.P >> 4) + sub;
+}
+
+// A wave takes 16 rows and one KV head: the groups of rows that begin among
+// them, each the rows of one block (up to 15 of them behind the 16).  A block
+// has one group, the one that a search of the session's rows for the block's
+// first slot finds, so that no two waves write a block even where the slots do
+// not ascend.  Keys go as they come, 1 KiB of a block at a time; values turn in
+// LDS, from rows of dims to dims of four tokens.
+template <bool CODES>
+__global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
+    __shared__ __align__(16) uint16_t turn[kWaves][16 * kPitch];
+    const int lane = lane_id(), wv = threadIdx.x >> 6;
+    const int64_t task = (int64_t)blockIdx.x * kWaves + wv;
+    const int r0 = (int)(task / c.Hkv) * 16, kv = (int)(task % c.Hkv);
+    if (r0 >= c.n_rows) return;
+    int status = 0;
+    const Span x = span_of(c, r0, status);
+    const int r = r0 + (lane & 31);
+    bool counts = x.in;
+    if (counts && r > x.lo && x.slot <= x.prev) {
+        status |= MD_DEV_BAD_ROW;
+        counts = false;
+    }
+    const bool goes_on = counts && r > x.lo && (x.prev >> 4) == (x.slot >> 4);
+    bool leads = counts && !goes_on && (lane & 31) < 16 && lane < 32;
+    if (leads && c.row_slot != nullptr) {   // the first row that is not below the block
+        int lo = x.lo, hi = x.hi;
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            if (c.row_slot[mid] < (x.slot & ~15)) lo = mid + 1; else hi = mid;
+        }
+        leads = lo == r;
+    }
+    const bool coded = c.quant && counts && c.page_format[x.phys] != 0;
+    if (coded && c.k != nullptr) status |= MD_DEV_BAD_ROW;
+    const uint32_t more = (uint32_t)__ballot(goes_on);
+    uint64_t todo = __ballot(leads);
+    uint16_t* const buf = turn[wv];
+    const int m = lane & 15, g = lane >> 4;
+    while (todo != 0) {
+        const int i = __ffsll((unsigned long long)todo) - 1;
+        todo &= todo - 1;
+        const uint32_t rest = i < 31 ? more >> (i + 1) : 0u;
+        const int len = 1 + (rest == 0xFFFFFFFFu ? 32 : __ffs(~rest) - 1);
+        const int o = __builtin_amdgcn_readlane(x.t, i), phys = __builtin_amdgcn_readlane(x.phys, i);
+        const int sub = __builtin_amdgcn_readlane(x.sub, i), s = __builtin_amdgcn_readlane(x.s, i);
+        const int row = r0 + i;
+        const int lo = __builtin_amdgcn_readlane(x.lo, i), hi = __builtin_amdgcn_readlane(x.hi, i);
+        const bool first = row == lo, last = row + len == hi;
+        const bool skip_k = c.quant && __builtin_amdgcn_readlane(coded ? 1 : 0, i);
+        const int n_slots = __builtin_amdgcn_readlane(x.nt, i);
+        auto slot_at = [&](int q) { return c.row_slot != nullptr ? c.row_slot[q] : n_slots - (hi - q); };
+        // whether the session's rows start with a block (or with nothing that counts)
+        bool starts_block = true;
+        if (CODES && last && !first) {
+            const int begin = slot_at(lo);
+            starts_block = begin < 0 || begin >= n_slots || (begin & 15) == 0;
+        }
+        // which tokens of the block the group holds (in order; gaps only from lists)
+        uint32_t have = 0;
+        if (__builtin_amdgcn_readlane(x.t, i + len - 1) - o == len - 1) {
+            have = ((1u << len) - 1u) << o;
+        } else {
+            for (int k = 0; k < len; ++k) have |= 1u << __builtin_amdgcn_readlane(x.t, i + k);
+        }
+        // lane (m, g): dims 8g .. of token m
+        const bool has = (have >> m) & 1u;
+        const int64_t at = (int64_t)(row + __popc(have & ((1u << m) - 1u))) * c.stride + kv * kHeadDim + 8 * g;
+        const size_t tile = tile_of(c, phys, sub, kv);
+        if (c.k != nullptr && !skip_k && has) {
+            const uint16_t* from = static_cast<const uint16_t*>(c.k) + at;
+            uint16_t* to = c.k_pool + tile + 8 * lane;
+            u32x4 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4*>(from + 32 * j);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(to + 512 * j) = w[j];
+        }
+        if (c.v == nullptr) continue;
+        u32x4 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = u32x4{0u, 0u, 0u, 0u};
+        uint16_t* const open = CODES ? c.values.v_open + ((((size_t)s * c.L + c.layer) * c.Hkv + kv) * 16 + m) * kHeadDim + 8 * g : nullptr;
+        if (has || (CODES && first && m < o)) {
+            const uint16_t* from = has ? static_cast<const uint16_t*>(c.v) + at : open;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4*>(from + 32 * j);
+        }
+        wave_lds();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(buf + m * kPitch + 32 * j + 8 * g) = w[j];
+        wave_lds();
+        if constexpr (CODES) {
+            // The open block becomes the session's last one.  Where the rows go
+            // on inside a block, this wave alone has read it, and writes it too:
+            // from the rows, for a block that is another wave's.
+            if (last && (first || starts_block)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(open + 32 * j) = w[j];
+            } else if (first && o > 0) {
+                const int q = hi - 1 - m;   // the last rows, backwards
+                const int behind = slot_at(hi - 1), mine = q >= row ? slot_at(q) : -1;
+                const bool same = mine >= 0 && (mine >> 4) == (behind >> 4);
+                int from = -1;               // the row of token m
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const int tk = __builtin_amdgcn_readlane(same ? mine & 15 : -1, k);
+                    if (tk == m) from = hi - 1 - k;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    u32x4 y{0u, 0u, 0u, 0u};
+                    if (from >= 0)
+                        y = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(c.v) + (int64_t)from * c.stride +
+                                                            kv * kHeadDim + 8 * g + 32 * j);
+                    *reinterpret_cast<u32x4*>(open + 32 * j) = y;
+                }
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top = max(top, top_of(w[j][k]));
+            const float scale = scale_of(wave_max_u32(top));
+            uint8_t* to = c.values.v_codes + tile + 16 * lane;
+#pragma unroll
+            for (int a = 0; a < 2; ++a) *reinterpret_cast<u32x4*>(to + 1024 * a) = block_codes(buf, a, scale);
+            if (lane == 0) c.values.v_scale[scale_at(c, phys, sub, kv)] = scale;
+        } else {
+            uint16_t* to = c.values.v_pool + tile + 8 * lane;
+            const uint32_t quad = (have >> (4 * g)) & 15u;   // which of this lane's four tokens come
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint16_t y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = buf[(4 * g + (e & 3)) * kPitch + 32 * j + 16 * (e >> 2) + m];
+                if (quad == 15u) {
+                    *reinterpret_cast<u32x4*>(to + 512 * j) = u32x4{y[0] | (uint32_t)y[1] << 16, y[2] | (uint32_t)y[3] << 16,
+                                                                    y[4] | (uint32_t)y[5] << 16, y[6] | (uint32_t)y[7] << 16};
+                } else if (quad != 0u) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((quad >> (e & 3)) & 1u) to[512 * j + e] = y[e];
+                }
+            }
+        }
+    }
+    if (status != 0) atomicOr(c.status, status);
+}
+
+template <bool F32>
+__device__ __forceinline__ void put8(void* p, int64_t at, const float (&x)[8]) {
+    if constexpr (F32) {
+        f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p) + at);
+        o[0] = f32x4{x[0], x[1], x[2], x[3]};
+        o[1] = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+        typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
+        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + at) = w;
+    }
+}
+
+// Eight bf16 values (words) times a scale; the scale 1 changes nothing.
+__device__ __forceinline__ void widen8(const u32x4& w, float scale, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16) * scale;
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) * scale;
+    }
+}
+
+// A wave takes 16 rows and one KV head.  Lane (m, g) fetches row m's key, 16
+// bytes at a time (consecutive rows of a block make 1 KiB); the values' blocks
+// come whole and turn in LDS, one for each run of rows of the same block.
+template <bool CODES, bool F32>
+__global__ void __launch_bounds__(64 * kWaves) k_read_rows(RowCall c) {
+    __shared__ __align__(16) uint16_t turn[kWaves][16 * kPitch];
+    const int lane = lane_id(), wv = threadIdx.x >> 6;
+    const int64_t task = (int64_t)blockIdx.x * kWaves + wv;
+    const int r0 = (int)(task / c.Hkv) * 16, kv = (int)(task % c.Hkv);
+    if (r0 >= c.n_rows) return;
+    int status = 0;
+    Span x = span_of(c, r0, status);
+    const int m = lane & 15, g = lane >> 4;
+    // lane (m, g) works on row m
+    const int phys = __shfl(x.phys, m), sub = __shfl(x.sub, m), t = __shfl(x.t, m);
+    const bool mine = __shfl(x.mine ? 1 : 0, m) != 0, in = __shfl(x.in ? 1 : 0, m) != 0;
+    const int64_t at = (int64_t)(r0 + m) * c.stride + kv * kHeadDim + 8 * g;
+    if (c.k != nullptr && mine) {
+        const uint16_t* tile = c.k_pool + tile_of(c, phys, sub, kv);
+        u32x4 w[4];
+        float scale = 1.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = u32x4{0u, 0u, 0u, 0u};
+        if (in && c.quant && c.page_format[phys] != 0) {
+            const uint8_t* b = reinterpret_cast<const uint8_t*>(tile);
+            scale = *reinterpret_cast<const float*>(b + 2048);
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const u32x4 k = *reinterpret_cast<const u32x4*>(b + 1024 * a + 16 * (t + 16 * g));
+                w[2 * a] = codes_to_bf16<0>(k);
+                w[2 * a + 1] = codes_to_bf16<1>(k);
+            }
+        } else if (in) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4*>(tile + 512 * j + 8 * (16 * g + t));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float y[8];
+            widen8(w[j], scale, y);
+            put8<F32>(c.k, at + 32 * j, y);
+        }
+    }
+    if (c.v != nullptr) {
+        uint16_t* const buf = turn[wv];
+        uint32_t left = (uint32_t)__ballot(in) & 0xFFFFu;
+        if (mine && !in) {
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) put8<F32>(c.v, at + 32 * j, none);
+        }
+        while (left != 0) {
+            const int i = __ffs(left) - 1;
+            const int p = __builtin_amdgcn_readlane(phys, i), b = __builtin_amdgcn_readlane(sub, i);
+            const bool here = in && phys == p && sub == b;
+            left &= ~(uint32_t)__ballot(here);
+            const size_t tile = tile_of(c, p, b, kv);
+            float scale = 1.0f;
+            wave_lds();
+            if constexpr (CODES) {
+                scale = c.values.v_scale[scale_at(c, p, b, kv)];
+                u32x4 w[2];
+#pragma unroll
+                for (int a = 0; a < 2; ++a) w[a] = *reinterpret_cast<const u32x4*>(c.values.v_codes + tile + 1024 * a + 16 * lane);
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // word e: tokens 4g .. of dim 64 a + 16 e + m
+                        const uint32_t lo = codes_pair_to_bf16<false>(w[a][e]), hi = codes_pair_to_bf16<true>(w[a][e]);
+                        uint16_t* to = buf + 4 * g * kPitch + 64 * a + 16 * e + m;
+                        to[0] = (uint16_t)lo;
+                        to[kPitch] = (uint16_t)(lo >> 16);
+                        to[2 * kPitch] = (uint16_t)hi;
+                        to[3 * kPitch] = (uint16_t)(hi >> 16);
+                    }
+            } else {
+                u32x4 w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4*>(c.values.v_pool + tile + 512 * j + 8 * lane);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // words 0, 1: tokens 4g .. of dim 32 j + m; 2, 3: of 32 j + 16 + m
+                        uint16_t* to = buf + (4 * g + 2 * (e & 1)) * kPitch + 32 * j + 16 * (e >> 1) + m;
+                        to[0] = (uint16_t)w[j][e];
+                        to[kPitch] = (uint16_t)(w[j][e] >> 16);
+                    }
+            }
+            wave_lds();
+            if (here) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float y[8];
+                    widen8(*reinterpret_cast<const u32x4*>(buf + t * kPitch + 32 * j + 8 * g), scale, y);
+                    put8<F32>(c.v, at + 32 * j, y);
+                }
+            }
+        }
+    }
+    if (status != 0) atomicOr(c.status, status);
+}
+
+// One wave per (session, layer, KV head), two dims a lane.  The scale can
+// only grow within a block, and max and division keep their order under
+// rounding: scale = max(scale before, |v|'s own), so a token that does not
+// raise it costs its own 128 codes.  One that does has the block's codes
+// written anew, from the open block's values.
+__global__ void __launch_bounds__(64 * kWaves) k_append_codes(Dims dm, View v, const uint16_t* __restrict__ new_v,
+                                                              md_values values) {
+    __shared__ __align__(16) uint16_t turn[kWaves][16 * kPitch];
+    const int lane = lane_id(), wv = threadIdx.x >> 6, s = blockIdx.y;
+    const int row = blockIdx.x * kWaves + wv;   // (layer, KV head)
+    if (row >= dm.LHkv) return;
+    const uint32_t mine = reinterpret_cast<const uint32_t*>(new_v)[((size_t)s * dm.LHkv + row) * (kHeadDim / 2) + lane];
+    const int np = v.n_pages[s], nt = v.n_tokens[s];
+    if (!counters_ok(np, nt, dm) || np == 0) return;
+    const int p = v.page_table[(size_t)s * dm.MP + np - 1];
+    if ((unsigned)p >= (unsigned)dm.NP) return;
+    const int slot = nt - 1 - (np - 1) * dm.P, o = slot & 15;
+    if (v.t_ins[(size_t)p * dm.P + slot] != v.clock[s]) return;
+    const size_t tile = ((size_t)p * dm.LHkv + row) * dm.P * kHeadDim + (size_t)(slot & ~15) * kHeadDim;
+    float* const scale_p = values.v_scale + ((size_t)p * dm.LHkv + row) * (dm.P >> 4) + (slot >> 4);
+    uint32_t* const open = reinterpret_cast<uint32_t*>(values.v_open) + ((size_t)s * dm.LHkv + row) * 16 * (kHeadDim / 2) + lane;
+    const float before = o > 0 ? *scale_p : 0.0f;
+    const uint32_t own_top = wave_max_u32(top_of(mine));
+    const float own_scale = scale_of(own_top);
+    open[o * (kHeadDim / 2)] = mine;
+    uint8_t* const codes = values.v_codes + tile;
+    if (o > 0 && (own_scale <= before || before != before)) {
+        const int e = 2 * lane;   // dims e and e + 1: neighbours m, m + 1 of the same 16
+        const uint32_t w = four_codes(in_scale(bf16_value((uint16_t)mine), before), in_scale(bf16_value((uint16_t)(mine >> 16)), before),
+                                      0.0f, 0.0f);
+        uint8_t* to = codes + (e / 64) * 1024 + (o / 4) * 256 + (e % 16) * 16 + ((e / 16) % 4) * 4 + o % 4;
+        to[0] = (uint8_t)w;
+        to[16] = (uint8_t)(w >> 8);
+        return;
+    }
+    uint16_t* const buf = turn[wv];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        uint32_t w = 0u;
+        if (t < o) w = open[t * (kHeadDim / 2)];
+        if (t == o) w = mine;
+        if (o == 0 && t > 0) open[t * (kHeadDim / 2)] = 0u;
+        *reinterpret_cast<uint32_t*>(buf + t * kPitch + 2 * lane) = w;
+    }
+    wave_lds();
+#pragma unroll
+    for (int a = 0; a < 2; ++a) *reinterpret_cast<u32x4*>(codes + 1024 * a + 16 * lane) = block_codes(buf, a, own_scale);
+    if (lane == 0) *scale_p = own_scale;
+}
+
+RowCall row_call(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_row_list& rows) {
+    RowCall c{};
+    c.S = dm.S;
+    c.L = dm.L;
+    c.Hkv = dm.Hkv;
+    c.P = dm.P;
+    c.Pshift = dm.Pshift;
+    c.MP = dm.MP;
+    c.NP = dm.NP;
+    c.layer = layer;
+    c.quant = dm.quant;
+    c.page_elems = (size_t)dm.LHkv * dm.P * kHeadDim;
+    c.k_pool = v.k_pool;
+    c.page_table = v.page_table;
+    c.n_pages = v.n_pages;
+    c.n_tokens = v.n_tokens;
+    c.page_format = v.page_format;
+    c.status = sc.status;
+    c.row_start = rows.row_start;
+    c.row_slot = rows.row_slot;
+    c.n_rows = rows.n_rows;
+    return c;
+}
+
+hipError_t launch(const void* fn, RowCall& c, hipStream_t st) {
+    const int64_t waves = ((int64_t)c.n_rows + 15) / 16 * c.Hkv;
+    void* args[] = {&c};
+    return hipLaunchKernel(fn, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(64 * kWaves), args, 0, st);
+}
+
+}  // namespace
+
+hipError_t launch_append_codes(const Dims& dm, const View& v, const uint16_t* new_v, const md_values& values, hipStream_t st) {
+    Dims d = dm;
+    View vv = v;
+    md_values w = values;
+    void* args[] = {&d, &vv, &new_v, &w};
+    const dim3 grid((unsigned)((dm.LHkv + kWaves - 1) / kWaves), (unsigned)dm.S);
+    return hipLaunchKernel(reinterpret_cast<const void*>(&k_append_codes), grid, dim3(64 * kWaves), args, 0, st);
+}
+
+hipError_t launch_write_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
+                             hipStream_t st) {
+    RowCall c = row_call(dm, v, sc, layer, a.rows);
+    c.values = a.values;
+    c.k = const_cast<uint16_t*>(a.k);
+    c.v = const_cast<uint16_t*>(a.v);
+    c.stride = a.stride;
+    return launch(a.v != nullptr && a.values.v_pool == nullptr ? reinterpret_cast<const void*>(&k_write_rows<true>)
+                                                               : reinterpret_cast<const void*>(&k_write_rows<false>), c, st);
+}
+
+hipError_t launch_read_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_read_args& a, hipStream_t st) {
+    RowCall c = row_call(dm, v, sc, layer, a.rows);
+    c.values = a.values;
+    c.k = a.k;
+    c.v = a.v;
+    c.stride = a.stride;
+    const bool codes = a.v != nullptr && a.values.v_pool == nullptr, wide = a.type == MD_F32;
+    const void* fn = codes ? (wide ? reinterpret_cast<const void*>(&k_read_rows<true, true>)
+                                   : reinterpret_cast<const void*>(&k_read_rows<true, false>))
+                           : (wide ? reinterpret_cast<const void*>(&k_read_rows<false, true>)
+                                   : reinterpret_cast<const void*>(&k_read_rows<false, false>));
+    return launch(fn, c, st);
+}
+
+}  // namespace md
