@@ -113,9 +113,10 @@ enum {
                                 /* which need not count itself (of 5 3 4 5: 5,  */
                                 /* 4 and 5 again; of 0 2^30 1: 0)               */
 #define MD_DEV_BAD_ROW    0x40  /* md_write_rows, md_read_rows or md_attend_rows */
-                                /* got a row whose slot its session does not    */
-                                /* hold, or (md_write_rows) that is not above   */
-                                /* the row before it or sits in a page of codes */
+                                /* got a row_start that does not ascend, a row  */
+                                /* whose slot its session does not hold, or     */
+                                /* (md_write_rows) that is not above the row    */
+                                /* before it or sits in a page of 8-bit keys    */
 #define MD_DEV_TIMEOUT    0x10  /* a bounded wait between the workgroups of the */
                                 /* fused observation kernel ran out; the step's */
                                 /* attention mass is not valid (the session     */
@@ -691,8 +692,9 @@ md_status md_decode_workspace(md_handle h, uint64_t* attend_bytes, uint64_t* sel
  *     md_norm_rope -> md_write_rows -> md_attend_rows        (per layer)
  *
  * md_row_list says which: rows row_start[s] .. row_start[s + 1] - 1 of a call's
- * arrays are session s's (row_start ascends from 0; rows behind row_start[S]
- * belong to nobody and are left as they were), and row_slot tells each row's
+ * arrays are session s's (row_start ascends within 0 .. n_rows, or no row counts;
+ * rows before row_start[0] and behind row_start[S] belong to nobody and are
+ * left as they were), and row_slot tells each row's
  * slot among the session's (page * P + offset, pages in logical order; NULL:
  * the session's last ones, in order).  The page tables, counts and region
  * codes of these slots are there before the call: the caller has placed the

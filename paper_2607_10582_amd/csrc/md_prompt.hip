@@ -20,6 +20,7 @@
 // token), HBM for a few rows over a long cache.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "md_arrive.h"
 #include "md_decode.h"
@@ -32,8 +33,6 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
 constexpr int kStep = 64;                  // tokens of a step: four blocks
 constexpr int kStepBytes = kStep * kHeadDim * 2;
 // A column's maximum is only followed when it has grown by more than this
@@ -75,7 +74,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// The other half-wave's value (lane ^ 32).
+// acc plus both bf16 values of a word.
+__device__ __forceinline__ float add_pair(uint32_t w, float acc) {
+    typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), acc, false);
+}
+
+// The larger, or the sum, of both half-waves' values.
 __device__ __forceinline__ float max_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -121,23 +126,27 @@ __device__ __forceinline__ float log_sum(float m, float l) { return (m + log2f(l
 
 // What a lane knows of block `base + lane` of the list that a tile walks.
 struct Block {
-    int phys, at;      // page; slot of the block's first token
+    int64_t tile;      // elements before its tile in the pools of keys and values
+    int at;            // slot of its first token
     int live;          // its tokens, 0 .. 16
     int coded;         // 8-bit keys
-    float ks, vs;      // scales of keys and values
+    int ks, vs;        // scales of keys and values (float bits)
 };
 
-// A workgroup takes the tile's columns 4 waves x 32 CT, whose waves share each
-// step of 64 tokens through LDS; the next step's loads are under way while this
-// one is worked on.  TERMS: bf16 terms of queries and weights (1: bf16 in and
-// out; 3: exact).
-template <int TERMS, int CT, bool QT, bool V8>
-__global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
-    constexpr int kCols = kWaves * 32 * CT;
+// A workgroup takes a tile of 32 columns for each of its W waves, which share
+// the steps of 64 tokens through LDS: keys of two steps, values of three.
+// TERMS: bf16 terms of queries and weights (1: bf16 in and out; 3: exact);
+// QT: pages may hold 8-bit keys; V8: the values are 8-bit codes, which widen to
+// bf16 on their way into LDS, their scales going to the weights.
+template <int W, int TERMS, bool QT, bool V8>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W / 4))) k_rows_attend(PromptCall c) {
+    constexpr int kThreads = 64 * W;
+    constexpr int kCols = W * 32;
+    constexpr int kPer = kStepBytes / (16 * kThreads);   // 16-byte loads of a thread for a step's keys
     __shared__ __align__(16) uint8_t kl[2][kStepBytes];
-    __shared__ __align__(16) uint8_t vl[2][kStepBytes];
+    __shared__ __align__(16) uint8_t vl[3][kStepBytes];
     __shared__ int scan_lds[17];
-    __shared__ int range_lds[2][kWaves];
+    __shared__ int range_lds[2][W];
     __shared__ int sh_last;
     extern __shared__ int pref[];   // [S + 1] tiles of the sessions before
     const int tid = threadIdx.x, lane = lane_id(), wv = uni(tid >> 6);
@@ -146,12 +155,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
     int status = 0;
     // ---- this workgroup's tile
     int before = 0;
+    bool broken = false;   // (rows of several sessions, or more than there are, would make more tiles than the grid has)
     for (int k = 0; k < c.S; k += kThreads) {
         const int s = k + tid;
         int tiles = 0;
         if (s < c.S) {
             const int lo = c.row_start[s], hi = c.row_start[s + 1];
-            if (lo >= 0 && lo <= hi && hi <= c.n_rows) tiles = ((hi - lo) * c.G + kCols - 1) / kCols;
+            broken |= lo < 0 || lo > hi || hi > c.n_rows;
+            tiles = broken ? 0 : ((hi - lo) * c.G + kCols - 1) / kCols;
         }
         int total;
         const int ex = block_exclusive_scan(tiles, scan_lds, &total);
@@ -159,7 +170,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
         before += total;
     }
     if (tid == 0) pref[c.S] = before;
-    __syncthreads();
+    if (__syncthreads_or(broken ? 1 : 0)) {
+        if (tid == 0) atomicOr(c.status, MD_DEV_BAD_ROW);
+        return;
+    }
     const int kv = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv;
     const int split = rest % c.splits;
     const int tile = uni(before) - 1 - rest / c.splits;   // the longest of a session first
@@ -174,53 +188,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
         nt = 0;
     }
     // ---- the wave's columns and their queries
-    const int col0 = (tile - uni(pref[s])) * kCols + wv * 32 * CT;
-    int own[CT];          // slot of the column's row (-1: it sees nothing)
-    int64_t row_of[CT];   // -1: not a column
-    int head_of[CT];
-    u32x4 qf[TERMS][CT][8];
-    int smin = 0x7FFFFFFF, smax = -1;
+    const int col0 = (tile - uni(pref[s])) * kCols + wv * 32, col = col0 + n;
+    const bool mine = col < rows * c.G;
+    int64_t row = row_lo + (mine ? col / c.G : 0);
+    int head = kv * c.G + (mine ? col % c.G : 0);
+    int own = -1;   // slot of the column's row (-1: it sees nothing)
+    if (mine) {
+        const int slot = c.row_slot != nullptr ? c.row_slot[row] : nt - (rows - (int)(row - row_lo));
+        if (slot >= 0 && slot < nt) own = slot; else status |= MD_DEV_BAD_ROW;
+    }
+    int smin = own >= 0 ? own : 0x7FFFFFFF, smax = own;
+    u32x4 qf[TERMS][8];
+    const int64_t q_at = row * c.q_stride + head * kHeadDim + 8 * h;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        const int col = col0 + 32 * ct + n;
-        const bool mine = col < rows * c.G;
-        const int r = mine ? col / c.G : 0;
-        head_of[ct] = kv * c.G + (mine ? col % c.G : 0);
-        row_of[ct] = mine ? row_lo + r : -1;
-        own[ct] = -1;
-        if (mine) {
-            const int slot = c.row_slot != nullptr ? c.row_slot[row_lo + r] : nt - (rows - r);
-            if (slot >= 0 && slot < nt) own[ct] = slot; else status |= MD_DEV_BAD_ROW;
-        }
-        if (own[ct] >= 0) {
-            smin = min(smin, own[ct]);
-            smax = max(smax, own[ct]);
-        }
-        const int64_t at = (mine ? row_of[ct] : (int64_t)row_lo) * c.q_stride + head_of[ct] * kHeadDim + 8 * h;
+    for (int kk = 0; kk < 8; ++kk) {
+        if (TERMS == 1 || !c.q_f32) {
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-            if constexpr (TERMS == 1) {
-                qf[0][ct][kk] = mine ? *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(c.q) + at + 16 * kk)
-                                     : u32x4{0u, 0u, 0u, 0u};
-            } else if (!c.q_f32) {
-                qf[0][ct][kk] = mine ? *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(c.q) + at + 16 * kk)
-                                     : u32x4{0u, 0u, 0u, 0u};
-                qf[1][ct][kk] = qf[2][ct][kk] = u32x4{0u, 0u, 0u, 0u};
-            } else {
-                f32x4 x[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-                if (mine) {
-                    const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(c.q) + at + 16 * kk);
-                    x[0] = p[0];
-                    x[1] = p[1];
-                }
+            for (int t = 0; t < TERMS; ++t) qf[t][kk] = u32x4{0u, 0u, 0u, 0u};
+            if (mine) qf[0][kk] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(c.q) + q_at + 16 * kk);
+        } else {
+            f32x4 y[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+            if (mine) {
+                const f32x4* from = reinterpret_cast<const f32x4*>(static_cast<const float*>(c.q) + q_at + 16 * kk);
+                y[0] = from[0];
+                y[1] = from[1];
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t a[3], b[3];
-                    split3(x[i >> 1][2 * (i & 1)], a[0], a[1], a[2]);
-                    split3(x[i >> 1][2 * (i & 1) + 1], b[0], b[1], b[2]);
+            for (int i = 0; i < 4; ++i) {
+                uint32_t a[3], b[3];
+                split3(y[i >> 1][2 * (i & 1)], a[0], a[1], a[2]);
+                split3(y[i >> 1][2 * (i & 1) + 1], b[0], b[1], b[2]);
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) qf[k % TERMS][ct][kk][i] = a[k] | (b[k] << 16);
-                }
+                for (int t = 0; t < TERMS; ++t) qf[t][kk][i] = a[t] | (b[t] << 16);
             }
         }
     }
@@ -233,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
     __syncthreads();
     int gmin = range_lds[0][0], gmax = range_lds[1][0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
+    for (int w = 1; w < W; ++w) {
         gmin = min(gmin, range_lds[0][w]);
         gmax = max(gmax, range_lds[1][w]);
     }
@@ -255,265 +254,456 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
     const int begin = split * share, end = min(steps, begin + share);
 
     const size_t row_elems = ((size_t)c.layer * c.Hkv + kv) * c.P * kHeadDim;
-    auto describe = [&](int base) {
-        Block b{0, 0, 0, 0, 1.0f, 0.0f};
+    auto page_of = [&](int base) __attribute__((always_inline)) {   // of block base + lane
+        const int i = min(base + lane, n_blocks - 1);
+        return c.page_table[(size_t)s * c.MP + ((16 * (i < first ? i : i + low - first)) >> c.Pshift)];
+    };
+    auto describe = [&](int base, int p) __attribute__((always_inline)) {
+        Block b{(int64_t)row_elems, 0, 0, 0, 0x3F800000, 0};   // (page 0: there is one)
         const int i = base + lane;
         if (i >= n_blocks) return b;
         const int blk = i < first ? i : i + low - first;
         b.at = 16 * blk;
-        const int p = c.page_table[(size_t)s * c.MP + (b.at >> c.Pshift)];
         if ((unsigned)p >= (unsigned)c.NP) {
             status |= kDevCorrupt;
             return b;
         }
         const int sub = blk & (per - 1);
-        b.phys = p;
+        b.tile = (int64_t)((size_t)p * c.page_elems + row_elems + (size_t)sub * 16 * kHeadDim);
         b.live = min(16, nt - b.at);
         if (c.aligned) b.live = min(b.live, tokens_before_holes(c.region + (size_t)p * c.P + 16 * sub));
         if constexpr (QT) {
             b.coded = c.page_format[p] != 0;
             if (b.coded)
-                b.ks = *reinterpret_cast<const float*>(c.k_pool + (size_t)p * c.page_elems + row_elems + (size_t)sub * 16 * kHeadDim + 1024);
+                b.ks = *reinterpret_cast<const int*>(c.k_pool + b.tile + 1024);
         }
         if constexpr (V8)
-            if (b.live > 0) b.vs = c.v_scale[(((size_t)p * c.L + c.layer) * c.Hkv + kv) * (size_t)per + sub];
+            if (b.live > 0) b.vs = reinterpret_cast<const int*>(c.v_scale)[(((size_t)p * c.L + c.layer) * c.Hkv + kv) * (size_t)per + sub];
         return b;
     };
-    Block mine = describe(4 * begin), ahead = describe(4 * begin + 64);
-    auto of = [&](int x, int i) { return __builtin_amdgcn_readlane(x, i); };
-    auto off = [&](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    auto of = [](int x, int i) { return __builtin_amdgcn_readlane(x, i); };
+    auto off = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    // Lanes know of 16 steps: kLot of them to work on, and the three behind
+    // these that are on their way into LDS.  A bit for each block that every
+    // column of the wave sees in full, that lacks tokens, that holds 8-bit keys;
+    // four of them are step i's.
+    constexpr int kLot = 13;
+    Block cur = begin < end ? describe(4 * begin, page_of(4 * begin)) : Block{}, next = cur;
+    int next_page = 0;
+    uint64_t full, part, coded;
+    auto look = [&]() __attribute__((always_inline)) {
+        const int at = cur.at;
+        full = __ballot((cur.live == 16) & (at + 15 <= smin) & ((at > smax - win) | (at + 15 < c.sinks)));
+        part = __ballot(cur.live < 16);
+        coded = QT ? __ballot(cur.coded != 0) : 0;
+    };
+    look();
+    auto bits = [](uint64_t of_blocks, int i) { return (uint32_t)(of_blocks >> (4 * i)) & 15u; };
 
     // ---- a step's loads, and their way into LDS
-    u32x4 rk[4], rv[4];
-    auto load = [&](int j, const Block& d) {
-        const int i0 = (4 * (j - begin)) & 63;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const size_t at = (size_t)of(d.phys, i0 + b) * c.page_elems + row_elems +
-                              (size_t)((of(d.at, i0 + b) >> 4) & (per - 1)) * 16 * kHeadDim;
-            const uint8_t* kp = reinterpret_cast<const uint8_t*>(c.k_pool + at);
-            const bool coded = QT && of(d.coded, i0 + b) != 0;
-            rk[b] = *reinterpret_cast<const u32x4*>(kp + 16 * (coded ? tid & 127 : tid));
-            const uint8_t* vp = V8 ? c.v_codes + at : reinterpret_cast<const uint8_t*>(c.v_pool + at);
-            rv[b] = *reinterpret_cast<const u32x4*>(vp + 16 * (V8 ? tid & 127 : tid));
+    // thread tid takes 16 bytes of block 4 x / kPer ..: a block is 256 such pieces, of codes 128
+    u32x4 rk[kPer], rv[V8 ? (kPer + 1) / 2 : kPer];
+    constexpr int kVals = V8 ? (kPer + 1) / 2 : kPer;
+    // Where the thread's pieces go, once for all steps (kept as they are: taken
+    // apart into what does not change they would cost the loop its registers).
+    // Keys in LDS: [half][8 dims pairs][32 tokens] 16 bytes; values: [block][d / 32]
+    // [tokens 4h .. and 8+4h ..][32 dims] 16 bytes.
+    constexpr int kApart = W / 4;   // blocks between a thread's pieces
+    const int c16 = tid & 255, c8 = tid & 127;
+    uint32_t from = 16 * c16, from8 = 16 * c8;
+    uint32_t key_at = 512 * (c16 >> 4) + 16 * (c16 & 15) + 256 * (tid >> 8);
+    uint32_t key8_at = 4096 * (c16 >> 6) + 512 * ((c16 >> 4) & 3) + 16 * (c16 & 15) + 256 * (tid >> 8);
+    uint32_t value_at = 512 * ((tid >> 4) & 1) + 16 * (tid & 15) + 8 * ((tid >> 5) & 1) +
+                        (V8 ? 2048 * (c8 >> 6) + 4096 * (tid >> 7) : 1024 * (c16 >> 6) + 4096 * (tid >> 8));
+    asm volatile("" : "+v"(from), "+v"(from8), "+v"(key_at), "+v"(key8_at), "+v"(value_at));
+    // Requests piece x of the lot's step i.
+    auto tile_ptr = [&](const void* pool, int i, int b, int shift) __attribute__((always_inline)) {
+        const uint64_t t = (uint64_t)(uint32_t)of((int)(uint32_t)cur.tile, 4 * i + b) |
+                           ((uint64_t)(uint32_t)of((int)(cur.tile >> 32), 4 * i + b) << 32);
+        return (gbytes)(reinterpret_cast<uint64_t>(pool) + (t << shift));
+    };
+    auto load_key = [&](int i, int x) __attribute__((always_inline)) {
+        const int b = (x * W + wv) >> 2;   // (uniform)
+        const bool codes = QT && ((bits(coded, i) >> b) & 1) != 0;
+        rk[x] = *reinterpret_cast<gvec>(tile_ptr(c.k_pool, i, b, 1) + (codes ? from8 : from));
+    };
+    auto load_value = [&](int i, int x) __attribute__((always_inline)) {
+        if constexpr (V8) rv[x] = *reinterpret_cast<gvec>(tile_ptr(c.v_codes, i, (x * W + wv) >> 1, 0) + from8);
+        else rv[x] = *reinterpret_cast<gvec>(tile_ptr(c.v_pool, i, (x * W + wv) >> 2, 1) + from);
+    };
+    auto store_key = [&](int i, int x, uint8_t* kbuf) __attribute__((always_inline)) {
+        const int b = (x * W + wv) >> 2;
+        // (block kApart x + tid / 256)
+        uint8_t* to = kbuf + (kApart == 2 ? 8192 * x : 8192 * (x >> 1) + 256 * (x & 1));
+        if (QT && ((bits(coded, i) >> b) & 1) != 0) {
+            // codes (a, g, t): dims 64 a + 8 g .. and 64 a + 32 + 8 g .. of token t
+            if (c16 < 128) {
+                *reinterpret_cast<u32x4*>(to + key8_at) = codes_to_bf16<0>(rk[x]);
+                *reinterpret_cast<u32x4*>(to + key8_at + 2048) = codes_to_bf16<1>(rk[x]);
+            }
+        } else {
+            *reinterpret_cast<u32x4*>(to + key_at) = rk[x];
         }
     };
-    auto store = [&](int j, const Block& d, int buf) {
-        const int i0 = (4 * (j - begin)) & 63;
+    // (four tokens 4g .. of dims m and 16 + m, g = (tid / 16) % 4, m = tid % 16)
+    auto put_values = [&](uint8_t* to, u32x2 a, u32x2 b) __attribute__((always_inline)) {
+        *reinterpret_cast<u32x2*>(to) = a;
+        *reinterpret_cast<u32x2*>(to + 256) = b;
+    };
+    auto store_value = [&](int i, int x, uint8_t* vbuf) __attribute__((always_inline)) {
+        const int b = (x * W + wv) >> (V8 ? 1 : 2);
+        // a slot without a token may hold anything, and 0 times an infinity
+        // or NaN is NaN: its values become 0
+        uint32_t m0 = 0xFFFFFFFFu, m1 = 0xFFFFFFFFu;
+        if (__builtin_expect((bits(part, i) >> b) & 1, 0)) {
+            const int k4 = of(cur.live, 4 * i + b) - 4 * ((tid >> 4) & 3);
+            m0 = k4 >= 2 ? 0xFFFFFFFFu : k4 == 1 ? 0x0000FFFFu : 0u;
+            m1 = k4 >= 4 ? 0xFFFFFFFFu : k4 == 3 ? 0x0000FFFFu : 0u;
+        }
+        uint8_t* to = vbuf + value_at + (V8 ? 4096 * (W / 2) : 4096 * kApart) * x;
+        if constexpr (V8) {   // codes (a, g, m): words of dims 64 a + 16 i + m
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            uint8_t* kb = kl[buf] + 4096 * b;
-            uint8_t* vb = vl[buf] + 4096 * b;
-            if (QT && of(d.coded, i0 + b) != 0) {
-                // codes (a, g, t): dims 64 a + 8 g .. and 64 a + 32 + 8 g .. of token t
-                if (tid < 128) {
-                    uint8_t* to = kb + 2048 * (tid >> 6) + 16 * (tid & 63);
-                    *reinterpret_cast<u32x4*>(to) = codes_to_bf16<0>(rk[b]);
-                    *reinterpret_cast<u32x4*>(to + 1024) = codes_to_bf16<1>(rk[b]);
-                }
-            } else {
-                *reinterpret_cast<u32x4*>(kb + 16 * tid) = rk[b];
+            for (int y = 0; y < 2; ++y) {
+                const uint32_t u = rv[x][2 * y], v = rv[x][2 * y + 1];
+                put_values(to + 1024 * y, u32x2{codes_pair_to_bf16<false>(u) & m0, codes_pair_to_bf16<true>(u) & m1},
+                           u32x2{codes_pair_to_bf16<false>(v) & m0, codes_pair_to_bf16<true>(v) & m1});
             }
-            // a slot without a token may hold anything, and 0 times an infinity
-            // or NaN is NaN: its values become 0
-            const int live = of(d.live, i0 + b);
-            const int k4 = live - 4 * ((tid >> 4) & 3);
-            const uint32_t m0 = k4 >= 2 ? 0xFFFFFFFFu : k4 == 1 ? 0x0000FFFFu : 0u;
-            const uint32_t m1 = k4 >= 4 ? 0xFFFFFFFFu : k4 == 3 ? 0x0000FFFFu : 0u;
-            if constexpr (V8) {
-                if (tid < 128) {   // codes (a, g, m): words of dims 64 a + 16 i + m
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t x = rv[b][2 * i], y = rv[b][2 * i + 1];
-                        *reinterpret_cast<u32x4*>(vb + 2048 * (tid >> 6) + 1024 * i + 16 * (tid & 63)) =
-                            u32x4{codes_pair_to_bf16<false>(x) & m0, codes_pair_to_bf16<true>(x) & m1,
-                                  codes_pair_to_bf16<false>(y) & m0, codes_pair_to_bf16<true>(y) & m1};
-                    }
-                }
-            } else {
-                *reinterpret_cast<u32x4*>(vb + 16 * tid) = rv[b] & u32x4{m0, m1, m0, m1};
-            }
+        } else {
+            put_values(to, u32x2{rv[x][0] & m0, rv[x][1] & m1}, u32x2{rv[x][2] & m0, rv[x][3] & m1});
         }
     };
 
     // (the sums that lse tells of, and those of the weights as the products get
     // them, by which a result is divided: rounding a weight then moves it between
     // values, and does not scale the result)
-    float m[CT], l[CT], lw[CT];
-    f32x16 o[CT][4];
+    float m = -INFINITY, l = 0.0f, lw = 0.0f;
+    f32x16 o[4];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        m[ct] = -INFINITY;
-        l[ct] = lw[ct] = 0.0f;
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    // ---- A step is two halves of 32 tokens.  While a half's logits become
+    // weights, the matrix cores work on its neighbours: the sums of the half
+    // before and the logits of the half behind, product by product between the
+    // weights' instructions.  (A wave alone issues one of those in 7 cycles, not
+    // 4; with the products of one wave beside the weights of the other, section
+    // by section, a prompt of 16,384 rows took 1.13 ms; in this order FIG_MIX.)
+    f32x16 x[2];
+    uint32_t pw[TERMS][2][8];   // weights, two to a word: 4 b .. are those of the half's block b
+    // Sixteen operands from LDS and their products, kAhead reads under way: left
+    // to itself the compiler has each product wait for its own.
+    auto stream = [&](auto count, auto&& read, auto&& product, auto&& beside) {
+        constexpr int N = decltype(count)::value, kAhead = 4;
+        u32x4 a[kAhead];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[ct][d][i] = 0.0f;
-    }
+        for (int i = 0; i < kAhead; ++i) a[i] = read(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            product(i, __builtin_bit_cast(bf16x8, a[i % kAhead]));
+            if (i + kAhead < N) a[i % kAhead] = read(i + kAhead);
+            beside(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    using std::integral_constant;
+    const uint8_t* const k_lane = kl[0] + 16 * lane;
+    const uint8_t* const v_lane = vl[0] + 16 * lane;
+    auto key_part = [&](int u, uint32_t buf, int kk) { return *reinterpret_cast<const u32x4*>(k_lane + buf + 8192 * u + 1024 * kk); };
+    auto value_part = [&](int u, uint32_t buf, int i) { return *reinterpret_cast<const u32x4*>(v_lane + buf + 8192 * u + 1024 * i); };
+    auto logit = [&](int u, int kk, bf16x8 a) {
+        const f32x16 none = {};
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+            x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[t][kk]), kk == 0 && t == 0 ? none : x[u], 0, 0, 0);
+    };
+    auto sum = [&](int u, int i, bf16x8 a) {   // block i / 4, dims 32 (i % 4) ..
+        const int b = i >> 2, d = i & 3;
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                a, __builtin_bit_cast(bf16x8, u32x4{pw[t][u][4 * b], pw[t][u][4 * b + 1], pw[t][u][4 * b + 2], pw[t][u][4 * b + 3]}),
+                o[d], 0, 0, 0);
+    };
+    auto nothing = [](int) {};
+    // 8-bit keys and values: the keys' scale goes to the logits, the values' to
+    // the weights (through the exponent where those are rounded to bf16 anyway)
+    // and out of their sums again.
+    float sc[2], vs[2], rs[2], lg[2], shift[2];
+    bool lost[2] = {false, false};   // values that are not numbers
+    float mx;
+    // A half's scales, what its columns see of it and their maxima: whether one
+    // has grown enough to be followed.  i: the step's place in the lot.
+    auto peak = [&](int u, int i) __attribute__((always_inline)) {
+        const int i0 = 4 * i + 2 * u;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            sc[b] = kLogitScale;
+            if constexpr (QT) {
+                const float ks = __uint_as_float(of(cur.ks, i0 + b));
+                if (__builtin_expect(ks > 0.0f && ks < INFINITY, 1)) {
+                    sc[b] *= ks;
+                } else {   // (no factor for the -infinity of a token that is not seen)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[u][8 * b + k] *= ks;
+                }
+            }
+            if constexpr (V8) {
+                vs[b] = __uint_as_float(of(cur.vs, i0 + b));
+                lost[b] = !(vs[b] < INFINITY);
+                if (vs[b] == 0.0f || (TERMS == 1 && lost[b])) vs[b] = 1.0f;   // (0: all its values are)
+                rs[b] = __builtin_amdgcn_rcpf(vs[b]);
+                lg[b] = log2f(vs[b]);
+            }
+        }
+        if (__builtin_expect(((full >> i0) & 3) != 3, 0)) {
+            int h4 = 4 * h, own_here = own;
+            asm volatile("" : "+v"(h4), "+v"(own_here));   // (or the loop would carry 16 registers of what follows)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int at = of(cur.at, i0 + b), live = of(cur.live, i0 + b);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int t = 8 * (k >> 2) + h4 + (k & 3);
+                    const bool sees = (t < live) & (at + t <= own_here) & ((at + t > own_here - win) | (at + t < c.sinks));
+                    x[u][8 * b + k] = sees ? x[u][8 * b + k] : -INFINITY;
+                }
+            }
+        }
+        float mb[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float y = fmaxf(fmaxf(x[u][8 * b], x[u][8 * b + 1]), x[u][8 * b + 2]);
+            const float z = fmaxf(fmaxf(x[u][8 * b + 3], x[u][8 * b + 4]), x[u][8 * b + 5]);
+            mb[b] = fmaxf(fmaxf(y, z), fmaxf(x[u][8 * b + 6], x[u][8 * b + 7]));
+        }
+        mx = max_halves(QT ? fmaxf(mb[0] * sc[0], mb[1] * sc[1]) : fmaxf(mb[0], mb[1]) * kLogitScale);
+        return __any(mx > m + kSlack || (m == -INFINITY && mx > -INFINITY)) != 0;
+    };
+    // Follows the maxima, in whole steps: what was weighed before (the sums, and
+    // the half before this one's weights, whose sums come later) moves by a
+    // power of two, without a rounding.
+    auto follow = [&](int last) __attribute__((always_inline)) {
+        const float mn = fmaxf(m, ceilf(mx));
+        const float f = mn == -INFINITY ? 1.0f : ldexpf(1.0f, (int)fmaxf(m - mn, -300.0f));
+        l *= f;
+        lw *= f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[d] *= f;
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) pw[t][last][k] = pack_bf16(bf16_lo(pw[t][last][k]) * f, bf16_hi(pw[t][last][k]) * f);
+        m = mn;
+    };
+    // The half's weights, pair by pair: begun, and a pair later finished.
+    float p, q, all_sum, w_sum;
+    auto finish = [&](int u, int k) __attribute__((always_inline)) {
+        const int b = k >> 2;
+        if ((k & 3) == 0) all_sum = w_sum = 0.0f;
+        all_sum += p + q;
+        if constexpr (TERMS != 1 && V8) {
+            p *= vs[b];
+            q *= vs[b];
+        }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            uint32_t w = pack_bf16(p, q);
+            asm volatile("" : "+v"(w));
+            pw[t][u][k] = w;
+            if constexpr (TERMS == 1) {
+                w_sum = add_pair(w, w_sum);
+            } else {
+                p -= bf16_lo(w);
+                q -= bf16_hi(w);
+            }
+        }
+        if ((k & 3) != 3) return;
+        if constexpr (TERMS == 1 && V8) {
+            l = fmaf(all_sum, rs[b], l);
+            lw = fmaf(w_sum, rs[b], lw);
+            if (lost[b] && all_sum > 0.0f) lw = __uint_as_float(0x7FC00000u);   // (settled at the end)
+        } else {
+            l += all_sum;
+            lw += w_sum;
+        }
+    };
+    auto pair = [&](int u, int k) __attribute__((always_inline)) {
+        const int b = k >> 2;
+        float y = hw_exp2(fmaf(x[u][2 * k], sc[b], shift[b])), z = hw_exp2(fmaf(x[u][2 * k + 1], sc[b], shift[b]));
+        asm volatile("" : "+v"(y), "+v"(z));   // (here, between these products, not where they are used)
+        if (k > 0) finish(u, k - 1);
+        p = y;
+        q = z;
+    };
+    constexpr int kPeak = 3;   // the product beside which a half's maxima are looked at
+    // One half: its weights, beside the logits of the half behind it and the sums
+    // of the one before it, both the other half of a step in LDS.  A half that no
+    // column sees gets weights of 0 (two ways through here would keep the sums
+    // in two places).
+    auto half = [&](auto which, int i, uint32_t k_buf, uint32_t v_buf, auto&& beside) __attribute__((always_inline)) {
+        constexpr int u = decltype(which)::value;
+        // The sums come first: they need nothing of this half, whose logits are
+        // the products just begun.  Its maxima are looked at beside them (moving
+        // sums and weights by the same power of two is right between any two of
+        // them), its eight pairs of weights spread over what is left.
+        stream(integral_constant<int, 16>{},
+               [&](int j) { return j < 8 ? value_part(1 - u, v_buf, j) : key_part(1 - u, k_buf, j - 8); },
+               [&](int j, bf16x8 a) {
+                   if (j < 8) sum(1 - u, j, a); else logit(1 - u, j - 8, a);
+               },
+               [&](int j) {
+                   if (j == kPeak) {
+                       if (__builtin_expect(peak(u, i), 0)) follow(1 - u);
+                       const float ms = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                       for (int b = 0; b < 2; ++b) shift[b] = TERMS == 1 && V8 ? lg[b] - ms : -ms;
+                   }
+                   constexpr int kLeft = 15 - kPeak;   // slots behind it
+#pragma unroll
+                   for (int k = 0; k < 8; ++k)
+                       if (j == kPeak + 1 + k * kLeft / 8) pair(u, k);
+                   if (!(j & 1)) beside(j >> 1);
+               });
+        finish(u, 7);
+    };
     if (begin < end) {
-        load(begin, mine);
-        store(begin, mine, 0);
+        const int count = end - begin;
+        auto load_keys = [&](int i) {
+#pragma unroll
+            for (int x = 0; x < kPer; ++x) load_key(i, x);
+        };
+        auto load_values = [&](int i) {
+#pragma unroll
+            for (int x = 0; x < kVals; ++x) load_value(i, x);
+        };
+        auto store_keys = [&](int i, uint32_t buf) {
+#pragma unroll
+            for (int x = 0; x < kPer; ++x) store_key(i, x, kl[0] + buf);
+        };
+        auto store_values = [&](int i, uint32_t buf) {
+#pragma unroll
+            for (int x = 0; x < kVals; ++x) store_value(i, x, vl[0] + buf);
+        };
+        // (behind the last step: page 0, which nobody looks at)
+        load_keys(0);
+        load_values(0);
+        store_keys(0, 0);
+        store_values(0, 0);
+        load_keys(1);
+        load_values(1);
+        store_keys(1, kStepBytes);
+        load_keys(2);
         lds_sync();
-    }
-    for (int j = begin; j < end; ++j) {
-        const int buf = (j - begin) & 1, i0 = (4 * (j - begin)) & 63;
-        const Block now = mine;
-        if (i0 == 60) {   // the next step's blocks are the next lot's
-            mine = ahead;
-            ahead = describe(4 * (j + 1) + 64);
-        }
-        const bool more = j + 1 < end;
-        if (more) load(j + 1, mine);
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            const int b0 = i0 + 2 * sub;
-            int at[2], live[2];
-            bool any = false, all = true;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                at[b] = of(now.at, b0 + b);
-                live[b] = of(now.live, b0 + b);
-                any |= live[b] > 0 && at[b] <= smax && (at[b] + 15 > smin - win || at[b] < c.sinks);
-                all &= live[b] == 16 && at[b] + 15 <= smin && (at[b] > smax - win || at[b] + 15 < c.sinks);
+        // the step's keys; the values of the step before (weights of 0 at first, of
+        // anything that was written), its own, and where the next one's go
+        uint32_t k_now = 0, v_last = 0, v_now = 0, v_new = kStepBytes;
+        auto turn = [&](int at, int& i) __attribute__((always_inline)) {
+            if (__builtin_expect(i == kLot / 2 - 3, 0)) next_page = page_of(4 * (begin + at - i + kLot));   // in good time
+            if (__builtin_expect(i == kLot / 2, 0)) next = describe(4 * (begin + at - i + kLot), next_page);
+            if (__builtin_expect(i == kLot - 1, 0)) {
+                cur = next;
+                look();
+                i = -1;
             }
-            if (!any) continue;   // (no column of the wave sees any of it)
-            f32x16 x[CT];
+            k_now = kStepBytes - k_now;
+            v_last = v_now;
+            v_now = v_new;
+            v_new = v_new == 2 * kStepBytes ? 0 : v_new + kStepBytes;
+        };
+        if (smax >= 0) {
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
+            for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[ct][i] = 0.0f;
-            const uint8_t* kb = kl[buf] + 8192 * sub + 4096 * (n >> 4) + 16 * (n & 15) + 256 * h;
+                for (int k = 0; k < 8; ++k) pw[t][1][k] = 0u;
+            stream(integral_constant<int, 8>{}, [&](int j) { return key_part(0, 0, j); }, [&](int j, bf16x8 a) { logit(0, j, a); },
+                   nothing);
+            // A piece of the caches' bytes goes to LDS and the same one of the step
+            // behind is requested a whole step before it goes: keys beside one half,
+            // values beside the other (all beside one: FIG_SPREAD).
+            auto pieces = [](int k, int n, auto&& put, auto&& get) {
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kb + 512 * kk));
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t)
-                        x[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[t][ct][kk]), x[ct], 0, 0, 0);
+                for (int x = 0; x < n; ++x) {
+                    if (k == (4 / n) * x) put(x);
+                    if (k == 4 + (4 / n) * x) get(x);
+                }
+            };
+            // Of a SIMD's two waves the older one goes first wherever both could,
+            // and would wait for the other at every step's end: each gets one half
+            // of the step to go first in (1.084 ms for 16,384 rows, 1.108 without).
+            const bool younger = wv >= W / 2;
+            auto go_first = [&](bool mine_now) __attribute__((always_inline)) {
+                if (mine_now) __builtin_amdgcn_s_setprio(1); else __builtin_amdgcn_s_setprio(0);
+            };
+            for (int at = 0, i = 0; at < count; ++at, ++i) {   // i: the step's place in the lot
+                if (W == 8) go_first(!younger);
+                half(integral_constant<int, 0>{}, i, k_now, v_last, [&](int k) {
+                    pieces(k, kVals, [&](int x) { store_value(i + 1, x, vl[0] + v_new); }, [&](int x) { load_value(i + 2, x); });
+                });
+                lds_sync();   // (what all waves have read makes room)
+                if (W == 8) go_first(younger);
+                half(integral_constant<int, 1>{}, i, kStepBytes - k_now, v_now, [&](int k) {
+                    pieces(k, kPer, [&](int x) { store_key(i + 2, x, kl[0] + k_now); }, [&](int x) { load_key(i + 3, x); });
+                });
+                turn(at, i);
             }
-            float sc[2] = {kLogitScale, kLogitScale}, vs[2] = {1.0f, 1.0f}, rs[2] = {1.0f, 1.0f};
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                if constexpr (QT) sc[b] *= off(now.ks, b0 + b);
-                if constexpr (V8) {
-                    vs[b] = off(now.vs, b0 + b);
-                    if (vs[b] == 0.0f) vs[b] = 1.0f;   // (all its values are 0)
-                    rs[b] = 1.0f / vs[b];
-                }
-            }
-            uint32_t pw[TERMS][CT][8];   // the weights, two to a word
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                float mx = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[ct][i] *= sc[i >> 3];
-                if (!all) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int t = 8 * ((i >> 2) & 1) + 4 * h + (i & 3), at_t = at[i >> 3] + t;
-                        const bool sees = t < live[i >> 3] && at_t <= own[ct] && (at_t > own[ct] - win || at_t < c.sinks);
-                        x[ct][i] = sees ? x[ct][i] : -INFINITY;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[ct][i]);
-                mx = max_halves(mx);
-                if (__any(mx > m[ct] + kSlack || (m[ct] == -INFINITY && mx > -INFINITY))) {
-                    const float mn = fmaxf(m[ct], mx);
-                    const float f = mn == -INFINITY ? 1.0f : hw_exp2(m[ct] - mn);
-                    l[ct] *= f;
-                    lw[ct] *= f;
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) o[ct][d] *= f;
-                    m[ct] = mn;
-                }
-                const float ms = m[ct] == -INFINITY ? 0.0f : m[ct];
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    float a = hw_exp2(x[ct][i] - ms), b = hw_exp2(x[ct][i + 1] - ms);
-                    l[ct] += a + b;
-                    if constexpr (V8) {
-                        a *= vs[i >> 3];
-                        b *= vs[i >> 3];
-                    }
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t) {
-                        const uint32_t w = pack_bf16(a, b);
-                        pw[t][ct][i >> 1] = w;
-                        if constexpr (TERMS == 1) {
-                            lw[ct] = fmaf(bf16_lo(w) + bf16_hi(w), rs[i >> 3], lw[ct]);
-                        } else {
-                            a -= bf16_lo(w);
-                            b -= bf16_hi(w);
-                        }
-                    }
-                }
-            }
-            // words 4 b .. 4 b + 3: block b's tokens 4h .. 4h+3, 8+4h .. 8+4h+3
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const uint8_t* vb = vl[buf] + 8192 * sub + 4096 * b + 256 * h + 16 * (n & 15) + 8 * (n >> 4);
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const u32x2 lo = *reinterpret_cast<const u32x2*>(vb + 1024 * d), hi = *reinterpret_cast<const u32x2*>(vb + 1024 * d + 512);
-                    const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                        for (int t = 0; t < TERMS; ++t)
-                            o[ct][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                a, __builtin_bit_cast(bf16x8, u32x4{pw[t][ct][4 * b], pw[t][ct][4 * b + 1], pw[t][ct][4 * b + 2],
-                                                                    pw[t][ct][4 * b + 3]}),
-                                o[ct][d], 0, 0, 0);
-                }
+            stream(integral_constant<int, 8>{}, [&](int j) { return value_part(1, v_last, j); },
+                   [&](int j, bf16x8 a) { sum(1, j, a); }, nothing);
+        } else {   // a wave without a column that sees anything helps with the loads
+            for (int at = 0, i = 0; at < count; ++at, ++i) {
+                store_values(i + 1, v_new);
+                load_values(i + 2);
+                lds_sync();
+                store_keys(i + 2, k_now);
+                load_keys(i + 3);
+                turn(at, i);
             }
         }
-        if (more) store(j + 1, mine, buf ^ 1);
-        lds_sync();
+        __syncthreads();
     }
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        l[ct] = add_halves(l[ct]);
-        lw[ct] = TERMS == 1 ? add_halves(lw[ct]) : l[ct];
+    {   // (worked out again, not kept through the loop)
+        int again = col0 + n;
+        asm volatile("" : "+v"(again));
+        row = row_lo + (mine ? again / c.G : 0);
+        head = kv * c.G + (mine ? again % c.G : 0);
     }
+    l = add_halves(l);
+    lw = TERMS == 1 ? add_halves(lw) : l;
     // ---- A value that is not finite reaches, as 0 times it, the columns of its
     // step that do not see it.  Those with a finite sum and a result that is not
     // are worked out again, token by token: here, where it costs nothing else.
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        float z = lw[ct] * 0.0f;   // NaN unless everything is finite
+    {
+        float z = lw * 0.0f;   // NaN unless everything is finite
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z = fmaf(o[ct][d][i], 0.0f, z);
+            for (int i = 0; i < 16; ++i) z = fmaf(o[d][i], 0.0f, z);
         z = add_halves(z);
-        uint32_t bad = (uint32_t)__ballot(row_of[ct] >= 0 && own[ct] >= 0 && l[ct] * 0.0f == 0.0f && z != 0.0f);
-        if (bad == 0) continue;
+        uint32_t bad = (uint32_t)__ballot(mine && own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
         float* const y_lds = reinterpret_cast<float*>(kl[0]) + kHeadDim * wv;
         const int e = 2 * lane;   // this lane's dims: e and e + 1
         while (bad != 0) {
             const int who = __ffs(bad) - 1;
             bad &= bad - 1;
-            const int own_slot = of(own[ct], who), head = of(head_of[ct], who);
-            const float top = off(m[ct], who);
-            const int64_t q_at = (row_lo + (int64_t)((col0 + 32 * ct + who) / c.G)) * c.q_stride + head * kHeadDim + e;
+            const int own_slot = of(own, who), who_head = of(head, who);
+            const float top = off(m, who);
+            const int64_t who_q = (row_lo + (int64_t)((col0 + who) / c.G)) * c.q_stride + who_head * kHeadDim + e;
             float q0, q1, y0 = 0.0f, y1 = 0.0f;
             if (c.q_f32) {
-                q0 = static_cast<const float*>(c.q)[q_at];
-                q1 = static_cast<const float*>(c.q)[q_at + 1];
+                q0 = static_cast<const float*>(c.q)[who_q];
+                q1 = static_cast<const float*>(c.q)[who_q + 1];
             } else {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(c.q) + q_at);
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(c.q) + who_q);
                 q0 = bf16_lo(w);
                 q1 = bf16_hi(w);
             }
             for (int i = 4 * begin; i < min(n_blocks, 4 * end); ++i) {
-                if (((i - 4 * begin) & 63) == 0) mine = describe(i);
-                const int at = of(mine.at, (i - 4 * begin) & 63), live = of(mine.live, (i - 4 * begin) & 63);
-                const size_t tile_at = (size_t)of(mine.phys, (i - 4 * begin) & 63) * c.page_elems + row_elems +
-                                       (size_t)((at >> 4) & (per - 1)) * 16 * kHeadDim;
-                const bool coded = QT && of(mine.coded, (i - 4 * begin) & 63) != 0;
-                const float ks = off(mine.ks, (i - 4 * begin) & 63), vs = off(mine.vs, (i - 4 * begin) & 63);
+                if (((i - 4 * begin) & 63) == 0) cur = describe(i, page_of(i));
+                const int at = of(cur.at, (i - 4 * begin) & 63), live = of(cur.live, (i - 4 * begin) & 63);
+                const size_t tile_at = (uint64_t)(uint32_t)of((int)(uint32_t)cur.tile, (i - 4 * begin) & 63) |
+                                       ((uint64_t)(uint32_t)of((int)(cur.tile >> 32), (i - 4 * begin) & 63) << 32);
+                const bool coded = QT && of(cur.coded, (i - 4 * begin) & 63) != 0;
+                const float ks = __uint_as_float(of(cur.ks, (i - 4 * begin) & 63)), vs = __uint_as_float(of(cur.vs, (i - 4 * begin) & 63));
                 for (int t = 0; t < live; ++t) {
                     if (at + t > own_slot || (at + t <= own_slot - win && at + t >= c.sinks)) continue;
                     uint32_t kw;
@@ -542,11 +732,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
             if (n == who) {
-                lw[ct] = l[ct];
+                lw = l;
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[ct][d][i] = y_lds[32 * d + 8 * (i >> 2) + 4 * h + (i & 3)];
+                    for (int i = 0; i < 16; ++i) o[d][i] = y_lds[32 * d + 8 * (i >> 2) + 4 * h + (i & 3)];
             }
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
@@ -554,8 +744,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
     }
 
     if (status != 0) atomicOr(c.status, status);
-    // ---- register i of o[ct][d]: dim 32 d + 8 (i / 4) + 4 h + i % 4
-    auto write4 = [&](int64_t row, int head, int dim, f32x4 y) {
+    // ---- register i of o[d]: dim 32 d + 8 (i / 4) + 4 h + i % 4
+    auto write4 = [&](int dim, f32x4 y) {
         const int64_t at = row * c.out_stride + head * kHeadDim + dim;
         if (c.out_bf16)
             *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(c.out) + at) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
@@ -563,35 +753,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
             *reinterpret_cast<f32x4*>(static_cast<float*>(c.out) + at) = y;
     };
     if (parts == 1) {
+        if (!mine) return;
+        const float inv = inverse(lw);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            if (row_of[ct] < 0) continue;
-            const float inv = inverse(lw[ct]);
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    write4(row_of[ct], head_of[ct], 32 * d + 2 * i + 4 * h,
-                           f32x4{o[ct][d][i], o[ct][d][i + 1], o[ct][d][i + 2], o[ct][d][i + 3]} * inv);
-            if (c.lse != nullptr && h == 0) c.lse[row_of[ct] * c.Hq + head_of[ct]] = log_sum(m[ct], l[ct]);
-        }
+            for (int i = 0; i < 16; i += 4) write4(32 * d + 2 * i + 4 * h, f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * inv);
+        if (c.lse != nullptr && h == 0) c.lse[row * c.Hq + head] = log_sum(m, l);
         return;
     }
     // ---- the tile's parts meet in the workgroup that comes last
     const int unit = tile * c.Hkv + kv;
     float* const part0 = c.part + (size_t)unit * c.splits * kCols * kPartWords;
-    float* const part = part0 + (size_t)split * kCols * kPartWords;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        if (row_of[ct] < 0) continue;
-        float* p = part + (size_t)(wv * 32 * CT + 32 * ct + n) * kPartWords;
+    float* const own_part = part0 + (size_t)split * kCols * kPartWords;
+    if (mine) {
+        float* to = own_part + (size_t)(wv * 32 + n) * kPartWords;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) put2(p + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3), o[ct][d][i], o[ct][d][i + 1]);
+            for (int i = 0; i < 16; i += 2) put2(to + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3), o[d][i], o[d][i + 1]);
         if (h == 0) {
-            put2(p + kHeadDim, m[ct], l[ct]);
-            put2(p + kHeadDim + 2, lw[ct], 0.0f);
+            put2(to + kHeadDim, m, l);
+            put2(to + kHeadDim + 2, lw, 0.0f);
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -600,9 +783,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
     __syncthreads();
     if (sh_last == 0) return;
     const int cols = min(kCols, rows * c.G - (tile - uni(pref[s])) * kCols);
-    for (int col = wv; col < cols; col += kWaves) {   // a wave a column, two dims a lane
+    for (int k = wv; k < cols; k += W) {   // a wave a column, two dims a lane
         float M = -INFINITY, lsum = 0.0f, wsum = 0.0f, y0 = 0.0f, y1 = 0.0f;
-        const float* p = part0 + (size_t)col * kPartWords;
+        const float* p = part0 + (size_t)k * kPartWords;
 #pragma unroll 4
         for (int z = 0; z < parts; ++z) {
             const float2 st = get2(p + (size_t)z * kCols * kPartWords + kHeadDim);
@@ -616,27 +799,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_rows_attend(PromptCall c) {
             y1 = y1 * fa + y.y * fb;
             M = mn;
         }
-        const int g = (tile - uni(pref[s])) * kCols + col;
-        const int64_t row = row_lo + g / c.G;
-        const int head = kv * c.G + g % c.G;
+        const int g = (tile - uni(pref[s])) * kCols + k;
+        const int64_t to_row = row_lo + g / c.G;
+        const int to_head = kv * c.G + g % c.G;
         const float inv = inverse(wsum);
-        const int64_t at = row * c.out_stride + head * kHeadDim + 2 * lane;
+        const int64_t at = to_row * c.out_stride + to_head * kHeadDim + 2 * lane;
         if (c.out_bf16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(c.out) + at) = pack_bf16(y0 * inv, y1 * inv);
         else *reinterpret_cast<float2*>(static_cast<float*>(c.out) + at) = make_float2(y0 * inv, y1 * inv);
-        if (c.lse != nullptr && lane == 0) c.lse[row * c.Hq + head] = log_sum(M, lsum);
+        if (c.lse != nullptr && lane == 0) c.lse[to_row * c.Hq + to_head] = log_sum(M, lsum);
     }
 }
 
-template <int TERMS, int CT>
+template <int W, int TERMS>
 const void* prompt_kernel(bool keys8, bool values8) {
-    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_rows_attend<TERMS, CT, true, true>)
-                            : reinterpret_cast<const void*>(&k_rows_attend<TERMS, CT, true, false>))
-                 : (values8 ? reinterpret_cast<const void*>(&k_rows_attend<TERMS, CT, false, true>)
-                            : reinterpret_cast<const void*>(&k_rows_attend<TERMS, CT, false, false>));
+    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, true, true>)
+                            : reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, true, false>))
+                 : (values8 ? reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, false, true>)
+                            : reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, false, false>));
 }
 
-constexpr int kWideCols = kWaves * 64;    // columns of a tile, bf16 in and out
-constexpr int kExactCols = kWaves * 32;   // and in three terms
+// Waves of a workgroup, one workgroup a CU: eight where the weights are one bf16
+// term (215 - 240 registers), four where they are three (up to 400).
+constexpr int kWideWaves = 8, kExactWaves = 4;
+constexpr int kWideCols = kWideWaves * 32;    // columns of a tile, bf16 in and out
+constexpr int kExactCols = kExactWaves * 32;   // and in three terms
 
 // Parts that all tiles of a call may be cut into: a workgroup per CU.
 int most_parts(int n_cu) { return n_cu; }
@@ -696,8 +882,8 @@ hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, 
     c.part = static_cast<float*>(a.workspace) + count_words(n_cu);
     void* args[] = {&c};
     const bool keys8 = dm.quant != 0, values8 = a.values.v_pool == nullptr;
-    const void* fn = exact ? prompt_kernel<3, 1>(keys8, values8) : prompt_kernel<1, 2>(keys8, values8);
-    return hipLaunchKernel(fn, dim3((unsigned)(tiles * dm.Hkv * c.splits)), dim3(kThreads), args,
+    const void* fn = exact ? prompt_kernel<kExactWaves, 3>(keys8, values8) : prompt_kernel<kWideWaves, 1>(keys8, values8);
+    return hipLaunchKernel(fn, dim3((unsigned)(tiles * dm.Hkv * c.splits)), dim3(64 * (exact ? kExactWaves : kWideWaves)), args,
                            (size_t)(dm.S + 1) * sizeof(int), st);
 }
 

@@ -93,8 +93,14 @@ __device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
     Span x{};
     // the sessions that end at or before a row, for 32 rows at once
     int s = 0;
+    bool broken = false;   // row_start does not ascend within the rows: nobody's rows
     for (int base = 0; base < c.S; base += 64) {
-        const int end = base + lane < c.S ? c.row_start[base + lane + 1] : 0x7FFFFFFF;
+        int end = 0x7FFFFFFF;
+        if (base + lane < c.S) {
+            const int begin = c.row_start[base + lane];
+            end = c.row_start[base + lane + 1];
+            broken |= begin < 0 || begin > end || end > c.n_rows;
+        }
 #pragma unroll 8
         for (int i = 0; i < 32; ++i) {
             const int n = __popcll(__ballot(end <= r0 + i));
@@ -104,7 +110,9 @@ __device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
     x.s = min(s, c.S - 1);
     x.lo = c.row_start[x.s];
     x.hi = c.row_start[x.s + 1];
-    x.mine = s < c.S && x.lo >= 0 && x.lo <= r && r < x.hi && x.hi <= c.n_rows;
+    broken = __any(broken);
+    if (broken) status |= MD_DEV_BAD_ROW;
+    x.mine = !broken && s < c.S && x.lo <= r && r < x.hi;
     x.prev = -1;
     if (!x.mine) return x;
     const int np = c.n_pages[x.s], nt = c.n_tokens[x.s];

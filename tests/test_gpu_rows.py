@@ -192,14 +192,24 @@ def test_rows_that_do_not_count():
         have = {int(t) for t in (~got[:, 0, 0, 0].isnan()).nonzero()}
         assert have <= {t for z, t in want if z == s} and torch.equal(got.nan_to_num(-1), vals.nan_to_num(-1))
     assert int((~pool_slots(w, 1)[0][:, 0, 0, 0].isnan()).sum()) == 4
-    # row_start that does not ascend, or goes behind the rows: nobody's rows
-    for bad in ([0, 9, 5], [3, 20, 20], [-4, 2, 14], [0, -1, 14]):
-        u = World(1, 1, 1, 16, [40, 40], seed=16, coded=False, fill=False)
-        u.md.write_rows(0, u.i32(bad), k, k, row_slot=u.i32([0] * 14))
-        u.md.read_rows(0, u.i32(bad), k.clone(), k.clone(), row_slot=u.i32([0] * 14))
-        q = torch.zeros((14, 1, D), device=u.dev)
-        u.md.attend_rows(0, q, torch.empty_like(q), u.i32(bad), row_slot=u.i32([0] * 14))
-        torch.cuda.synchronize()
+
+
+def test_row_starts_that_do_not_ascend():
+    """Nobody's rows: nothing is written, read or attended."""
+    w = World(1, 1, 1, 16, [40, 40, 40], seed=16, coded=False, fill=False)
+    before = w.cache.k_pool.clone()
+    k, v = (torch.full((14, 1, D), 5.0, dtype=BF16, device=w.dev) for _ in "kv")
+    for bad in ([0, 9, 5, 14], [3, 14, 15, 15], [-4, 2, 14, 14], [0, -1, 14, 14], [0, 14, 0, 14], [14, 0, 14, 0], [0, 0, 2 ** 31 - 1, 3]):
+        for types in ((torch.float32, torch.float32), (BF16, BF16)):
+            w.md.write_rows(0, w.i32(bad), k, v, row_slot=w.i32(list(range(14))))
+            assert w.md.device_status() == B.MD_DEV_BAD_ROW, bad
+            out = torch.full((14, 1, D), 5.0, dtype=types[1], device=w.dev)
+            w.md.attend_rows(0, torch.zeros((14, 1, D), dtype=types[0], device=w.dev), out, w.i32(bad), row_slot=w.i32([0] * 14))
+            assert w.md.device_status() == B.MD_DEV_BAD_ROW, bad
+            assert (out == 5).all()
+            w.md.read_rows(0, w.i32(bad), k, v, row_slot=w.i32([0] * 14))
+            assert w.md.device_status() == B.MD_DEV_BAD_ROW and (k == 5).all() and (v == 5).all()
+    assert torch.equal(before.view(torch.uint8), w.cache.k_pool.view(torch.uint8))
 
 
 def test_descending_lists_give_the_same_bits_every_time():
