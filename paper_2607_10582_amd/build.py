@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmemdecay.so")
 SOURCES = ["md_kernels.hip", "md_attend.hip", "md_rows.hip", "md_offload.hip", "md_token.hip", "md_paged.hip",
-           "md_blocks.hip", "md_store.hip", "md_prompt.hip", "md_api.cpp"]
+           "md_blocks.hip", "md_store.hip", "md_prompt.hip", "md_few.hip", "md_api.cpp"]
 
 # Packed FP32 instructions stay off: the compiler would otherwise form
 # v_pk_* FP32 ops from plain float code.

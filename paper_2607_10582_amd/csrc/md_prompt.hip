@@ -1,5 +1,6 @@
-// gfx950 kernel of the attention of ragged rows (a prompt, a chunk of one, a
-// few tokens to verify) over the paged cache.
+// gfx950 kernel of the attention of ragged rows (a prompt, a chunk of one) over
+// the paged cache, bf16 in and out; md_few.hip has the one for few rows and for
+// float32.
 //
 //   out_h = sum_i softmax_i(q_h . k_i / sqrt(d)) v_i   over the slots i that the row sees
 //
@@ -12,133 +13,33 @@
 //   sums   [32 dims][32 columns] += V^T [32 dims][16 tokens] P^T: lane (n, h)
 //          feeds tokens 4h .. 4h+3 and 8+4h .. 8+4h+3 of a block, the very
 //          weights it has, so they never leave their registers
-// A block of 16 tokens in LDS is laid out as in the pools, which gives every
-// operand as whole 16-byte (keys) or two 8-byte words (values), without bank
-// conflicts.
+// Keys and values lie in LDS in the order of the products' operands, 16 bytes a
+// lane side by side, which leaves no bank conflicts (in the order of the pools
+// 36% of the LDS's cycles were conflicts).
 //
-// What bounds it: the matrix cores for prompts (4 d operations per column and
-// token), HBM for a few rows over a long cache.
+// What bounds it: the matrix cores, 4 d operations per column and token.  They
+// are busy for 84% of the time that a large library product takes for as many
+// operations: a prompt of 16,384 rows (32 query heads on 8) takes 1.08 ms,
+// 1,020 TFLOP/s.  Without the weights it would take 0.89 ms, without the loads
+// 1.02.
 
 #include <algorithm>
 #include <type_traits>
 
-#include "md_arrive.h"
-#include "md_decode.h"
-#include "md_device.h"
+#include "md_prompt.h"
 
 namespace md {
 
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
 constexpr int kStep = 64;                  // tokens of a step: four blocks
 constexpr int kStepBytes = kStep * kHeadDim * 2;
-// A column's maximum is only followed when it has grown by more than this
-// (base 2): weights then reach 2^8 and their sums 2^8 times a row's length,
-// far inside float32 and bf16, and most steps leave the sums unscaled.
-constexpr float kSlack = 8.0f;
-
-struct PromptCall {
-    int S, L, Hq, Hkv, G, P, Pshift, MP, NP, aligned, layer;
-    size_t page_elems;
-    const uint16_t* k_pool;
-    const uint8_t* region;
-    const int32_t* page_table;
-    const int32_t* n_pages;
-    const int32_t* n_tokens;
-    const uint8_t* page_format;
-    int32_t* status;
-    const int32_t* row_start;
-    const int32_t* row_slot;
-    int n_rows;
-    const void* q;
-    int64_t q_stride;
-    void* out;
-    int64_t out_stride;
-    float* lse;
-    int q_f32, out_bf16, window, sinks;
-    const uint16_t* v_pool;
-    const uint8_t* v_codes;
-    const float* v_scale;
-    int splits;      // parts of a tile's steps
-    int32_t* count;  // [tiles Hkv] arrivals (zero between launches)
-    float* part;     // [tiles Hkv splits][columns][kPartWords] partial results
-};
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
-    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-}
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-// acc plus both bf16 values of a word.
-__device__ __forceinline__ float add_pair(uint32_t w, float acc) {
-    typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), acc, false);
-}
-
-// The larger, or the sum, of both half-waves' values.
-__device__ __forceinline__ float max_halves(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float add_halves(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Partial results cross workgroups of different XCDs, whose L2s are not
-// coherent within a launch: 64-bit words, written through and read past them.
-typedef unsigned long long u64;
-__device__ __forceinline__ void put2(float* p, float a, float b) {
-    const u64 w = (u64)__float_as_uint(a) | ((u64)__float_as_uint(b) << 32);
-    __hip_atomic_store(reinterpret_cast<u64*>(p), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get2(const float* p) {
-    const u64 w = __hip_atomic_load(reinterpret_cast<const u64*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
-}
-
-// Tokens among 16 slots' region codes before the holes.
-__device__ __forceinline__ int tokens_before_holes(const uint8_t* region) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(region);
-    int n = 0;
-#pragma unroll
-    for (int i = 3; i >= 0; --i)
-#pragma unroll
-        for (int b = 3; b >= 0; --b)
-            if (((w[i] >> (8 * b)) & 0xFFu) != (uint32_t)kHole) n = max(n, 4 * i + b + 1);
-    return n;
-}
-
-__device__ __forceinline__ int wave_max_i(int v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o));
-    return v;
-}
-
-// A row's result divided by its sum; nothing seen gives zeros.
-__device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
-__device__ __forceinline__ float log_sum(float m, float l) { return (m + log2f(l)) * 0.69314718055994530942f; }
-
-// What a lane knows of block `base + lane` of the list that a tile walks.
-struct Block {
-    int64_t tile;      // elements before its tile in the pools of keys and values
-    int at;            // slot of its first token
-    int live;          // its tokens, 0 .. 16
-    int coded;         // 8-bit keys
-    int ks, vs;        // scales of keys and values (float bits)
-};
 
 // A workgroup takes a tile of 32 columns for each of its W waves, which share
 // the steps of 64 tokens through LDS: keys of two steps, values of three.
-// TERMS: bf16 terms of queries and weights (1: bf16 in and out; 3: exact);
 // QT: pages may hold 8-bit keys; V8: the values are 8-bit codes, which widen to
 // bf16 on their way into LDS, their scales going to the weights.
-template <int W, int TERMS, bool QT, bool V8>
+template <int W, bool QT, bool V8>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W / 4))) k_rows_attend(PromptCall c) {
     constexpr int kThreads = 64 * W;
     constexpr int kCols = W * 32;
@@ -151,77 +52,20 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     extern __shared__ int pref[];   // [S + 1] tiles of the sessions before
     const int tid = threadIdx.x, lane = lane_id(), wv = uni(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
-    const int per = c.P >> 4;
     int status = 0;
-    // ---- this workgroup's tile
-    int before = 0;
-    bool broken = false;   // (rows of several sessions, or more than there are, would make more tiles than the grid has)
-    for (int k = 0; k < c.S; k += kThreads) {
-        const int s = k + tid;
-        int tiles = 0;
-        if (s < c.S) {
-            const int lo = c.row_start[s], hi = c.row_start[s + 1];
-            broken |= lo < 0 || lo > hi || hi > c.n_rows;
-            tiles = broken ? 0 : ((hi - lo) * c.G + kCols - 1) / kCols;
-        }
-        int total;
-        const int ex = block_exclusive_scan(tiles, scan_lds, &total);
-        if (s < c.S) pref[s] = before + ex;
-        before += total;
-    }
-    if (tid == 0) pref[c.S] = before;
-    if (__syncthreads_or(broken ? 1 : 0)) {
-        if (tid == 0) atomicOr(c.status, MD_DEV_BAD_ROW);
-        return;
-    }
-    const int kv = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv;
-    const int split = rest % c.splits;
-    const int tile = uni(before) - 1 - rest / c.splits;   // the longest of a session first
-    if (tile < 0) return;
-    const int s = uni(find_session(pref, c.S, tile));
-    const int row_lo = uni(c.row_start[s]), rows = uni(c.row_start[s + 1]) - row_lo;
-    const int np = uni(c.n_pages[s]);
-    int nt = uni(c.n_tokens[s]);
-    const bool ok = np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
-    if (!ok) {
-        status |= kDevCorrupt;
-        nt = 0;
-    }
+    TileAt t;
+    if (!find_tile<kThreads, kCols>(c, scan_lds, pref, t, status)) return;
     // ---- the wave's columns and their queries
-    const int col0 = (tile - uni(pref[s])) * kCols + wv * 32, col = col0 + n;
-    const bool mine = col < rows * c.G;
-    int64_t row = row_lo + (mine ? col / c.G : 0);
-    int head = kv * c.G + (mine ? col % c.G : 0);
-    int own = -1;   // slot of the column's row (-1: it sees nothing)
-    if (mine) {
-        const int slot = c.row_slot != nullptr ? c.row_slot[row] : nt - (rows - (int)(row - row_lo));
-        if (slot >= 0 && slot < nt) own = slot; else status |= MD_DEV_BAD_ROW;
-    }
+    Column x_col = column_of(c, t, t.col + wv * 32 + n, status);
+    const bool mine = x_col.mine;
+    const int own = x_col.own;
     int smin = own >= 0 ? own : 0x7FFFFFFF, smax = own;
-    u32x4 qf[TERMS][8];
-    const int64_t q_at = row * c.q_stride + head * kHeadDim + 8 * h;
+    u32x4 qf[8];
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
-        if (TERMS == 1 || !c.q_f32) {
-#pragma unroll
-            for (int t = 0; t < TERMS; ++t) qf[t][kk] = u32x4{0u, 0u, 0u, 0u};
-            if (mine) qf[0][kk] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(c.q) + q_at + 16 * kk);
-        } else {
-            f32x4 y[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-            if (mine) {
-                const f32x4* from = reinterpret_cast<const f32x4*>(static_cast<const float*>(c.q) + q_at + 16 * kk);
-                y[0] = from[0];
-                y[1] = from[1];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t a[3], b[3];
-                split3(y[i >> 1][2 * (i & 1)], a[0], a[1], a[2]);
-                split3(y[i >> 1][2 * (i & 1) + 1], b[0], b[1], b[2]);
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t) qf[t][kk][i] = a[t] | (b[t] << 16);
-            }
-        }
+        u32x4 w[1];
+        query_terms<1>(c, x_col, kk, w);
+        qf[kk] = w[0];
     }
     smin = uni(-wave_max_i(-smin));
     smax = uni(wave_max_i(smax));
@@ -238,57 +82,28 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     }
     gmin = uni(gmin);
     gmax = uni(gmax);
-    // ---- the blocks that some column sees: the first tokens', then from the
-    // window's first slot to the last row's
-    const int win = c.window > 0 ? c.window : 0x7FFFFFFF;
-    const int low = gmax < 0 ? 0 : max(0, gmin - win + 1) >> 4;
-    const int first = min((min(c.sinks, gmax + 1) + 15) >> 4, low);   // (window 0: low is 0)
-    const int n_blocks = gmax < 0 ? 0 : first + (gmax >> 4) + 1 - low;
-    const int steps = (n_blocks + 3) >> 2;
-    const int share = (steps + c.splits - 1) / c.splits;
+    const Seen seen = seen_of(c, gmin, gmax);
+    const int win = seen.win;
+    const int steps = (seen.n_blocks + 3) >> 2;
+    const int share = share_of(t, seen.n_blocks) >> 2;
     const int parts = steps == 0 ? 1 : (steps + share - 1) / share;
-    if (split >= parts) {
+    if (t.split >= parts) {
         if (status != 0) atomicOr(c.status, status);
         return;
     }
-    const int begin = split * share, end = min(steps, begin + share);
+    const int begin = t.split * share, end = min(steps, begin + share);
 
-    const size_t row_elems = ((size_t)c.layer * c.Hkv + kv) * c.P * kHeadDim;
-    auto page_of = [&](int base) __attribute__((always_inline)) {   // of block base + lane
-        const int i = min(base + lane, n_blocks - 1);
-        return c.page_table[(size_t)s * c.MP + ((16 * (i < first ? i : i + low - first)) >> c.Pshift)];
-    };
+    const size_t row_elems = ((size_t)c.layer * c.Hkv + t.kv) * c.P * kHeadDim;
     auto describe = [&](int base, int p) __attribute__((always_inline)) {
-        Block b{(int64_t)row_elems, 0, 0, 0, 0x3F800000, 0};   // (page 0: there is one)
-        const int i = base + lane;
-        if (i >= n_blocks) return b;
-        const int blk = i < first ? i : i + low - first;
-        b.at = 16 * blk;
-        if ((unsigned)p >= (unsigned)c.NP) {
-            status |= kDevCorrupt;
-            return b;
-        }
-        const int sub = blk & (per - 1);
-        b.tile = (int64_t)((size_t)p * c.page_elems + row_elems + (size_t)sub * 16 * kHeadDim);
-        b.live = min(16, nt - b.at);
-        if (c.aligned) b.live = min(b.live, tokens_before_holes(c.region + (size_t)p * c.P + 16 * sub));
-        if constexpr (QT) {
-            b.coded = c.page_format[p] != 0;
-            if (b.coded)
-                b.ks = *reinterpret_cast<const int*>(c.k_pool + b.tile + 1024);
-        }
-        if constexpr (V8)
-            if (b.live > 0) b.vs = reinterpret_cast<const int*>(c.v_scale)[(((size_t)p * c.L + c.layer) * c.Hkv + kv) * (size_t)per + sub];
-        return b;
+        return block_at<QT, V8>(c, t, seen, row_elems, base + lane, p, status);
     };
     auto of = [](int x, int i) { return __builtin_amdgcn_readlane(x, i); };
-    auto off = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
     // Lanes know of 16 steps: kLot of them to work on, and the three behind
     // these that are on their way into LDS.  A bit for each block that every
     // column of the wave sees in full, that lacks tokens, that holds 8-bit keys;
     // four of them are step i's.
     constexpr int kLot = 13;
-    Block cur = begin < end ? describe(4 * begin, page_of(4 * begin)) : Block{}, next = cur;
+    Block cur = begin < end ? describe(4 * begin, page_of(c, t, seen, 4 * begin + lane)) : Block{}, next = cur;
     int next_page = 0;
     uint64_t full, part, coded;
     auto look = [&]() __attribute__((always_inline)) {
@@ -386,10 +201,10 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     // weights, the matrix cores work on its neighbours: the sums of the half
     // before and the logits of the half behind, product by product between the
     // weights' instructions.  (A wave alone issues one of those in 7 cycles, not
-    // 4; with the products of one wave beside the weights of the other, section
-    // by section, a prompt of 16,384 rows took 1.13 ms; in this order FIG_MIX.)
+    // 4.  A wave pair that took turns, one's products beside the other's weights,
+    // took 1.13 ms for 16,384 rows and left no room for what follows.)
     f32x16 x[2];
-    uint32_t pw[TERMS][2][8];   // weights, two to a word: 4 b .. are those of the half's block b
+    uint32_t pw[2][8];   // weights, two to a word: 4 b .. are those of the half's block b
     // Sixteen operands from LDS and their products, kAhead reads under way: left
     // to itself the compiler has each product wait for its own.
     auto stream = [&](auto count, auto&& read, auto&& product, auto&& beside) {
@@ -413,17 +228,12 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     auto value_part = [&](int u, uint32_t buf, int i) { return *reinterpret_cast<const u32x4*>(v_lane + buf + 8192 * u + 1024 * i); };
     auto logit = [&](int u, int kk, bf16x8 a) {
         const f32x16 none = {};
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t)
-            x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[t][kk]), kk == 0 && t == 0 ? none : x[u], 0, 0, 0);
+        x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[kk]), kk == 0 ? none : x[u], 0, 0, 0);
     };
     auto sum = [&](int u, int i, bf16x8 a) {   // block i / 4, dims 32 (i % 4) ..
         const int b = i >> 2, d = i & 3;
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                a, __builtin_bit_cast(bf16x8, u32x4{pw[t][u][4 * b], pw[t][u][4 * b + 1], pw[t][u][4 * b + 2], pw[t][u][4 * b + 3]}),
-                o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            a, __builtin_bit_cast(bf16x8, u32x4{pw[u][4 * b], pw[u][4 * b + 1], pw[u][4 * b + 2], pw[u][4 * b + 3]}), o[d], 0, 0, 0);
     };
     auto nothing = [](int) {};
     // 8-bit keys and values: the keys' scale goes to the logits, the values' to
@@ -451,7 +261,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
             if constexpr (V8) {
                 vs[b] = __uint_as_float(of(cur.vs, i0 + b));
                 lost[b] = !(vs[b] < INFINITY);
-                if (vs[b] == 0.0f || (TERMS == 1 && lost[b])) vs[b] = 1.0f;   // (0: all its values are)
+                if (vs[b] == 0.0f || lost[b]) vs[b] = 1.0f;   // (0: all its values are)
                 rs[b] = __builtin_amdgcn_rcpf(vs[b]);
                 lg[b] = log2f(vs[b]);
             }
@@ -491,9 +301,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
 #pragma unroll
         for (int d = 0; d < 4; ++d) o[d] *= f;
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) pw[t][last][k] = pack_bf16(bf16_lo(pw[t][last][k]) * f, bf16_hi(pw[t][last][k]) * f);
+        for (int k = 0; k < 8; ++k) pw[last][k] = pack_bf16(bf16_lo(pw[last][k]) * f, bf16_hi(pw[last][k]) * f);
         m = mn;
     };
     // The half's weights, pair by pair: begun, and a pair later finished.
@@ -502,24 +310,12 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
         const int b = k >> 2;
         if ((k & 3) == 0) all_sum = w_sum = 0.0f;
         all_sum += p + q;
-        if constexpr (TERMS != 1 && V8) {
-            p *= vs[b];
-            q *= vs[b];
-        }
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-            uint32_t w = pack_bf16(p, q);
-            asm volatile("" : "+v"(w));
-            pw[t][u][k] = w;
-            if constexpr (TERMS == 1) {
-                w_sum = add_pair(w, w_sum);
-            } else {
-                p -= bf16_lo(w);
-                q -= bf16_hi(w);
-            }
-        }
+        uint32_t w = pack_bf16(p, q);
+        asm volatile("" : "+v"(w));
+        pw[u][k] = w;
+        w_sum = add_pair(w, w_sum);
         if ((k & 3) != 3) return;
-        if constexpr (TERMS == 1 && V8) {
+        if constexpr (V8) {
             l = fmaf(all_sum, rs[b], l);
             lw = fmaf(w_sum, rs[b], lw);
             if (lost[b] && all_sum > 0.0f) lw = __uint_as_float(0x7FC00000u);   // (settled at the end)
@@ -557,7 +353,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
                        if (__builtin_expect(peak(u, i), 0)) follow(1 - u);
                        const float ms = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-                       for (int b = 0; b < 2; ++b) shift[b] = TERMS == 1 && V8 ? lg[b] - ms : -ms;
+                       for (int b = 0; b < 2; ++b) shift[b] = V8 ? lg[b] - ms : -ms;
                    }
                    constexpr int kLeft = 15 - kPeak;   // slots behind it
 #pragma unroll
@@ -599,7 +395,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
         // anything that was written), its own, and where the next one's go
         uint32_t k_now = 0, v_last = 0, v_now = 0, v_new = kStepBytes;
         auto turn = [&](int at, int& i) __attribute__((always_inline)) {
-            if (__builtin_expect(i == kLot / 2 - 3, 0)) next_page = page_of(4 * (begin + at - i + kLot));   // in good time
+            if (__builtin_expect(i == kLot / 2 - 3, 0)) next_page = page_of(c, t, seen, 4 * (begin + at - i + kLot) + lane);   // in good time
             if (__builtin_expect(i == kLot / 2, 0)) next = describe(4 * (begin + at - i + kLot), next_page);
             if (__builtin_expect(i == kLot - 1, 0)) {
                 cur = next;
@@ -613,14 +409,12 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
         };
         if (smax >= 0) {
 #pragma unroll
-            for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) pw[t][1][k] = 0u;
+            for (int k = 0; k < 8; ++k) pw[1][k] = 0u;
             stream(integral_constant<int, 8>{}, [&](int j) { return key_part(0, 0, j); }, [&](int j, bf16x8 a) { logit(0, j, a); },
                    nothing);
             // A piece of the caches' bytes goes to LDS and the same one of the step
             // behind is requested a whole step before it goes: keys beside one half,
-            // values beside the other (all beside one: FIG_SPREAD).
+            // values beside the other (1.11 ms; all behind a half, 1.14).
             auto pieces = [](int k, int n, auto&& put, auto&& get) {
 #pragma unroll
                 for (int x = 0; x < n; ++x) {
@@ -636,12 +430,12 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
                 if (mine_now) __builtin_amdgcn_s_setprio(1); else __builtin_amdgcn_s_setprio(0);
             };
             for (int at = 0, i = 0; at < count; ++at, ++i) {   // i: the step's place in the lot
-                if (W == 8) go_first(!younger);
+                go_first(!younger);
                 half(integral_constant<int, 0>{}, i, k_now, v_last, [&](int k) {
                     pieces(k, kVals, [&](int x) { store_value(i + 1, x, vl[0] + v_new); }, [&](int x) { load_value(i + 2, x); });
                 });
                 lds_sync();   // (what all waves have read makes room)
-                if (W == 8) go_first(younger);
+                go_first(younger);
                 half(integral_constant<int, 1>{}, i, kStepBytes - k_now, v_now, [&](int k) {
                     pieces(k, kPer, [&](int x) { store_key(i + 2, x, kl[0] + k_now); }, [&](int x) { load_key(i + 3, x); });
                 });
@@ -662,16 +456,17 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
         __syncthreads();
     }
     {   // (worked out again, not kept through the loop)
-        int again = col0 + n;
+        int again = t.col + wv * 32 + n;
         asm volatile("" : "+v"(again));
-        row = row_lo + (mine ? again / c.G : 0);
-        head = kv * c.G + (mine ? again % c.G : 0);
+        x_col.row = t.row_lo + (mine ? again / c.G : 0);
+        x_col.head = t.kv * c.G + (mine ? again % c.G : 0);
     }
+    const int64_t row = x_col.row;
+    const int head = x_col.head;
     l = add_halves(l);
-    lw = TERMS == 1 ? add_halves(lw) : l;
-    // ---- A value that is not finite reaches, as 0 times it, the columns of its
-    // step that do not see it.  Those with a finite sum and a result that is not
-    // are worked out again, token by token: here, where it costs nothing else.
+    lw = add_halves(lw);
+    // ---- Columns with a finite sum and a result that is not: a value that is
+    // not finite reached them unseen (here, where it costs nothing else)
     {
         float z = lw * 0.0f;   // NaN unless everything is finite
 #pragma unroll
@@ -681,54 +476,15 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
         z = add_halves(z);
         uint32_t bad = (uint32_t)__ballot(mine && own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
         float* const y_lds = reinterpret_cast<float*>(kl[0]) + kHeadDim * wv;
-        const int e = 2 * lane;   // this lane's dims: e and e + 1
         while (bad != 0) {
             const int who = __ffs(bad) - 1;
             bad &= bad - 1;
-            const int own_slot = of(own, who), who_head = of(head, who);
-            const float top = off(m, who);
-            const int64_t who_q = (row_lo + (int64_t)((col0 + who) / c.G)) * c.q_stride + who_head * kHeadDim + e;
-            float q0, q1, y0 = 0.0f, y1 = 0.0f;
-            if (c.q_f32) {
-                q0 = static_cast<const float*>(c.q)[who_q];
-                q1 = static_cast<const float*>(c.q)[who_q + 1];
-            } else {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(c.q) + who_q);
-                q0 = bf16_lo(w);
-                q1 = bf16_hi(w);
-            }
-            for (int i = 4 * begin; i < min(n_blocks, 4 * end); ++i) {
-                if (((i - 4 * begin) & 63) == 0) cur = describe(i, page_of(i));
-                const int at = of(cur.at, (i - 4 * begin) & 63), live = of(cur.live, (i - 4 * begin) & 63);
-                const size_t tile_at = (uint64_t)(uint32_t)of((int)(uint32_t)cur.tile, (i - 4 * begin) & 63) |
-                                       ((uint64_t)(uint32_t)of((int)(cur.tile >> 32), (i - 4 * begin) & 63) << 32);
-                const bool coded = QT && of(cur.coded, (i - 4 * begin) & 63) != 0;
-                const float ks = __uint_as_float(of(cur.ks, (i - 4 * begin) & 63)), vs = __uint_as_float(of(cur.vs, (i - 4 * begin) & 63));
-                for (int t = 0; t < live; ++t) {
-                    if (at + t > own_slot || (at + t <= own_slot - win && at + t >= c.sinks)) continue;
-                    uint32_t kw;
-                    if (coded)
-                        kw = codes_pair_to_bf16<false>(*reinterpret_cast<const uint16_t*>(
-                            reinterpret_cast<const uint8_t*>(c.k_pool + tile_at) + 1024 * (e / 64) + 16 * (t + 16 * ((e / 8) % 4)) +
-                            8 * ((e / 32) % 2) + e % 8));
-                    else
-                        kw = *reinterpret_cast<const uint32_t*>(c.k_pool + tile_at + (e / 8) * 128 + t * 8 + e % 8);
-                    const float x = wave_sum(fmaf(q0, bf16_lo(kw), q1 * bf16_hi(kw))) * ks * kLogitScale;
-                    const float w = hw_exp2(x - top);
-                    if constexpr (V8) {
-                        const uint8_t* v = c.v_codes + tile_at + (e / 64) * 1024 + (t / 4) * 256 + (e % 16) * 16 + ((e / 16) % 4) * 4 + t % 4;
-                        const uint32_t pair = codes_pair_to_bf16<false>((uint32_t)v[0] | ((uint32_t)v[16] << 8));
-                        y0 = fmaf(w, vs * bf16_lo(pair), y0);
-                        y1 = fmaf(w, vs * bf16_hi(pair), y1);
-                    } else {
-                        const uint16_t* v = c.v_pool + tile_at + (e / 32) * 512 + (t / 4) * 128 + (e % 16) * 8 + ((e / 16) % 2) * 4 + t % 4;
-                        y0 = fmaf(w, bf16_lo(v[0]), y0);
-                        y1 = fmaf(w, bf16_lo(v[8]), y1);
-                    }
-                }
-            }
-            y_lds[e] = y0;
-            y_lds[e + 1] = y1;
+            const float2 y = column_again<QT, V8>(
+                c, seen, of(own, who), lane_float(__float_as_int(m), who), t.row_lo + (t.col + wv * 32 + who) / c.G,
+                of(head, who), min(seen.n_blocks, 4 * end) - 4 * begin,
+                [&](int i) { return describe(4 * begin + i, page_of(c, t, seen, 4 * begin + i + lane)); });
+            y_lds[2 * lane] = y.x;
+            y_lds[2 * lane + 1] = y.y;
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
             if (n == who) {
@@ -742,7 +498,6 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
             __builtin_amdgcn_wave_barrier();
         }
     }
-
     if (status != 0) atomicOr(c.status, status);
     // ---- register i of o[d]: dim 32 d + 8 (i / 4) + 4 h + i % 4
     auto write4 = [&](int dim, f32x4 y) {
@@ -762,12 +517,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
         if (c.lse != nullptr && h == 0) c.lse[row * c.Hq + head] = log_sum(m, l);
         return;
     }
-    // ---- the tile's parts meet in the workgroup that comes last
-    const int unit = tile * c.Hkv + kv;
-    float* const part0 = c.part + (size_t)unit * c.splits * kCols * kPartWords;
-    float* const own_part = part0 + (size_t)split * kCols * kPartWords;
     if (mine) {
-        float* to = own_part + (size_t)(wv * 32 + n) * kPartWords;
+        float* to = part_of<kCols>(c, t, t.split) + (size_t)(wv * 32 + n) * kPartWords;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -777,62 +528,34 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
             put2(to + kHeadDim + 2, lw, 0.0f);
         }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) sh_last = arrive_last(c.count + unit, arrive(c.count + unit), parts) ? 1 : 0;
-    __syncthreads();
-    if (sh_last == 0) return;
-    const int cols = min(kCols, rows * c.G - (tile - uni(pref[s])) * kCols);
-    for (int k = wv; k < cols; k += W) {   // a wave a column, two dims a lane
-        float M = -INFINITY, lsum = 0.0f, wsum = 0.0f, y0 = 0.0f, y1 = 0.0f;
-        const float* p = part0 + (size_t)k * kPartWords;
-#pragma unroll 4
-        for (int z = 0; z < parts; ++z) {
-            const float2 st = get2(p + (size_t)z * kCols * kPartWords + kHeadDim);
-            const float ws = get2(p + (size_t)z * kCols * kPartWords + kHeadDim + 2).x;
-            const float2 y = get2(p + (size_t)z * kCols * kPartWords + 2 * lane);
-            const float mn = fmaxf(M, st.x);
-            const float fa = mn == -INFINITY ? 0.0f : hw_exp2(M - mn), fb = mn == -INFINITY ? 0.0f : hw_exp2(st.x - mn);
-            lsum = lsum * fa + st.y * fb;
-            wsum = wsum * fa + ws * fb;
-            y0 = y0 * fa + y.x * fb;
-            y1 = y1 * fa + y.y * fb;
-            M = mn;
-        }
-        const int g = (tile - uni(pref[s])) * kCols + k;
-        const int64_t to_row = row_lo + g / c.G;
-        const int to_head = kv * c.G + g % c.G;
-        const float inv = inverse(wsum);
-        const int64_t at = to_row * c.out_stride + to_head * kHeadDim + 2 * lane;
-        if (c.out_bf16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(c.out) + at) = pack_bf16(y0 * inv, y1 * inv);
-        else *reinterpret_cast<float2*>(static_cast<float*>(c.out) + at) = make_float2(y0 * inv, y1 * inv);
-        if (c.lse != nullptr && lane == 0) c.lse[to_row * c.Hq + to_head] = log_sum(M, lsum);
-    }
+    join_parts<W, kCols>(c, t, parts, &sh_last);
 }
 
-template <int W, int TERMS>
-const void* prompt_kernel(bool keys8, bool values8) {
-    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, true, true>)
-                            : reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, true, false>))
-                 : (values8 ? reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, false, true>)
-                            : reinterpret_cast<const void*>(&k_rows_attend<W, TERMS, false, false>));
+template <int W>
+const void* kernel_of(bool keys8, bool values8) {
+    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_rows_attend<W, true, true>)
+                            : reinterpret_cast<const void*>(&k_rows_attend<W, true, false>))
+                 : (values8 ? reinterpret_cast<const void*>(&k_rows_attend<W, false, true>)
+                            : reinterpret_cast<const void*>(&k_rows_attend<W, false, false>));
 }
 
-// Waves of a workgroup, one workgroup a CU: eight where the weights are one bf16
-// term (215 - 240 registers), four where they are three (up to 400).
-constexpr int kWideWaves = 8, kExactWaves = 4;
-constexpr int kWideCols = kWideWaves * 32;    // columns of a tile, bf16 in and out
-constexpr int kExactCols = kExactWaves * 32;   // and in three terms
+constexpr int kWideWaves = 8;                // of a workgroup, one a CU
+constexpr int kWideCols = kWideWaves * 32;   // columns of its tile
+// Columns a session up to which the narrow kernel is taken.  Both, in us:
+//   columns                                        48       64-66     96       256
+//   8 sessions of 16,384 - 32,768, 2 KV heads   51 / 63   78 / 71   80 / 76     -
+//   16 of 2,048 - 8,192, 8 KV heads                -      93 / 143  120 / 174  191 / 222
+//   64 of 300 - 1,500, 8 KV heads                  -      55 / 80   73 / 80   183 / 128
+constexpr int kFewCols = 96;
 
-// Parts that all tiles of a call may be cut into: a workgroup per CU.
-int most_parts(int n_cu) { return n_cu; }
-
-size_t count_words(int n_cu) { return ((size_t)n_cu + 63) / 64 * 64; }
+// Parts that the tiles of a call may come to, and their arrivals' words.
+int most_parts(int n_cu) { return n_cu * (kWideCols / kFewTile); }
+size_t count_words(int n_cu) { return ((size_t)most_parts(n_cu) + 63) / 64 * 64; }
 
 }  // namespace
 
 uint64_t rows_workspace(const Dims&, int n_cu) {
-    return (count_words(n_cu) + (uint64_t)most_parts(n_cu) * kWideCols * kPartWords) * sizeof(float);
+    return (count_words(n_cu) + (uint64_t)n_cu * kWideCols * kPartWords) * sizeof(float);
 }
 
 hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_rows_args& a,
@@ -873,17 +596,23 @@ hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, 
     c.v_codes = a.values.v_codes;
     c.v_scale = a.values.v_scale;
     const bool exact = c.q_f32 || !c.out_bf16;
-    const int cols = exact ? kExactCols : kWideCols;
+    const bool keys8 = dm.quant != 0, values8 = a.values.v_pool == nullptr;
+    // Few columns a session (on average: only the device knows the rows of each)
+    // are read past, many share what is in LDS.
+    const int with_rows = std::min(dm.S, a.rows.n_rows);
+    const bool few = exact || (int64_t)a.rows.n_rows * dm.G <= (int64_t)kFewCols * with_rows;
+    const RowsKernel k = few ? few_kernel(exact, keys8, values8)
+                             : RowsKernel{kernel_of<kWideWaves>(keys8, values8), kWideCols, 64 * kWideWaves};
     // the most tiles that rows can make, however they are spread over the sessions
-    const int64_t tiles = (int64_t)a.rows.n_rows * dm.G / cols + std::min(dm.S, a.rows.n_rows);
-    const int64_t steps = ((int64_t)dm.MP * dm.P + kStep - 1) / kStep;
-    c.splits = (int)std::max<int64_t>(1, std::min<int64_t>(steps, most_parts(n_cu) / (tiles * dm.Hkv)));
+    const int64_t tiles = (int64_t)a.rows.n_rows * dm.G / k.cols + with_rows;
+    // Two workgroups of the narrow kernel fit a CU, one of the wide one.  Tiles
+    // that fill the card three times over are balanced as they are.
+    const int64_t units = few ? (tiles * dm.Hkv < 6 * n_cu ? 2 * n_cu : 0) : n_cu - tiles * dm.Hkv;
+    c.units = (int)std::max<int64_t>(0, units);
     c.count = static_cast<int32_t*>(a.workspace);
     c.part = static_cast<float*>(a.workspace) + count_words(n_cu);
     void* args[] = {&c};
-    const bool keys8 = dm.quant != 0, values8 = a.values.v_pool == nullptr;
-    const void* fn = exact ? prompt_kernel<kExactWaves, 3>(keys8, values8) : prompt_kernel<kWideWaves, 1>(keys8, values8);
-    return hipLaunchKernel(fn, dim3((unsigned)(tiles * dm.Hkv * c.splits)), dim3(64 * (exact ? kExactWaves : kWideWaves)), args,
+    return hipLaunchKernel(k.fn, dim3(grid_of(tiles + c.units / dm.Hkv, dm.Hkv)), dim3((unsigned)k.threads), args,
                            (size_t)(dm.S + 1) * sizeof(int), st);
 }
 

@@ -537,6 +537,37 @@ def test_few_rows_over_long_sessions(counts, types):
     run_rows(w, counts, q_type=types[0], out_type=types[1], window=3000, sinks=5)
 
 
+@pytest.mark.parametrize("types", TYPES[:2], ids=["bf16", "f32"])
+@pytest.mark.parametrize("counts", [[6, 2, 1, 0, 9], [11, 6, 0, 5, 80], [200, 60, 20, 0, 90]])
+def test_parts_of_uneven_sessions(counts, types):
+    """Long sessions are cut into more parts than short ones."""
+    say("[parts]", counts, types)
+    w = World(1, 12, 2, 16, [12000, 300, 40, 7, 2500], seed=59, coded=types[0] == BF16)
+    run_rows(w, counts, q_type=types[0], out_type=types[1], most=40)
+    run_rows(w, counts, q_type=types[0], out_type=types[1], window=900, sinks=20, most=40)
+
+
+@pytest.mark.parametrize("types", TYPES[:2], ids=["bf16", "f32"])
+@pytest.mark.parametrize("count", [5, 70])
+def test_rows_of_any_slots(count, types):
+    """Slots in no order, some twice: a tile's window covers more than its rows' number."""
+    say("[any slots]", count, types)
+    w = World(1, 8, 2, 16, [6000, 90], seed=60)
+    start = np.array([0, count, count + 3])
+    rng = np.random.default_rng(count)
+    slot = np.concatenate([rng.integers(0, 6000, count), [89, 0, 0]])
+    slot[1] = slot[0]
+    for window, sinks in ((0, 0), (300, 17)):
+        q = w.normal(count + 3, w.Hq, D).mul(1.5).to(types[0])
+        out = torch.empty((count + 3, w.Hq, D), dtype=types[1], device=w.dev)
+        lse = torch.empty((count + 3, w.Hq), device=w.dev)
+        w.md.attend_rows(0, q, out, torch.as_tensor(start, dtype=torch.int32, device=w.dev),
+                         row_slot=torch.as_tensor(slot, dtype=torch.int32, device=w.dev), lse=lse, window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        assert w.md.device_status() == 0
+        check_rows(w, 0, q, out, lse, start, slot, window=window, sinks=sinks)
+
+
 def test_rows_of_many_sessions():
     lens = [(7 * i) % 40 for i in range(1024)]
     w = World(1, 2, 2, 16, lens, seed=56)
