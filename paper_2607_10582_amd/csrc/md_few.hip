@@ -155,8 +155,25 @@ __global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_pe
         store_values(k);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
+        // what the lanes know of this half, before they may learn of the next lot
+        int at[2], live[2];
+        float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};
+        bool coded[2] = {false, false};
+        const bool all = ((full >> (2 * k)) & 3) == 3;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            at[b] = lane_int(cur.at, 2 * k + b);
+            live[b] = lane_int(cur.live, 2 * k + b);
+            if (QT) coded[b] = lane_int(cur.coded, 2 * k + b) != 0;
+            if (QT) ks[b] = lane_float(cur.ks, 2 * k + b);
+            if (V8) vs[b] = lane_float(cur.vs, 2 * k + b);
+        }
+        // (unconditional: behind the last half its own bytes again, out of the cache)
+        const int next = min(i + 1, count - 1);
+        if ((next & 31) == 0 && next > i) look(next);
+        load_values(cur, next & 31);
         if (QT) {
-            const bool first = lane_int(cur.coded, 2 * k) != 0, second = lane_int(cur.coded, 2 * k + 1) != 0;
+            const bool first = coded[0], second = coded[1];
             if (first || second) {
                 const bool mine = n < 16 ? first : second;
                 u32x4 w[4] = {rk[0], rk[1], rk[2], rk[3]};
@@ -169,11 +186,8 @@ __global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_pe
                 }
             }
         }
-        // this half's scales, before the lanes may learn of the next lot
-        float sc[2], vs[2], rs[2], lg[2];
-        int at[2], live[2];
+        float sc[2], rs[2], lg[2];
         bool lost[2];
-        const bool all = ((full >> (2 * k)) & 3) == 3;
         f32x16 x;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
@@ -186,34 +200,26 @@ __global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_pe
             }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            at[b] = lane_int(cur.at, 2 * k + b);
-            live[b] = lane_int(cur.live, 2 * k + b);
             sc[b] = kLogitScale;
             if constexpr (QT) {
-                const float ks = lane_float(cur.ks, 2 * k + b);
-                if (ks > 0.0f && ks < INFINITY) {
-                    sc[b] *= ks;
+                if (ks[b] > 0.0f && ks[b] < INFINITY) {
+                    sc[b] *= ks[b];
                 } else {   // (no factor for the -infinity of a token that is not seen)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[8 * b + e] *= ks;
+                    for (int e = 0; e < 8; ++e) x[8 * b + e] *= ks[b];
                 }
             }
-            vs[b] = rs[b] = 1.0f;
+            rs[b] = 1.0f;
             lg[b] = 0.0f;
             lost[b] = false;
             if constexpr (V8) {
-                vs[b] = lane_float(cur.vs, 2 * k + b);
                 lost[b] = !(vs[b] < INFINITY);
                 if (vs[b] == 0.0f || (TERMS == 1 && lost[b])) vs[b] = 1.0f;   // (0: all its values are)
                 rs[b] = 1.0f / vs[b];
                 lg[b] = log2f(vs[b]);
             }
         }
-        // (unconditional: behind the last half its own bytes again, out of the cache)
-        const int next = min(i + 1, count - 1);
-        if ((next & 31) == 0 && next > i) look(next);
         load_keys(cur, next & 31);
-        load_values(cur, next & 31);
         if (!all) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
