@@ -16,7 +16,7 @@
 //
 // What bounds it: the bytes of keys and values for up to 32 columns a session, the
 // products above.  5 rows of 6 columns over 8 sessions of 16,384 to 32,768 tokens
-// in float32 take 55 us (the 200 MB alone, 28); 11 us of it are the same for a
+// in float32 take 48 us (the 200 MB alone, 28); 11 us of it are the same for a
 // single session: finding the tile, the page, the first tokens, and the join.
 // Through LDS, with a barrier a step and one wave of four at work, 130 us.
 
@@ -26,20 +26,19 @@ namespace md {
 
 namespace {
 
-constexpr int kFewWaves = 4;
 constexpr int kRowWords = kHeadDim + 4;   // of a column's result in LDS
 
-template <int TERMS, bool QT, bool V8>
-__global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) k_rows_few(PromptCall c) {
-    constexpr int W = kFewWaves, kThreads = 64 * W;
+template <int W, int TERMS, bool QT, bool V8>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) k_rows_few(PromptCall c) {
+    constexpr int kThreads = 64 * W;
     constexpr int kQueryBytes = TERMS * 8 * 1024, kValueBytes = 32 * kHeadDim * 2;
     constexpr int kResultBytes = W * kFewTile * kRowWords * 4;
     constexpr int kBytes = kQueryBytes + W * kValueBytes > kResultBytes ? kQueryBytes + W * kValueBytes : kResultBytes;
     __shared__ __align__(16) uint8_t lds[kBytes];   // queries and values, then the waves' results
-    __shared__ int scan_lds[17];
+    __shared__ int scan_lds[2 * 17];
     __shared__ int sh_last;
     extern __shared__ int pref[];   // [S + 1] tiles of the sessions before
-    static_assert(2 * (kBytes + 256 + (kMaxSessions + 1) * 4) <= 160 * 1024, "two workgroups a CU");
+    static_assert(8 / W * (kBytes + 256 + (kMaxSessions + 1) * 4) <= 160 * 1024, "eight waves a CU");
     const int tid = threadIdx.x, lane = lane_id(), wv = uni(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
     int status = 0;
@@ -334,12 +333,14 @@ __global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_pe
         if (h == 0) *reinterpret_cast<f32x4*>(to + kHeadDim) = f32x4{m, l, lw, 0.0f};
     }
     __syncthreads();
+    // (eight threads a column: of eight waves, four take the columns)
     const int k = tid >> 3, j = tid & 7;   // column, and which of its dims
+    const bool there = k < kFewTile && t.col + k < t.rows * c.G;
     float M = -INFINITY, lsum = 0.0f, wsum = 0.0f;
     f32x4 y[4] = {};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        const float* from = result + (size_t)(w * kFewTile + k) * kRowWords;
+        const float* from = result + (size_t)(w * kFewTile + k % kFewTile) * kRowWords;
         const f32x4 st = *reinterpret_cast<const f32x4*>(from + kHeadDim);
         const float mn = fmaxf(M, st[0]);
         const float fa = mn == -INFINITY ? 0.0f : hw_exp2(M - mn), fb = mn == -INFINITY ? 0.0f : hw_exp2(st[0] - mn);
@@ -349,7 +350,6 @@ __global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_pe
         for (int i = 0; i < 4; ++i) y[i] = y[i] * fa + *reinterpret_cast<const f32x4*>(from + 4 * j + 32 * i) * fb;
         M = mn;
     }
-    const bool there = t.col + k < t.rows * c.G;
     if (parts == 1) {
         const int g = t.col + k;
         if (there) write_column(c, t.row_lo + g / c.G, t.kv * c.G + g % c.G, j, y, M, lsum, wsum);
@@ -370,18 +370,19 @@ __global__ void __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_pe
     join_parts<W, kFewTile>(c, t, parts, &sh_last);
 }
 
-template <int TERMS>
+template <int W, int TERMS>
 const void* kernel_of(bool keys8, bool values8) {
-    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_rows_few<TERMS, true, true>)
-                            : reinterpret_cast<const void*>(&k_rows_few<TERMS, true, false>))
-                 : (values8 ? reinterpret_cast<const void*>(&k_rows_few<TERMS, false, true>)
-                            : reinterpret_cast<const void*>(&k_rows_few<TERMS, false, false>));
+    return keys8 ? (values8 ? reinterpret_cast<const void*>(&k_rows_few<W, TERMS, true, true>)
+                            : reinterpret_cast<const void*>(&k_rows_few<W, TERMS, true, false>))
+                 : (values8 ? reinterpret_cast<const void*>(&k_rows_few<W, TERMS, false, true>)
+                            : reinterpret_cast<const void*>(&k_rows_few<W, TERMS, false, false>));
 }
 
 }  // namespace
 
-RowsKernel few_kernel(bool exact, bool keys8, bool values8) {
-    return RowsKernel{exact ? kernel_of<3>(keys8, values8) : kernel_of<1>(keys8, values8), kFewTile, 64 * kFewWaves};
+RowsKernel few_kernel(bool all, bool exact, bool keys8, bool values8) {
+    return all ? RowsKernel{exact ? kernel_of<8, 3>(keys8, values8) : kernel_of<8, 1>(keys8, values8), kFewTile, 512}
+               : RowsKernel{exact ? kernel_of<4, 3>(keys8, values8) : kernel_of<4, 1>(keys8, values8), kFewTile, 256};
 }
 
 }  // namespace md

@@ -38,7 +38,8 @@ struct PromptCall {
     const uint16_t* v_pool;
     const uint8_t* v_codes;
     const float* v_scale;
-    int units;       // parts that the tiles may be cut into beyond one each
+    int units;       // parts that all tiles should come to, if they are fewer,
+    int least_units; // and those that they may be cut into besides one each if not
     int32_t* count;  // [parts] arrivals of a tile's, at its first (zero between launches)
     float* part;     // [parts][columns][kPartWords] partial results
 };
@@ -118,8 +119,9 @@ struct TileAt {
 
 // The parts are of one size over all sessions, so that a session three times as
 // long as another has three times as many and all end together (cut into the same
-// number, 16 sessions of 2,048 to 8,192 tokens, 16 rows, float32, took 137 us
-// instead of 115).  A group is 8
+// number, a call on 16 sessions of 2,048 to 8,192 tokens, 8 rows, 8-bit values
+// took 58 us instead of 55, one on 8 of 16,384 to 32,768, 16 rows, 102 instead of
+// 66).  A group is 8
 // blocks; a part has at least kLeastGroups, what joining it costs.
 constexpr int kGroup = 128, kLeastGroups = 4;
 
@@ -149,19 +151,24 @@ __device__ __forceinline__ bool find_tile(const PromptCall& c, int* scan_lds, in
     };
     int share = 0;
     if (c.units > 0) {   // (then tiles Hkv < 2^11)
-        int all = 0;
+        int all = 0, most = 0;
         for (int k = 0; k < c.S; k += kThreads) {
-            int total;
-            block_exclusive_scan(tiles_of(k + tid) * groups_of(k + tid), scan_lds, &total);
-            all += total;
+            const int tiles = tiles_of(k + tid), of[2] = {tiles * groups_of(k + tid), tiles};
+            int ex[2], total[2];
+            block_exclusive_scan_n<2>(of, scan_lds, ex, total);
+            all += total[0];
+            most += total[1];
         }
-        share = max(kLeastGroups, (all * c.Hkv + c.units - 1) / c.units);
+        // (with their short last parts they are no more than fit the card at once: a
+        // second round of a few cost a tenth to a fifth of the call)
+        const int units = max(c.units - most * c.Hkv, c.least_units);
+        if (units > 0) share = max(kLeastGroups, (all * c.Hkv + units - 1) / units);
     }
     int before = 0;
     for (int k = 0; k < c.S; k += kThreads) {
         const int s = k + tid;
         int n = tiles_of(s);
-        if (c.units > 0) n *= max(1, (groups_of(s) + share - 1) / share);
+        if (share > 0) n *= max(1, (groups_of(s) + share - 1) / share);
         int total;
         const int ex = block_exclusive_scan(n, scan_lds, &total);
         if (s < c.S) pref[s] = before + ex;
@@ -438,6 +445,6 @@ struct RowsKernel {
     const void* fn;
     int cols, threads;
 };
-RowsKernel few_kernel(bool exact, bool keys8, bool values8);   // md_few.hip
+RowsKernel few_kernel(bool all, bool exact, bool keys8, bool values8);   // md_few.hip; all: a CU's eight waves
 
 }  // namespace md

@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     constexpr int kPer = kStepBytes / (16 * kThreads);   // 16-byte loads of a thread for a step's keys
     __shared__ __align__(16) uint8_t kl[2][kStepBytes];
     __shared__ __align__(16) uint8_t vl[3][kStepBytes];
-    __shared__ int scan_lds[17];
+    __shared__ int scan_lds[2 * 17];
     __shared__ int range_lds[2][W];
     __shared__ int sh_last;
     extern __shared__ int pref[];   // [S + 1] tiles of the sessions before
@@ -542,12 +542,12 @@ const void* kernel_of(bool keys8, bool values8) {
 constexpr int kWideWaves = 8;                // of a workgroup, one a CU
 constexpr int kWideCols = kWideWaves * 32;   // columns of its tile
 // Columns a session up to which the narrow kernel is taken.  Both, in us:
-//   columns                                        48       64-66     96       256
-//   8 sessions of 16,384 - 32,768, 2 KV heads   51 / 63   78 / 71   80 / 76     -
-//   16 of 2,048 - 8,192, 8 KV heads                -      93 / 143  120 / 174  191 / 222
-//   64 of 300 - 1,500, 8 KV heads                  -      55 / 80   73 / 80   183 / 128
-constexpr int kFewCols = 96;
-
+//   columns                                        32      96      128-144    256-288
+//   8 sessions of 16,384 - 32,768, 2 KV heads   46 / 56  63 / 74   86 / 99   130 / 142
+//   16 of 2,048 - 8,192, 8 KV heads             78 / 114 114 / 121 131 / 124 199 / 228
+//   the same with 8-bit values                  55 / 125 102 / 136 119 / 140 191 / 253
+//   64 of 300 - 1,500, 8 KV heads               47 / 75  71 / 79   90 / 83   166 / 119
+constexpr int kFewCols = 128;
 // Parts that the tiles of a call may come to, and their arrivals' words.
 int most_parts(int n_cu) { return n_cu * (kWideCols / kFewTile); }
 size_t count_words(int n_cu) { return ((size_t)most_parts(n_cu) + 63) / 64 * 64; }
@@ -601,14 +601,18 @@ hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, 
     // are read past, many share what is in LDS.
     const int with_rows = std::min(dm.S, a.rows.n_rows);
     const bool few = exact || (int64_t)a.rows.n_rows * dm.G <= (int64_t)kFewCols * with_rows;
-    const RowsKernel k = few ? few_kernel(exact, keys8, values8)
-                             : RowsKernel{kernel_of<kWideWaves>(keys8, values8), kWideCols, 64 * kWideWaves};
     // the most tiles that rows can make, however they are spread over the sessions
-    const int64_t tiles = (int64_t)a.rows.n_rows * dm.G / k.cols + with_rows;
-    // Two workgroups of the narrow kernel fit a CU, one of the wide one.  Tiles
-    // that fill the card three times over are balanced as they are.
-    const int64_t units = few ? (tiles * dm.Hkv < 6 * n_cu ? 2 * n_cu : 0) : n_cu - tiles * dm.Hkv;
-    c.units = (int)std::max<int64_t>(0, units);
+    const int64_t tiles = (int64_t)a.rows.n_rows * dm.G / (few ? kFewTile : kWideCols) + with_rows;
+    const bool all = 2 * tiles * dm.Hkv <= n_cu;
+    const RowsKernel k = few ? few_kernel(all, exact, keys8, values8)
+                             : RowsKernel{kernel_of<kWideWaves>(keys8, values8), kWideCols, 64 * kWideWaves};
+    // Parts that are all on the card at once: one of eight waves a CU, or two of
+    // four of the narrow kernel, where tiles fill half the card and the next one's
+    // beginning hides behind another.  (5 rows over 8 sessions, 2 KV heads: 48 us
+    // with eight, whose parts are half as many to join, 55 with four.)  Tiles that
+    // fill the card three times over are balanced as they are.
+    c.units = few ? (tiles * dm.Hkv < 6 * n_cu ? (all ? 1 : 2) * n_cu : 0) : tiles * dm.Hkv < n_cu ? n_cu : 0;
+    c.least_units = few ? c.units / 2 : 0;
     c.count = static_cast<int32_t*>(a.workspace);
     c.part = static_cast<float*>(a.workspace) + count_words(n_cu);
     void* args[] = {&c};
