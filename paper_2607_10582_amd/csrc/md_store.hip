@@ -336,6 +336,28 @@ __global__ void __launch_bounds__(64 * kWaves) k_read_rows(RowCall c) {
     const int phys = __shfl(x.phys, m), sub = __shfl(x.sub, m), t = __shfl(x.t, m);
     const bool mine = __shfl(x.mine ? 1 : 0, m) != 0, in = __shfl(x.in ? 1 : 0, m) != 0;
     const int64_t at = (int64_t)(r0 + m) * c.stride + kv * kHeadDim + 8 * g;
+    // values, a block at a time, the first one's before the keys
+    uint32_t left = (uint32_t)__ballot(in) & 0xFFFFu;
+    bool here = false;
+    float v_scale = 1.0f;
+    u32x4 vw[CODES ? 2 : 4];
+    auto load_values = [&]() __attribute__((always_inline)) {
+        const int i = __ffs(left) - 1;
+        const int p = __builtin_amdgcn_readlane(phys, i), b = __builtin_amdgcn_readlane(sub, i);
+        here = in && phys == p && sub == b;
+        left &= ~(uint32_t)__ballot(here);
+        const size_t tile = tile_of(c, p, b, kv);
+        if constexpr (CODES) {
+            v_scale = c.values.v_scale[scale_at(c, p, b, kv)];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) vw[a] = *reinterpret_cast<const u32x4*>(c.values.v_codes + tile + 1024 * a + 16 * lane);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(c.values.v_pool + tile + 512 * j + 8 * lane);
+        }
+    };
+    bool more = c.v != nullptr && left != 0;
+    if (more) load_values();
     if (c.k != nullptr && mine) {
         const uint16_t* tile = c.k_pool + tile_of(c, phys, sub, kv);
         u32x4 w[4];
@@ -362,59 +384,47 @@ __global__ void __launch_bounds__(64 * kWaves) k_read_rows(RowCall c) {
             put8<F32>(c.k, at + 32 * j, y);
         }
     }
-    if (c.v != nullptr) {
-        uint16_t* const buf = turn[wv];
-        uint32_t left = (uint32_t)__ballot(in) & 0xFFFFu;
-        if (mine && !in) {
-            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c.v != nullptr && mine && !in) {
+        const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) put8<F32>(c.v, at + 32 * j, none);
-        }
-        while (left != 0) {
-            const int i = __ffs(left) - 1;
-            const int p = __builtin_amdgcn_readlane(phys, i), b = __builtin_amdgcn_readlane(sub, i);
-            const bool here = in && phys == p && sub == b;
-            left &= ~(uint32_t)__ballot(here);
-            const size_t tile = tile_of(c, p, b, kv);
-            float scale = 1.0f;
-            wave_lds();
-            if constexpr (CODES) {
-                scale = c.values.v_scale[scale_at(c, p, b, kv)];
-                u32x4 w[2];
+        for (int j = 0; j < 4; ++j) put8<F32>(c.v, at + 32 * j, none);
+    }
+    uint16_t* const buf = turn[wv];
+    while (more) {
+        wave_lds();
+        if constexpr (CODES) {
 #pragma unroll
-                for (int a = 0; a < 2; ++a) w[a] = *reinterpret_cast<const u32x4*>(c.values.v_codes + tile + 1024 * a + 16 * lane);
+            for (int a = 0; a < 2; ++a)
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {   // word e: tokens 4g .. of dim 64 a + 16 e + m
-                        const uint32_t lo = codes_pair_to_bf16<false>(w[a][e]), hi = codes_pair_to_bf16<true>(w[a][e]);
-                        uint16_t* to = buf + 4 * g * kPitch + 64 * a + 16 * e + m;
-                        to[0] = (uint16_t)lo;
-                        to[kPitch] = (uint16_t)(lo >> 16);
-                        to[2 * kPitch] = (uint16_t)hi;
-                        to[3 * kPitch] = (uint16_t)(hi >> 16);
-                    }
-            } else {
-                u32x4 w[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4*>(c.values.v_pool + tile + 512 * j + 8 * lane);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {   // words 0, 1: tokens 4g .. of dim 32 j + m; 2, 3: of 32 j + 16 + m
-                        uint16_t* to = buf + (4 * g + 2 * (e & 1)) * kPitch + 32 * j + 16 * (e >> 1) + m;
-                        to[0] = (uint16_t)w[j][e];
-                        to[kPitch] = (uint16_t)(w[j][e] >> 16);
-                    }
-            }
-            wave_lds();
-            if (here) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float y[8];
-                    widen8(*reinterpret_cast<const u32x4*>(buf + t * kPitch + 32 * j + 8 * g), scale, y);
-                    put8<F32>(c.v, at + 32 * j, y);
+                for (int e = 0; e < 4; ++e) {   // word e: tokens 4g .. of dim 64 a + 16 e + m
+                    const uint32_t lo = codes_pair_to_bf16<false>(vw[a][e]), hi = codes_pair_to_bf16<true>(vw[a][e]);
+                    uint16_t* to = buf + 4 * g * kPitch + 64 * a + 16 * e + m;
+                    to[0] = (uint16_t)lo;
+                    to[kPitch] = (uint16_t)(lo >> 16);
+                    to[2 * kPitch] = (uint16_t)hi;
+                    to[3 * kPitch] = (uint16_t)(hi >> 16);
                 }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {   // words 0, 1: tokens 4g .. of dim 32 j + m; 2, 3: of 32 j + 16 + m
+                    uint16_t* to = buf + (4 * g + 2 * (e & 1)) * kPitch + 32 * j + 16 * (e >> 1) + m;
+                    to[0] = (uint16_t)vw[j][e];
+                    to[kPitch] = (uint16_t)(vw[j][e] >> 16);
+                }
+        }
+        wave_lds();
+        const bool mine_now = here;
+        const float scale = v_scale;
+        more = left != 0;
+        if (more) load_values();
+        if (mine_now) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float y[8];
+                widen8(*reinterpret_cast<const u32x4*>(buf + t * kPitch + 32 * j + 8 * g), scale, y);
+                put8<F32>(c.v, at + 32 * j, y);
             }
         }
     }
