@@ -119,9 +119,8 @@ struct TileAt {
 
 // The parts are of one size over all sessions, so that a session three times as
 // long as another has three times as many and all end together (cut into the same
-// number, a call on 16 sessions of 2,048 to 8,192 tokens, 8 rows, 8-bit values
-// took 58 us instead of 55, one on 8 of 16,384 to 32,768, 16 rows, 102 instead of
-// 66).  A group is 8
+// number, 16 sessions of 2,048 to 8,192 tokens, 16 rows of 4 columns, 8-bit values
+// took 92 us instead of 76).  A group is 8
 // blocks; a part has at least kLeastGroups, what joining it costs.
 constexpr int kGroup = 128, kLeastGroups = 4;
 

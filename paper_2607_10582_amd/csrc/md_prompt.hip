@@ -19,7 +19,7 @@
 //
 // What bounds it: the matrix cores, 4 d operations per column and token.  They
 // are busy for 84% of the time that a large library product takes for as many
-// operations: a prompt of 16,384 rows (32 query heads on 8) takes 1.08 ms,
+// operations: a prompt of 16,384 rows (16 query heads on 2) takes 1.08 ms,
 // 1,020 TFLOP/s.  Without the weights it would take 0.89 ms, without the loads
 // 1.02.
 
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     auto bits = [](uint64_t of_blocks, int i) { return (uint32_t)(of_blocks >> (4 * i)) & 15u; };
 
     // ---- a step's loads, and their way into LDS
-    // thread tid takes 16 bytes of block 4 x / kPer ..: a block is 256 such pieces, of codes 128
+    // a thread's piece x is 16 bytes of the block (x W + its wave) / 4 (codes: / 2)
     u32x4 rk[kPer], rv[V8 ? (kPer + 1) / 2 : kPer];
     constexpr int kVals = V8 ? (kPer + 1) / 2 : kPer;
     // Where the thread's pieces go, once for all steps (kept as they are: taken

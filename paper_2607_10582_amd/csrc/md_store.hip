@@ -4,7 +4,11 @@
 //   scale = max |v| / 448 over a block of 16 tokens and KV head,  code = e4m3(v / scale)
 //
 // Each moves a value once and turns it by a few operations, so long calls are
-// bound by HBM, and a decode step's by the launch and its chain of loads.
+// bound by HBM, and a decode step's by the launch and its chain of loads
+// (sessions' bounds, slot, page, bytes).  Rows in: 4 x 8,192 of two KV heads, 13.8
+// us, 4.2 TB/s of reads and writes; 64 uneven chunks, 14.  Rows out: 16 x 32,768
+// into float32, 311 us, 4.4 TB/s (a copy of 4 GiB runs at 4.8); 32 x 1,700, 25.9
+// us.  The values of a decode step of 32 sessions, 36 layers: 6.0 us from Python.
 
 #include "md_decode.h"
 #include "md_device.h"
@@ -336,7 +340,8 @@ __global__ void __launch_bounds__(64 * kWaves) k_read_rows(RowCall c) {
     const int phys = __shfl(x.phys, m), sub = __shfl(x.sub, m), t = __shfl(x.t, m);
     const bool mine = __shfl(x.mine ? 1 : 0, m) != 0, in = __shfl(x.in ? 1 : 0, m) != 0;
     const int64_t at = (int64_t)(r0 + m) * c.stride + kv * kHeadDim + 8 * g;
-    // values, a block at a time, the first one's before the keys
+    // values, a block at a time, the first one's requested before the keys (behind
+    // them: 322 us for 311, 16 x 32,768 rows into float32)
     uint32_t left = (uint32_t)__ballot(in) & 0xFFFFu;
     bool here = false;
     float v_scale = 1.0f;
