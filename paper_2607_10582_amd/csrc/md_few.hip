@@ -212,8 +212,9 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
             lg[b] = 0.0f;
             lost[b] = false;
             if constexpr (V8) {
-                lost[b] = !(vs[b] < INFINITY);
-                if (vs[b] == 0.0f || (TERMS == 1 && lost[b])) vs[b] = 1.0f;   // (0: all its values are)
+                if (vs[b] == 0.0f) vs[b] = 1.0f;   // (all its values are 0)
+                lost[b] = !scale_fits(vs[b]);
+                if (lost[b]) vs[b] = 1.0f;
                 rs[b] = 1.0f / vs[b];
                 lg[b] = log2f(vs[b]);
             }
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
             }
             l = fmaf(sum, TERMS == 1 ? rs[b] : 1.0f, l);
             lw = fmaf(wsum, rs[b], lw);
-            if (TERMS == 1 && lost[b] && sum > 0.0f) lw = __uint_as_float(0x7FC00000u);   // (settled at the end)
+            if (lost[b] && sum > 0.0f) lw = __uint_as_float(0x7FC00000u);   // (settled at the end)
         }
 #pragma unroll
         for (int y = 0; y < 8; ++y) {   // block y / 4, dims 32 (y % 4) ..
@@ -287,7 +288,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
         __builtin_amdgcn_wave_barrier();
     }
     l = add_halves(l);
-    lw = TERMS == 1 ? add_halves(lw) : l;
+    lw = add_halves(lw);
+    if (TERMS != 1) lw += l;   // (0, or NaN)
     // ---- columns that a value reached which is not finite and which they do not see
     {
         float z = lw * 0.0f;

@@ -308,6 +308,11 @@ __device__ __forceinline__ int64_t lane_tile(const Block& b, int i) {
                      ((uint64_t)(uint32_t)lane_int((int)(b.tile >> 32), i) << 32));
 }
 
+// Whether a scale of values can go through the weights' exponents and out of
+// their sums again, with room for weights from 2^-30 to 2^8.  A column that sees
+// values with another (or none: NaN) is summed again.
+__device__ __forceinline__ bool scale_fits(float s) { return s > 0x1p-96f && s < 0x1p96f; }
+
 // One column's sum of weighted values again, token by token (dims e and e + 1,
 // e = 2 lane), from `count` blocks of which describe(k) tells 64 lanes: for
 // values that are not finite, which reach, as 0 times them, the columns of their

@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     // the weights (through the exponent where those are rounded to bf16 anyway)
     // and out of their sums again.
     float sc[2], vs[2], rs[2], lg[2], shift[2];
-    bool lost[2] = {false, false};   // values that are not numbers
+    bool lost[2] = {false, false};   // values whose scale is not taken so
     float mx;
     // A half's scales, what its columns see of it and their maxima: whether one
     // has grown enough to be followed.  i: the step's place in the lot.
@@ -260,8 +260,9 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
             }
             if constexpr (V8) {
                 vs[b] = __uint_as_float(of(cur.vs, i0 + b));
-                lost[b] = !(vs[b] < INFINITY);
-                if (vs[b] == 0.0f || lost[b]) vs[b] = 1.0f;   // (0: all its values are)
+                if (vs[b] == 0.0f) vs[b] = 1.0f;   // (all its values are 0)
+                lost[b] = !scale_fits(vs[b]);
+                if (lost[b]) vs[b] = 1.0f;
                 rs[b] = __builtin_amdgcn_rcpf(vs[b]);
                 lg[b] = log2f(vs[b]);
             }

@@ -452,7 +452,7 @@ def test_token_values_that_are_not_finite_outside_the_window():
 
 # ---------------------------------------------------------------- ragged rows
 
-def check_rows(w, layer, q, out, lse, start, slot, window=0, sinks=0, some=None):
+def check_rows(w, layer, q, out, lse, start, slot, window=0, sinks=0, some=None, least=0.0):
     rounded = q.dtype == BF16 and out.dtype == BF16
     session = np.repeat(np.arange(w.S), np.diff(start))
     pick = range(len(slot)) if some is None else some
@@ -470,11 +470,11 @@ def check_rows(w, layer, q, out, lse, start, slot, window=0, sinks=0, some=None)
             if not bool(seen.any()):
                 assert torch.equal(got, ref) and torch.equal(gl, rl), (r, kv)
                 continue
-            assert bool(((got - ref).abs() <= tol).all()), (r, s, slot[r], kv, float(((got - ref).abs() - tol).max()))
+            assert bool(((got - ref).abs() <= tol + least).all()), (r, s, slot[r], kv, float(((got - ref).abs() - tol).max()))
             assert bool(((gl - rl).abs() <= ltol).all()), (r, s, slot[r], kv, float((gl - rl).abs().max()))
 
 
-def run_rows(w, counts, first=None, layer=None, q_type=BF16, out_type=BF16, most=60, slots=True, scale=1.5, **kw):
+def run_rows(w, counts, first=None, layer=None, q_type=BF16, out_type=BF16, most=60, slots=True, scale=1.5, least=0.0, **kw):
     layer = w.L - 1 if layer is None else layer
     start_d, slot_d, start, slot = w.rows(counts, first)
     n = len(slot)
@@ -486,7 +486,7 @@ def run_rows(w, counts, first=None, layer=None, q_type=BF16, out_type=BF16, most
     assert w.md.device_status() == 0
     assert (out[n:] == 5.0).all()
     some = None if n <= most else sorted({0, n - 1} | set(np.random.default_rng(n).choice(n, most, replace=False).tolist()))
-    check_rows(w, layer, q, out[:n], lse, start, slot, some=some, **kw)
+    check_rows(w, layer, q, out[:n], lse, start, slot, some=some, least=least, **kw)
     return q, out[:n], lse, start_d, slot_d
 
 
@@ -630,6 +630,25 @@ def test_values_that_are_not_finite_reach_only_rows_that_see_them(many, coded, t
         check_rows(w, 0, q, out, lse, start, slot, some=[r for r in range(len(slot)) if not sees_bad[r]], **kw)
         for r in range(len(slot)):
             assert bool(out[r].isfinite().all()) != sees_bad[r], (r, slot[r])
+
+
+@pytest.mark.parametrize("types", TYPES[:2], ids=["bf16", "f32"])
+@pytest.mark.parametrize("power", [-122, -60, 60, 110])
+@pytest.mark.parametrize("some", [True, False])
+def test_scales_of_any_size(some, power, types):
+    """Scales of 8-bit values that are far from 1, of all blocks or of one."""
+    say("[scales]", some, power, types)
+    w = World(1, 4, 2, 16, [330, 40], seed=61)
+    for s in range(2):
+        blocks = [1] if some else range(len(w.ids[s]))
+        for b in blocks:
+            scale = w.cache.v_scale[int(w.ids[s][b])]   # [L][Hkv][1]
+            before = scale.cpu().double()
+            scale *= 2.0 ** power
+            w.v[s][16 * b:16 * b + 16] *= scale.cpu().double() / before   # (a small one loses bits)
+    # (results below 2^-126 are multiples of 2^-133 in bf16: off by at most half of it)
+    run_rows(w, [330, 40], q_type=types[0], out_type=types[1], least=2.0 ** -134)
+    run_rows(w, [3, 2], q_type=types[0], out_type=types[1], window=30, sinks=20, least=2.0 ** -134)
 
 
 def test_keys_that_are_not_finite_and_nan_queries_stay_where_they_are_seen():
