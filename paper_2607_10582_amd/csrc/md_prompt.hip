@@ -548,7 +548,13 @@ constexpr int kWideCols = kWideWaves * 32;   // columns of its tile
 //   16 of 2,048 - 8,192, 8 KV heads             78 / 114 114 / 121 131 / 124 199 / 228
 //   the same with 8-bit values                  55 / 125 102 / 136 119 / 140 191 / 253
 //   64 of 300 - 1,500, 8 KV heads               47 / 75  71 / 79   90 / 83   166 / 119
-constexpr int kFewCols = 128;
+// One session is few tiles for the wide kernel, and up to 2,048 columns go to the
+// narrow one: 1 of 16,384 tokens, 2 KV heads, 384 columns 32 / 106, 1,536 68 / 104,
+// 3,072 116 / 116, 6,144 200 / 156; 8,192 tokens, 8 KV heads, 2,048 columns 111 / 118,
+// 8,192 384 / 284.  (Only the device knows the rows of each session: a long prompt
+// beside many sessions without a row is taken for few rows of each, 942 for 700
+// us with 8,192 rows of it.)
+constexpr int kFewCols = 128, kFewAll = 2048;
 // Parts that the tiles of a call may come to, and their arrivals' words.
 int most_parts(int n_cu) { return n_cu * (kWideCols / kFewTile); }
 size_t count_words(int n_cu) { return ((size_t)most_parts(n_cu) + 63) / 64 * 64; }
@@ -601,7 +607,7 @@ hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, 
     // Few columns a session (on average: only the device knows the rows of each)
     // are read past, many share what is in LDS.
     const int with_rows = std::min(dm.S, a.rows.n_rows);
-    const bool few = exact || (int64_t)a.rows.n_rows * dm.G <= (int64_t)kFewCols * with_rows;
+    const bool few = exact || (int64_t)a.rows.n_rows * dm.G <= std::max<int64_t>((int64_t)kFewCols * with_rows, kFewAll);
     // the most tiles that rows can make, however they are spread over the sessions
     const int64_t tiles = (int64_t)a.rows.n_rows * dm.G / (few ? kFewTile : kWideCols) + with_rows;
     const bool all = 2 * tiles * dm.Hkv <= n_cu;

@@ -733,6 +733,160 @@ def test_strided_rows_and_untouched_neighbours():
         assert torch.equal(plain.view(80, 4, D), out[:, 1])
 
 
+# ---- The same where there are many columns (more than 2,048, and more than 128
+# a session): bf16 rows then take the kernel of 256 columns a workgroup.
+
+@pytest.mark.parametrize("coded", [True, False])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 200), (16, 0), (17, 16), (64, 4), (129, 70), (5000, 1), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_many_columns_windows(window, sinks, coded):
+    say("[columns window]", window, sinks, coded)
+    w = World(1, 16, 1, 16, [700, 3, 64, 0, 33], seed=81, coded=coded)
+    run_rows(w, [400, 3, 64, 0, 20], window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("shape", [(1, 16, 1), (2, 32, 2), (1, 14, 2), (1, 32, 8)])
+def test_many_columns_head_layouts(shape):
+    w = World(*shape, 64, [520, 0, 1, 290], seed=82, quant=0.5)
+    run_rows(w, [520, 0, 1, 290])
+
+
+@pytest.mark.parametrize("power", [-122, -60, 60, 110])
+@pytest.mark.parametrize("some", [True, False])
+def test_many_columns_scales(some, power):
+    say("[columns scales]", some, power)
+    w = World(1, 16, 1, 16, [330, 40], seed=83)
+    for s in range(2):
+        for b in [1] if some else range(len(w.ids[s])):
+            scale = w.cache.v_scale[int(w.ids[s][b])]
+            before = scale.cpu().double()
+            scale *= 2.0 ** power
+            w.v[s][16 * b:16 * b + 16] *= scale.cpu().double() / before
+    run_rows(w, [330, 40], least=2.0 ** -134)
+
+
+@pytest.mark.parametrize("coded", [True, False])
+def test_many_columns_values_that_are_not_finite(coded):
+    w = World(1, 16, 1, 16, [200], seed=84, coded=coded, quant=0.5)
+    for t in [150] if coded else [33, 150]:
+        page = int(w.ids[0][t // 16])
+        if coded:
+            w.cache.v_scale[page] = math.nan
+            w.v[0][t // 16 * 16:t // 16 * 16 + 16] = math.nan
+        else:
+            y = PagedCache.from_value_layout(w.cache.v_pool[page:page + 1]).contiguous()
+            y[0, t % 16] = w.v[0][t] = math.inf if t == 33 else math.nan
+            w.cache.v_pool[page:page + 1] = PagedCache.to_value_layout(y)
+    start_d, slot_d, start, slot = w.rows([200])
+    q = w.normal(200, 16, D).to(BF16)
+    for kw in (dict(), dict(window=20, sinks=2)):
+        out, lse = torch.zeros((200, 16, D), dtype=BF16, device=w.dev), torch.zeros((200, 16), device=w.dev)
+        w.md.attend_rows(0, q, out, start_d, lse=lse, **kw)
+        bad = ~w.v[0][:, 0, 0].isfinite().all(1)
+        sees_bad = [bool((visible(w.live[0], t, kw.get("window", 0), kw.get("sinks", 0)) & bad).any()) for t in slot]
+        check_rows(w, 0, q, out, lse, start, slot, some=[r for r in range(200) if not sees_bad[r]][::3], **kw)
+        for r in range(200):
+            assert bool(out[r].isfinite().all()) != sees_bad[r], (r, slot[r])
+
+
+def test_many_columns_keys_that_are_not_finite():
+    w = World(1, 16, 1, 16, [200], seed=85, coded=False)
+    page = int(w.ids[0][4])
+    y = PagedCache.from_pool_layout(w.cache.k_pool[page:page + 1]).contiguous()
+    y[0, 6] = math.nan
+    w.cache.k_pool[page:page + 1] = PagedCache.to_pool_layout(y)
+    w.k[0][70] = math.nan
+    start_d, slot_d, start, slot = w.rows([200])
+    q = w.normal(200, 16, D).to(BF16)
+    q[20, 1, 5] = math.nan
+    out, lse = torch.zeros((200, 16, D), dtype=BF16, device=w.dev), torch.zeros((200, 16), device=w.dev)
+    w.md.attend_rows(0, q, out, start_d, lse=lse)
+    assert out[20, 1].isnan().all() and lse[20, 1].isnan() and out[20, 0].isfinite().all()
+    assert out[70:].isnan().all()
+    check_rows(w, 0, q, out, lse, start, slot, some=[r for r in range(70) if r != 20])
+
+
+@pytest.mark.parametrize("grow", [0.002, 0.05, 0.5])
+def test_many_columns_growing_logits(grow):
+    w = World(1, 16, 1, 16, [600], seed=86, coded=False)
+    ramp = torch.arange(600, dtype=torch.float64)[:, None, None, None] * grow
+    w.k[0] = (w.k[0] * 0.05 + ramp / math.sqrt(D)).float().to(BF16).double()
+    ids = torch.as_tensor(w.ids[0], device=w.dev)
+    full = torch.zeros((len(ids) * 16, 1, 1, D), dtype=BF16, device=w.dev)
+    full[:600] = w.k[0].to(BF16).to(w.dev)
+    w.cache.k_pool[ids] = PagedCache.to_pool_layout(full.view(-1, 16, 1, 1, D))
+    start_d, slot_d, start, slot = w.rows([600])
+    q = torch.ones((600, 16, D), dtype=BF16, device=w.dev)
+    q[:, 1::2] *= -1
+    out, lse = torch.empty_like(q), torch.empty((600, 16), device=w.dev)
+    w.md.attend_rows(0, q, out, start_d, lse=lse)
+    check_rows(w, 0, q, out, lse, start, slot, some=list(range(0, 600, 23)))
+
+
+def test_many_columns_rows_that_do_not_count():
+    """Rows of nobody, of slots that are not there, of sessions that make no sense."""
+    w = World(1, 16, 1, 16, [300, 5, 40, 40], seed=87)
+    w.cache.n_tokens[2] = 4000
+    n = 260
+    start = w.i32([1, 200, 203, 223, 243])
+    slot = np.concatenate([[0], np.arange(100, 299), [-1, 5, 4], np.arange(20), np.arange(20), np.zeros(17, np.int64)])
+    q = w.normal(n, 16, D).to(BF16)
+    out, lse = torch.full((n, 16, D), 5.0, dtype=BF16, device=w.dev), torch.full((n, 16), 5.0, device=w.dev)
+    w.md.attend_rows(0, q, out, start, row_slot=w.i32(slot.tolist()), lse=lse)
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW | B.MD_DEV_CORRUPT
+    none = [i for i in range(n) if bool((out[i] == 0).all() and (lse[i] == -math.inf).all())]
+    left = [i for i in range(n) if bool((out[i] == 5).all() and (lse[i] == 5).all())]
+    assert none == [200, 201] + list(range(203, 223)) and left == [0] + list(range(243, 260))
+    rows = list(range(1, 200, 9)) + [202] + list(range(223, 243, 5))
+    check_rows(w, 0, q[1:243], out[1:243], lse[1:243], np.array([0, 199, 202, 222, 242]), slot[1:243], some=[r - 1 for r in rows])
+
+
+def test_many_columns_strided_rows():
+    w = World(2, 32, 2, 16, [200, 30], seed=88)
+    start_d, slot_d, start, slot = w.rows([140, 30])
+    q = torch.full((170, 3, 32, D), math.nan, dtype=BF16, device=w.dev)
+    q[:, 1] = w.normal(170, 32, D).to(BF16)
+    out = torch.full((170, 3, 32, D), 5.0, dtype=BF16, device=w.dev)
+    lse = torch.zeros((170, 32), device=w.dev)
+    w.md.attend_rows(1, q[:, 1], out[:, 1], start_d, lse=lse)
+    check_rows(w, 1, q[:, 1], out[:, 1], lse, start, slot, some=range(0, 170, 11))
+    assert (out[:, 0] == 5).all() and (out[:, 2] == 5).all()
+
+
+def test_many_columns_replayed_between_few():
+    """One work space for both kernels and their parts, captured and replayed."""
+    side = torch.cuda.Stream()
+    w = World(1, 16, 1, 16, [3000, 1100], seed=89, stream=side)
+    many, few = w.rows([200, 100]), w.rows([5, 2])
+    qs = [w.normal(n, 16, D).to(BF16) for n in (300, 7)]
+    outs = [torch.zeros_like(q) for q in qs]
+    torch.cuda.synchronize()
+
+    def calls():
+        w.md.attend_rows(0, qs[0], outs[0], many[0], row_slot=many[1])
+        w.md.attend_rows(0, qs[1], outs[1], few[0], row_slot=few[1], window=1500, sinks=3)
+
+    calls()
+    torch.cuda.synchronize()
+    want = [o.clone() for o in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for _ in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    lse = torch.zeros((300, 16), device=w.dev)
+    w.md.attend_rows(0, qs[0], outs[0], many[0], row_slot=many[1], lse=lse)
+    torch.cuda.synchronize()
+    check_rows(w, 0, qs[0], outs[0], lse, many[2], many[3], some=range(0, 300, 29))
+
+
 # ---------------------------------------------------------------- together
 
 def test_two_handles_and_another_stream():
