@@ -889,6 +889,33 @@ def test_many_columns_replayed_between_few():
 
 # ---------------------------------------------------------------- together
 
+@pytest.mark.parametrize("coded", [True, False])
+def test_pools_past_32_bits(coded):
+    """Pages whose keys and values lie more than 2^32 elements into the pools."""
+    say("[large pools]", coded)
+    w = World(1, 32, 2, 16, [300, 40], seed=91, coded=coded, fill=False, spare=800000)
+    assert max(int(i) for ids in w.ids for i in ids) * 2 * 16 * D > 2 ** 32
+    start_d, slot_d, start, slot = w.rows([300, 40])
+    k, v = kv_rows(w, start, slot, 0)
+    w.md.write_rows(0, start_d, k, v, row_slot=slot_d)
+    back = [torch.zeros((340, 2, D), device=w.dev) for _ in "kv"]
+    w.md.read_rows(0, start_d, *back, row_slot=slot_d)
+    torch.cuda.synchronize()
+    session = np.repeat([0, 1], [300, 40])
+    assert torch.equal(back[0], k.float())
+    want = torch.stack([w.v[s][t, 0] for s, t in zip(session, slot)])
+    assert torch.equal(back[1].cpu(), want.float())   # (codes: the product of scale and code, rounded once)
+    run_rows(w, [300, 40], most=20)
+    run_rows(w, [4, 3], window=100, sinks=20)
+    q, out = w.normal(2, 32, D), torch.zeros((2, 32, D), device=w.dev)
+    w.md.attend(0, q, out)
+    rows = torch.zeros((2, 32, D), device=w.dev)
+    w.md.attend_rows(0, q, rows, w.i32([0, 1, 2]))
+    torch.cuda.synchronize()
+    assert w.md.device_status() == 0
+    assert float((out - rows).abs().max()) < 1e-4
+
+
 def test_two_handles_and_another_stream():
     """Calls on a handle's own stream, whatever stream is current."""
     side = torch.cuda.Stream()
