@@ -44,7 +44,9 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
     int status = 0;
     TileAt t;
     if (!find_tile<kThreads, kFewTile>(c, scan_lds, pref, t, status)) return;
-    // ---- the columns, the same for every wave, and their queries
+    // ---- the columns, the same for every wave, and their queries (asked for before
+    // the first keys and values: behind them their wait is one for those too, 50 us
+    // for 48.5 in the case above)
     const Column col = column_of(c, t, t.col + n, status);
     u32x4* const q_lds = reinterpret_cast<u32x4*>(lds);   // [TERMS][8][64]
 #pragma unroll

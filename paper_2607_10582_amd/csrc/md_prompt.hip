@@ -550,7 +550,7 @@ constexpr int kWideCols = kWideWaves * 32;   // columns of its tile
 //   64 of 300 - 1,500, 8 KV heads               47 / 75  71 / 79   90 / 83   166 / 119
 // One session is few tiles for the wide kernel, and up to 2,048 columns go to the
 // narrow one: 1 of 16,384 tokens, 2 KV heads, 384 columns 32 / 106, 1,536 68 / 104,
-// 3,072 116 / 116, 6,144 200 / 156; 8,192 tokens, 8 KV heads, 2,048 columns 111 / 118,
+// 6,144 200 / 156; 8,192 tokens, 8 KV heads, 2,048 columns 111 / 118,
 // 8,192 384 / 284.  (Only the device knows the rows of each session: a long prompt
 // beside many sessions without a row is taken for few rows of each, 942 for 700
 // us with 8,192 rows of it.)
