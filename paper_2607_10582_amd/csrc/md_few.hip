@@ -292,6 +292,16 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
     l = add_halves(l);
     lw = add_halves(lw);
     if (TERMS != 1) lw += l;   // (0, or NaN)
+    // A column without a row, or whose row's slot is not there, saw what its
+    // neighbours see in full all the same; it has nothing.
+    if (col.own < 0) {
+        m = -INFINITY;
+        l = lw = 0.0f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    }
     // ---- columns that a value reached which is not finite and which they do not see
     {
         float z = lw * 0.0f;
@@ -300,7 +310,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
             for (int i = 0; i < 16; ++i) z = fmaf(o[d][i], 0.0f, z);
         z = add_halves(z);
-        uint32_t bad = (uint32_t)__ballot(col.mine && col.own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
+        uint32_t bad = (uint32_t)__ballot(col.own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
         float* const y_lds = reinterpret_cast<float*>(v_lds);
         while (bad != 0) {
             const int who = __ffs(bad) - 1;

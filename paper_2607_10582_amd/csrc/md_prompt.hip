@@ -466,6 +466,16 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
     const int head = x_col.head;
     l = add_halves(l);
     lw = add_halves(lw);
+    // A column without a row, or whose row's slot is not there, saw what its
+    // neighbours see in full all the same; it has nothing.
+    if (own < 0) {
+        m = -INFINITY;
+        l = lw = 0.0f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    }
     // ---- Columns with a finite sum and a result that is not: a value that is
     // not finite reached them unseen (here, where it costs nothing else)
     {
@@ -475,7 +485,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
 #pragma unroll
             for (int i = 0; i < 16; ++i) z = fmaf(o[d][i], 0.0f, z);
         z = add_halves(z);
-        uint32_t bad = (uint32_t)__ballot(mine && own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
+        uint32_t bad = (uint32_t)__ballot(own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
         float* const y_lds = reinterpret_cast<float*>(kl[0]) + kHeadDim * wv;
         while (bad != 0) {
             const int who = __ffs(bad) - 1;
