@@ -744,8 +744,12 @@ md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v
 
 /*
  * md_write_rows — keys and values of ragged rows of one layer into the pools.
- * The slots of a session's rows ascend; a row that is not above the one
- * before it, or whose page holds 8-bit keys, does not count (MD_DEV_BAD_ROW).
+ * Rows whose slot is not the session's are passed over, wherever they lie
+ * among the others (MD_DEV_BAD_ROW).  The slots of the others ascend; where
+ * they do not, a row that is not above those before it is left out, and others
+ * of its session may be with it (MD_DEV_BAD_ROW; no slot is written twice, and
+ * the same rows every time).  A row whose page holds 8-bit keys does not count
+ * (MD_DEV_BAD_ROW).
  * In the 8-bit pool a session's rows go on in one block after another: the
  * slots of a block behind the last row written to it get the code 0.
  * MD_E_UNSUPPORTED with an offload tier.

@@ -86,7 +86,7 @@ __device__ __forceinline__ void wave_lds() {
 // What the wave's row `lane & 31` of rows r0 .. r0 + 31 is.
 struct Span {
     int s, lo, hi, nt; // its session, that session's rows and slots in use
-    int slot, prev;    // its slot, and that of the session's row before it
+    int slot, prev;    // its slot, and that of the session's row before it (-1: its first)
     int phys, sub, t;  // page, block of it and token of the block
     bool mine;         // it is some session's row
     bool in;           // and its slot holds a token's place
@@ -117,7 +117,6 @@ __device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
     broken = __any(broken);
     if (broken) status |= MD_DEV_BAD_ROW;
     x.mine = !broken && s < c.S && x.lo <= r && r < x.hi;
-    x.prev = -1;
     if (!x.mine) return x;
     const int np = c.n_pages[x.s], nt = c.n_tokens[x.s];
     const bool ok = np == 0 ? nt == 0 : np > 0 && np <= c.MP && nt > (np - 1) * c.P && nt <= np * c.P;
@@ -127,7 +126,7 @@ __device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
     }
     x.nt = nt;
     x.slot = c.row_slot != nullptr ? c.row_slot[r] : nt - (x.hi - r);
-    if (r > x.lo) x.prev = c.row_slot != nullptr ? c.row_slot[r - 1] : x.slot - 1;
+    x.prev = r <= x.lo ? -1 : c.row_slot != nullptr ? c.row_slot[r - 1] : x.slot - 1;
     x.in = x.slot >= 0 && x.slot < nt;
     if (!x.in) {
         status |= MD_DEV_BAD_ROW;
@@ -151,12 +150,80 @@ __device__ __forceinline__ size_t scale_at(const RowCall& c, int phys, int sub, 
     return (((size_t)phys * c.L + c.layer) * c.Hkv + kv) * (size_t)(c.P >> 4) + sub;
 }
 
+// A session's rows lo .. hi - 1, some of whose slots may not be there (outside
+// of 0 .. nt - 1): these are passed over.  All of a wave call these together.
+struct SessionRows {
+    const int32_t* row_slot;
+    int lo, hi, nt;
+    __device__ __forceinline__ int slot(int r) const { return row_slot != nullptr ? row_slot[r] : nt - (hi - r); }
+    __device__ __forceinline__ bool there(int slot) const { return slot >= 0 && slot < nt; }
+
+    // The first of rows a .. b - 1 that is there and whose slot is not below
+    // `least`; b if there is none.  256 rows a round trip.
+    __device__ __forceinline__ int first_from(int a, int b, int least) const {
+        for (int q = a; q < b; q += 256) {
+            int x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = q + 64 * k + lane_id();
+                x[k] = r < b ? slot(r) : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t found = __ballot(there(x[k]) && x[k] >= least);
+                if (found != 0) return q + 64 * k + __ffsll((unsigned long long)found) - 1;
+            }
+        }
+        return b;
+    }
+
+    // The same over all rows, of those that ascend: by 64 probes at a time.
+    // The answer depends on the rows and on `least` alone, whatever the rows are.
+    __device__ __forceinline__ int search(int least) const {
+        int a = lo, b = hi;
+        while (b - a > 256) {
+            const int at = a + (int)((int64_t)(b - a) * lane_id() / 64), x = slot(at);
+            const uint64_t above = __ballot(there(x) && x >= least);
+            const int k = above != 0 ? __ffsll((unsigned long long)above) - 1 : 64;
+            const uint64_t below = __ballot(there(x) && x < least) & (k < 64 ? (1ull << k) - 1ull : ~0ull);
+            const int end = k < 64 ? __builtin_amdgcn_readlane(at, k) : b;
+            const int begin = below != 0 ? __builtin_amdgcn_readlane(at, 63 - __clzll(below)) + 1 : a;
+            const bool little = end - begin > (b - a) / 2;   // (the probes are not there)
+            a = begin;
+            b = end;
+            if (little) break;
+        }
+        return first_from(a, b, least);
+    }
+
+    // The rows of the last block that rows up to `end` (not itself) reach: lane
+    // m's is that of token m, or -1; `base`: its first slot (-1: no row is there).
+    __device__ __forceinline__ int last_block(int end, int& base) const {
+        int from = -1;
+        base = -1;
+        for (int q = end; q > lo; q -= 64) {
+            const int r = q - 1 - lane_id(), x = r >= lo ? slot(r) : -1;
+            uint64_t in = __ballot(there(x));
+            while (in != 0) {
+                const int i = __ffsll((unsigned long long)in) - 1, at = __builtin_amdgcn_readlane(x, i);
+                in &= in - 1;
+                if (base < 0) base = at & ~15;
+                if ((at & ~15) != base) return from;
+                if (from < 0 && (at & 15) == (lane_id() & 15)) from = q - 1 - i;
+            }
+        }
+        return from;
+    }
+};
+
 // A wave takes 16 rows and one KV head: the groups of rows that begin among
-// them, each the rows of one block (up to 15 of them behind the 16).  A block
-// has one group, the one that a search of the session's rows for the block's
-// first slot finds, so that no two waves write a block even where the slots do
-// not ascend.  Keys go as they come, 1 KiB of a block at a time; values turn in
-// LDS, from rows of dims to dims of four tokens.
+// them, each the rows of one block.  A block has one group, whose first row is
+// the one that a search of the session's rows for the block's first slot finds,
+// so that no two waves write a block even where the slots do not ascend; rows
+// whose slots are not there may lie anywhere between (the search by halves
+// gives way to one that passes over them where it meets one).  Keys go as they
+// come, 1 KiB of a block at a time; values turn in LDS, from rows of dims to
+// dims of four tokens.
 template <bool CODES>
 __global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
     __shared__ __align__(16) uint16_t turn[kWaves][16 * kPitch];
@@ -167,56 +234,98 @@ __global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
     int status = 0;
     const Span x = span_of(c, r0, status);
     const int r = r0 + (lane & 31);
-    bool counts = x.in;
-    if (counts && r > x.lo && x.slot <= x.prev) {
-        status |= MD_DEV_BAD_ROW;
-        counts = false;
+    // the slot of the session's row before it that is there, as far as these 32 rows
+    // and the one in front of them tell (below 0: none)
+    int prev = x.prev;
+    if (__builtin_expect(__any(x.in && r > x.lo && (prev < 0 || prev >= x.nt)), 0)) {
+        const uint32_t below = (uint32_t)__ballot(x.in) & ((1u << (lane & 31)) - 1u);
+        const int j = below != 0 ? 31 - __clz(below) : 0;
+        const int slot = __shfl(x.slot, j), s = __shfl(x.s, j), front = __builtin_amdgcn_readlane(x.prev, 0);
+        prev = below != 0 && s == x.s ? slot : r0 > x.lo && front < x.nt ? front : -1;
     }
-    const bool goes_on = counts && r > x.lo && (x.prev >> 4) == (x.slot >> 4);
-    bool leads = counts && !goes_on && (lane & 31) < 16 && lane < 32;
+    const bool ascends = x.in && x.slot > prev;
+    if (x.in && !ascends) status |= MD_DEV_BAD_ROW;
+    bool leads = ascends && lane < 16 && (prev >> 4) != (x.slot >> 4);   // (below 0 is no block)
+    bool odd = false;   // a row that is not there came into the search's way
     if (leads && c.row_slot != nullptr) {   // the first row that is not below the block
         int lo = x.lo, hi = x.hi;
-        while (lo < hi) {
-            const int mid = lo + (hi - lo) / 2;
-            if (c.row_slot[mid] < (x.slot & ~15)) lo = mid + 1; else hi = mid;
+        while (lo < hi && !odd) {
+            const int mid = lo + (hi - lo) / 2, slot = c.row_slot[mid];
+            odd = slot < 0 || slot >= x.nt;
+            if (slot < (x.slot & ~15)) lo = mid + 1; else hi = mid;
         }
-        leads = lo == r;
+        leads = !odd && lo == r;
     }
-    const bool coded = c.quant && counts && c.page_format[x.phys] != 0;
+    auto rows_of = [&](int i) {   // of lane i's session
+        return SessionRows{c.row_slot, __builtin_amdgcn_readlane(x.lo, i), __builtin_amdgcn_readlane(x.hi, i),
+                           __builtin_amdgcn_readlane(x.nt, i)};
+    };
+    for (uint64_t left = __ballot(odd); __builtin_expect(left != 0, 0); left &= left - 1) {
+        const int i = __ffsll((unsigned long long)left) - 1;
+        if (rows_of(i).search(__builtin_amdgcn_readlane(x.slot, i) & ~15) == r0 + i && lane == i) leads = true;
+    }
+    const bool coded = c.quant && x.in && c.page_format[x.phys] != 0;
     if (coded && c.k != nullptr) status |= MD_DEV_BAD_ROW;
-    const uint32_t more = (uint32_t)__ballot(goes_on);
+    const uint32_t ascending = (uint32_t)__ballot(ascends);
     uint64_t todo = __ballot(leads);
     uint16_t* const buf = turn[wv];
     const int m = lane & 15, g = lane >> 4;
     while (todo != 0) {
         const int i = __ffsll((unsigned long long)todo) - 1;
         todo &= todo - 1;
-        const uint32_t rest = i < 31 ? more >> (i + 1) : 0u;
-        const int len = 1 + (rest == 0xFFFFFFFFu ? 32 : __ffs(~rest) - 1);
         const int o = __builtin_amdgcn_readlane(x.t, i), phys = __builtin_amdgcn_readlane(x.phys, i);
         const int sub = __builtin_amdgcn_readlane(x.sub, i), s = __builtin_amdgcn_readlane(x.s, i);
-        const int row = r0 + i;
-        const int lo = __builtin_amdgcn_readlane(x.lo, i), hi = __builtin_amdgcn_readlane(x.hi, i);
-        const bool first = row == lo, last = row + len == hi;
+        const int row = r0 + i, block = __builtin_amdgcn_readlane(x.slot, i) >> 4;
+        const SessionRows rows = rows_of(i);
         const bool skip_k = c.quant && __builtin_amdgcn_readlane(coded ? 1 : 0, i);
-        const int n_slots = __builtin_amdgcn_readlane(x.nt, i);
-        auto slot_at = [&](int q) { return c.row_slot != nullptr ? c.row_slot[q] : n_slots - (hi - q); };
-        // whether the session's rows start with a block (or with nothing that counts)
-        bool starts_block = true;
-        if (CODES && last && !first) {
-            const int begin = slot_at(lo);
-            starts_block = begin < 0 || begin >= n_slots || (begin & 15) == 0;
-        }
-        // which tokens of the block the group holds (in order; gaps only from lists)
+        // the group's rows among the 32, up to the first that is there and in another block
+        const bool same = x.in && x.s == s && (x.slot >> 4) == block;
+        const uint32_t behind = 0xFFFFFFFFu << i;
+        uint32_t mine = (uint32_t)__ballot(same) & behind;
+        const uint32_t others = (uint32_t)__ballot(x.in && x.s == s && !same) & behind;
+        bool more = others == 0 && rows.hi > r0 + 32;   // it may go on behind them
+        if (others != 0) mine &= (others & -others) - 1u;
+        // which tokens of the block it holds, and the row of lane m's token
         uint32_t have = 0;
-        if (__builtin_amdgcn_readlane(x.t, i + len - 1) - o == len - 1) {
+        int from = row, top = -1;
+        const int len = __popc(mine);
+        if (__builtin_expect(mine >> i == (1u << (len & 31)) - 1u && len <= 16 &&
+                             __builtin_amdgcn_readlane(x.t, i + len - 1) - o == len - 1 && (mine & ~ascending) == 0, 1)) {
             have = ((1u << len) - 1u) << o;
+            from = row + m - o;
+            top = o + len - 1;
         } else {
-            for (int k = 0; k < len; ++k) have |= 1u << __builtin_amdgcn_readlane(x.t, i + k);
+            for (uint32_t left = mine; left != 0; left &= left - 1) {   // those that ascend
+                const int j = __ffs(left) - 1, t = __builtin_amdgcn_readlane(x.t, j);
+                if (t <= top) continue;
+                have |= 1u << t;
+                if (m == t) from = r0 + j;
+                top = t;
+            }
+        }
+        for (int q = r0 + 32; __builtin_expect(more && q < rows.hi, 0);) {   // (only behind rows that are not there)
+            q = rows.first_from(q, rows.hi, 0);
+            if (q == rows.hi) break;
+            const int slot = uni(rows.slot(q));
+            more = (slot >> 4) == block;
+            if (more && (slot & 15) > top) {
+                top = slot & 15;
+                have |= 1u << top;
+                if (m == top) from = q;
+            }
+            ++q;
+        }
+        const bool last = others == 0 && (more || rows.hi <= r0 + 32);   // no row behind it is there
+        // whether it is the session's first, and whether that starts with a block
+        bool first = row == rows.lo, starts_block = true;
+        if (CODES && c.v != nullptr && !first && (last || o > 0)) {
+            const int begin = uni(rows.first_from(rows.lo, row, 0));
+            first = begin == row;
+            starts_block = first || (uni(rows.slot(begin)) & 15) == 0;
         }
         // lane (m, g): dims 8g .. of token m
         const bool has = (have >> m) & 1u;
-        const int64_t at = (int64_t)(row + __popc(have & ((1u << m) - 1u))) * c.stride + kv * kHeadDim + 8 * g;
+        const int64_t at = (int64_t)from * c.stride + kv * kHeadDim + 8 * g;
         const size_t tile = tile_of(c, phys, sub, kv);
         if (c.k != nullptr && !skip_k && has) {
             const uint16_t* from = static_cast<const uint16_t*>(c.k) + at;
@@ -249,15 +358,8 @@ __global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(open + 32 * j) = w[j];
             } else if (first && o > 0) {
-                const int q = hi - 1 - m;   // the last rows, backwards
-                const int behind = slot_at(hi - 1), mine = q >= row ? slot_at(q) : -1;
-                const bool same = mine >= 0 && (mine >> 4) == (behind >> 4);
-                int from = -1;               // the row of token m
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const int tk = __builtin_amdgcn_readlane(same ? mine & 15 : -1, k);
-                    if (tk == m) from = hi - 1 - k;
-                }
+                int base;
+                const int from = rows.last_block(rows.hi, base);   // the row of token m
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     u32x4 y{0u, 0u, 0u, 0u};
