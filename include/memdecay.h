@@ -715,9 +715,10 @@ md_status md_decode_workspace(md_handle h, uint64_t* attend_bytes, uint64_t* sel
  *  v_open       uint16 bf16 bits [S][L][Hkv][16][d]: the values of the block
  *               that each session wrote last (zeros behind its last token).
  * A block's codes are those of its bf16 values, whichever calls wrote them:
- * rows that go on inside a block take its earlier values from v_open, which
- * holds them when a session's rows are written in order.  Half the bytes of a
- * bf16 pool, each value off by at most 2^-4 of itself or 2^-10 scale.
+ * rows that go on inside a block, and a step's token, take its earlier values
+ * from v_open, which holds them when a session's rows are written in order and
+ * none are taken back; md_open_blocks is for callers that take some back.
+ * Half the bytes of a bf16 pool, each value off by at most 2^-4 of itself or 2^-10 scale.
  */
 typedef struct md_row_list {
     const int32_t* row_start; /* [S + 1]                                                     */
@@ -734,11 +735,32 @@ typedef struct md_values {
 } md_values;                  /* all 16-byte aligned                                         */
 
 /*
+ * md_open_blocks — buffers in which md_append_codes and md_write_rows keep what
+ * the open blocks of 8-bit values hold, for callers that take a session's last
+ * tokens back (of tokens to verify, those that failed) and go on from there:
+ *  v_before     bf16 bits [S][L][Hkv][16][d]: the values of the block that each
+ *               session wrote before the one in v_open;
+ *  v_held       int32 [S][L][Hkv][4]: the block that v_open holds, as page *
+ *               (P / 16) + the block's place in it, and how many of its tokens;
+ *               then the same of v_before.  -1 for no block, which the caller
+ *               fills in at first and for a session that begins anew.
+ * Both 16-byte aligned and kept until another call; both NULL: none, as at
+ * first.  Rows and a step's token then go on inside the session's last block or
+ * the one before it, wherever its last tokens were taken back to; from further
+ * back they go on from a block's first token.  Inside a block that neither holds
+ * they do not count, and the block stays as it is (MD_DEV_BAD_ROW).  The codes
+ * of a block that tokens were taken from are those of all of them until it is
+ * written to again.  Host-only, no device work.  MD_E_UNSUPPORTED with an offload
+ * tier.
+ */
+md_status md_open_blocks(md_handle h, uint16_t* v_before, int32_t* v_held);
+
+/*
  * md_append_codes — md_append_values into 8-bit values: the values of the
  * tokens that the last md_observe_step appended, new_v bf16 bits
  * [S][L][Hkv][d].  A block whose scale does not change has its new codes
- * written; one whose scale grows, all of them.  Refusals as for
- * md_append_values.
+ * written; one whose scale grows, or that tokens were taken back from, all of
+ * them.  Refusals as for md_append_values.
  */
 md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v);
 
@@ -750,8 +772,10 @@ md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v
  * of its session may be with it (MD_DEV_BAD_ROW; no slot is written twice, and
  * the same rows every time).  A row whose page holds 8-bit keys does not count
  * (MD_DEV_BAD_ROW).
- * In the 8-bit pool a session's rows go on in one block after another: the
- * slots of a block behind the last row written to it get the code 0.
+ * In the 8-bit pool a session's rows go on in one block after another, without
+ * leaving tokens out: the slots of a block behind the last row written to it get
+ * the code 0, and one in front of it that is neither among the rows nor known
+ * from before makes the block's rows not count (MD_DEV_BAD_ROW).
  * MD_E_UNSUPPORTED with an offload tier.
  */
 typedef struct md_write_args {

@@ -45,7 +45,7 @@ EXPORTS = ("md_abi_version", "md_status_str", "md_init", "md_init_static", "md_o
            "md_profile_enable", "md_profile_read", "md_read_counters", "md_kernel_config", "md_observe_path",
            "md_calib_accumulate", "md_calib_fit",
            "md_norm_rope", "md_append_values", "md_attend_token", "md_key_bounds", "md_select_blocks",
-           "md_decode_workspace", "md_append_codes", "md_write_rows", "md_read_rows", "md_attend_values",
+           "md_decode_workspace", "md_open_blocks", "md_append_codes", "md_write_rows", "md_read_rows", "md_attend_values",
            "md_attend_rows", "md_rows_workspace", "md_destroy")
 
 # paths of md_observe_path
@@ -235,6 +235,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.md_select_blocks.argtypes = [vp, i32, vp]
     lib.md_decode_workspace.restype = i32
     lib.md_decode_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
+    lib.md_open_blocks.restype = i32
+    lib.md_open_blocks.argtypes = [vp, vp, vp]
     lib.md_append_codes.restype = i32
     lib.md_append_codes.argtypes = [vp, vp, vp]
     lib.md_write_rows.restype = i32
@@ -418,6 +420,10 @@ def md_decode_workspace(h: int):
     out = (ctypes.c_uint64(0), ctypes.c_uint64(0))
     _check("md_decode_workspace", load_library().md_decode_workspace(h, ctypes.byref(out[0]), ctypes.byref(out[1])))
     return int(out[0].value), int(out[1].value)
+
+
+def md_open_blocks(h: int, v_before: int, v_held: int) -> int:
+    return _check("md_open_blocks", load_library().md_open_blocks(h, v_before, v_held))
 
 
 def md_append_codes(h: int, new_v: int, values) -> int:

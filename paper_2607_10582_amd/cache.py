@@ -62,8 +62,11 @@ class PagedCache:
         self.v_codes = torch.empty((n_phys, L, Hkv, P // 16, d // 64, 4, 16, 4, 4), dtype=torch.uint8,
                                    device=dev) if coded else None
         self.v_scale = torch.empty((n_phys, L, Hkv, P // 16), dtype=torch.float32, device=dev) if coded else None
-        # the block that each session wrote last, in bf16
-        self.v_open = torch.zeros((S, L, Hkv, 16, d), dtype=torch.bfloat16, device=dev) if coded else None
+        # the block that each session wrote last, in bf16, the one it wrote before
+        # that, and which these are
+        self._v_open, self.v_before = (torch.zeros((S, L, Hkv, 16, d), dtype=torch.bfloat16, device=dev) if coded else None
+                                       for _ in range(2))
+        self.v_held = torch.full((S, L, Hkv, 4), -1, **i32) if coded else None
         self.key_bounds = torch.empty((n_phys, L, Hkv, 2, d), dtype=torch.int8, device=dev) if bounds else None
         self.bound_exp = torch.empty((n_phys, L, Hkv), dtype=torch.int8, device=dev) if bounds else None
         # offload tier: offload_pages host-memory pages per session, their
@@ -82,6 +85,17 @@ class PagedCache:
             self.off_format = torch.zeros((S, H), dtype=torch.uint8, device=dev)
             self.off_score = torch.zeros((S, H), dtype=torch.float32, device=dev)
             self.off_abar = torch.zeros((S, H, P), dtype=torch.float32, device=dev)
+
+    @property
+    def v_open(self) -> Optional[torch.Tensor]:
+        return self._v_open
+
+    @v_open.setter
+    def v_open(self, blocks: torch.Tensor):
+        # what a caller's own blocks hold is not known: they are taken for the
+        # block that a session's rows go on in (memdecay.h)
+        self._v_open = blocks
+        self.v_before = self.v_held = None
 
     OFFLOAD_BUFFERS = ("host_keys", "off_count", "off_serial", "off_slot", "off_region", "off_t_ins",
                        "off_t_ref", "off_importance", "off_format", "off_score", "off_abar")
@@ -229,7 +243,77 @@ class PagedCache:
         self.clock[s] = clock
         self.next_serial[s] = m
         self.budget[s] = budget
+        if self.v_held is not None:
+            self.v_held[s] = -1
         return ids, posd, m
+
+    def place_tokens(self, s: int, region, region_aligned: bool = False) -> np.ndarray:
+        """Room for more tokens of a session in use, as steps would append them
+        one by one (a chunk of a prompt, tokens to verify): their region codes
+        [n], their times from the session's clock on, and the pages that they
+        open, off the free list.  Their keys and values come through
+        MemDecay.write_rows.  Returns their slots."""
+        P, region = self.P, np.asarray(region, dtype=np.uint8)
+        n, nt, np_, clock = len(region), int(self.n_tokens[s]), int(self.n_pages[s]), int(self.clock[s])
+        if self.offload_pages > 0:
+            raise ValueError("tokens are not placed beside an offload tier")
+        if n == 0:
+            return np.zeros(0, np.int64)
+        old = self.page_table[s, :np_].cpu().numpy()
+        pos = np.arange(nt, nt + n)
+        if region_aligned:
+            ahead = nt % P   # the open page's tokens, the last one's region among them
+            last = [int(self.region[int(old[-1]), ahead - 1])] * ahead if ahead else []
+            pos = nt - ahead + self.positions(np.concatenate([np.array(last, np.uint8), region]), P, True)[ahead:]
+        end, free = int(pos[-1]) + 1, int(self.free_count[0])
+        m = -(-end // P)
+        if m > self.max_pages or m - np_ > free:
+            raise ValueError(f"{m - np_} more pages for session {s} with {np_} of {self.max_pages}, {free} pages are free")
+        ids = self.free_list[free - (m - np_):free].flip(0)
+        self.free_count[0] = free - (m - np_)
+        self.page_table[s, np_:m] = ids
+        serial = int(self.next_serial[s])
+        self.page_serial[s, np_:m] = torch.arange(serial, serial + m - np_, dtype=torch.int32, device=self.device)
+        self.next_serial[s] = serial + m - np_
+        self.page_format[ids.long()] = 0
+        table = self.page_table[s, :m].long()
+        flat = lambda at: table[torch.as_tensor(at // P, device=self.device)] * P + torch.as_tensor(at % P, device=self.device)
+        every, own = flat(np.arange(nt, end)), flat(pos)
+        t = torch.arange(clock + 1, clock + 1 + n, dtype=torch.int32, device=self.device)
+        for x, hole, token in ((self.region, B.MD_REGION_HOLE, torch.as_tensor(region, device=self.device)), (self.t_ins, 0, t),
+                               (self.t_ref, 0, t), (self.importance, 0.0, 0.0)):
+            x.view(-1)[every] = hole
+            x.view(-1)[own] = token
+        self.n_pages[s] = m
+        self.n_tokens[s] = end
+        self.n_live[s] += n
+        self.clock[s] = clock + n
+        return pos
+
+    def take_back(self, s: int, n: int):
+        """The last n tokens of a session leave (of tokens to verify, those that
+        failed): the pages that they alone were in go back to the free list,
+        and the clock to where it was before them."""
+        P, nt, np_ = self.P, int(self.n_tokens[s]), int(self.n_pages[s])
+        table = self.page_table[s, :np_].long()
+        live = np.flatnonzero((self.region[table].flatten()[:nt] != B.MD_REGION_HOLE).cpu().numpy())
+        if self.offload_pages > 0 or n < 0 or n > len(live):
+            raise ValueError(f"{n} of {len(live)} tokens of session {s} to take back")
+        if n == 0:
+            return
+        left = int(live[-n - 1]) + 1 if n < len(live) else 0
+        m = -(-left // P)
+        if left < m * P and int(self.page_format[table[m - 1]]):
+            raise ValueError(f"the page that session {s} would go on in holds 8-bit keys")
+        free = int(self.free_count[0])
+        self.free_list[free:free + np_ - m] = self.page_table[s, m:np_].flip(0)
+        self.free_count[0] = free + np_ - m
+        self.page_table[s, m:] = -1
+        self.page_serial[s, m:] = -1
+        self.n_pages[s] = m
+        self.n_tokens[s] = left
+        self.n_live[s] -= n
+        self.clock[s] -= n
 
     def load_values(self, s: int, values: torch.Tensor, region=None):
         """Place the values bf16 [n][L][Hkv][d] of a session's prompt next to
@@ -259,6 +343,10 @@ class PagedCache:
         self.v_scale.index_copy_(0, ids, scale)
         at = (slots - 1) % P // 16 * 16
         self.v_open[s] = full[-1, at:at + 16].permute(1, 2, 0, 3)
+        if self.v_held is not None:
+            self.v_held[s] = -1
+            self.v_held[s, ..., 0] = (ids[-1] * (P // 16) + at // 16).int()
+            self.v_held[s, ..., 1] = (slots - 1) % 16 + 1
 
     def set_free_pages(self, ids: Sequence[int]):
         """The free list: ids pop from the end."""
@@ -315,6 +403,7 @@ class MemDecay:
         # stream run one after another)
         self._attend_ws = self._select_ws = self._rows_ws = None
         self._device = cache.k_pool.get_device()
+        self._held = None   # the handle's md_open_blocks
         if cache.v_pool is not None or cache.v_codes is not None:   # now, so that a captured call allocates nothing
             self._workspace(True)
         if cache.key_bounds is not None:
@@ -439,8 +528,21 @@ class MemDecay:
         if c.v_codes is None:
             return self._values(), 0, 0, 0
         n = c.k_pool.numel()
+        if written and self._held is not c.v_held:
+            self._keep_open_blocks()
         return (0, _flat(c.v_codes, torch.uint8, n, dev), _flat(c.v_scale, torch.float32, n // (16 * c.d), dev),
                 _flat(c.v_open, torch.bfloat16, c.S * c.L * c.Hkv * 16 * c.d, dev) if written else 0)
+
+    def _keep_open_blocks(self):
+        """Tells the handle where the cache keeps what its open blocks hold."""
+        c, dev = self.cache, self._device
+        if c.v_held is None:
+            B.md_open_blocks(self.handle, None, None)
+        else:
+            n = c.S * c.L * c.Hkv
+            B.md_open_blocks(self.handle, _flat(c.v_before, torch.bfloat16, 16 * n * c.d, dev),
+                             _flat(c.v_held, torch.int32, 4 * n, dev))
+        self._held = c.v_held
 
     # ---- rows of the cache: prompts, chunks of them, tokens to verify.  The
     # rows of a call are ragged: row_start int32 [S + 1] tells where each
@@ -482,7 +584,12 @@ class MemDecay:
         layer into the pools, values as codes in a cache of 8-bit values.  A
         session's slots ascend, and its rows are written in order.  Keys of
         pages that hold 8-bit keys are left alone.  Runs on the handle's
-        stream, whatever stream is current."""
+        stream, whatever stream is current.
+
+        Of tokens to verify (PagedCache.place_tokens) the last ones may leave
+        again (PagedCache.take_back): with 8-bit values rows and steps then go on
+        inside the last block of 16 slots or the one before it; further back,
+        from a block's first slot (else they do not count: device_status())."""
         n, k_at, v_at, pitch, _ = self._kv_rows(k, v, (torch.bfloat16,))
         rows = self._row_list(n, row_start, row_slot)
         if n == 0:

@@ -32,6 +32,7 @@ struct md_handle_s {
     md::View v;
     md::Scratch sc;
     md::CodeTimes ct;    // the quantised tier's conversions (NULLs: not noted)
+    md::Held held;       // md_open_blocks
     hipStream_t stream;
     int device;
     void* scratch;
@@ -639,6 +640,7 @@ static md_status init_handle(const md_config* cfg, const md_region_params* rp, c
     h->logits_blocks = 3 * n_cu;
     h->mass_blocks = 4 * n_cu;
     h->score_blocks = 2 * n_cu;
+    h->held = md::Held{};
     h->have_step = false;
     h->last_step = 0;
     h->fused_first = fused_first;
@@ -1107,7 +1109,17 @@ md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v
     if (!h->fresh) return MD_E_STATE;
     const OnDevice on(h->device);
     if (!on.ok) return MD_E_HIP;
-    return md::launch_append_codes(h->dm, h->v, new_v, *v, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+    const hipError_t e = h->held.at != nullptr ? md::launch_append_held(h->dm, h->v, h->sc, new_v, *v, h->held, h->stream)
+                                               : md::launch_append_codes(h->dm, h->v, new_v, *v, h->stream);
+    return e == hipSuccess ? MD_OK : MD_E_HIP;
+}
+
+md_status md_open_blocks(md_handle h, uint16_t* v_before, int32_t* v_held) {
+    if (h == nullptr || (v_before == nullptr) != (v_held == nullptr) || !aligned(v_before, 16) || !aligned(v_held, 16))
+        return MD_E_INVALID;
+    if (h->dm.H > 0) return MD_E_UNSUPPORTED;
+    h->held = md::Held{v_before, v_held};
+    return MD_OK;
 }
 
 md_status md_write_rows(md_handle h, int32_t layer, const md_write_args* a) {
@@ -1120,7 +1132,10 @@ md_status md_write_rows(md_handle h, int32_t layer, const md_write_args* a) {
     if (a->rows.n_rows == 0) return MD_OK;
     const OnDevice on(h->device);
     if (!on.ok) return MD_E_HIP;
-    return md::launch_write_rows(h->dm, h->v, h->sc, layer, *a, h->stream) == hipSuccess ? MD_OK : MD_E_HIP;
+    const hipError_t e = h->held.at != nullptr && a->v != nullptr && a->values.v_pool == nullptr
+                             ? md::launch_write_held(h->dm, h->v, h->sc, layer, *a, h->held, h->stream)
+                             : md::launch_write_rows(h->dm, h->v, h->sc, layer, *a, h->stream);
+    return e == hipSuccess ? MD_OK : MD_E_HIP;
 }
 
 md_status md_read_rows(md_handle h, int32_t layer, const md_read_args* a) {

@@ -59,10 +59,20 @@ hipError_t launch_token(const Dims& dm, const View& v, const Scratch& sc, int n_
 hipError_t launch_token_values(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_attend_args& a,
                                const md_values& values, int window, int sinks, hipStream_t st);
 
+// What a caller keeps beside the open blocks of 8-bit values (md_open_blocks; NULLs: nothing).
+struct Held {
+    uint16_t* before;
+    int32_t* at;
+};
+
 // Rows into and out of the pools (md_store.hip), attention of ragged rows (md_prompt.hip).
 hipError_t launch_append_codes(const Dims& dm, const View& v, const uint16_t* new_v, const md_values& values, hipStream_t st);
 hipError_t launch_write_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
                              hipStream_t st);
+hipError_t launch_append_held(const Dims& dm, const View& v, const Scratch& sc, const uint16_t* new_v, const md_values& values,
+                              const Held& held, hipStream_t st);
+hipError_t launch_write_held(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
+                             const Held& held, hipStream_t st);
 hipError_t launch_read_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_read_args& a, hipStream_t st);
 uint64_t rows_workspace(const Dims& dm, int n_cu);
 hipError_t launch_attend_rows(const Dims& dm, const View& v, const Scratch& sc, int n_cu, int layer, const md_rows_args& a,

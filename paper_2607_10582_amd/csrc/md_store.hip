@@ -34,6 +34,7 @@ struct RowCall {
     const int32_t* row_slot;
     int n_rows;
     md_values values;
+    Held held;
     void* k;   // the caller's rows
     void* v;
     int64_t stride;
@@ -87,11 +88,13 @@ __device__ __forceinline__ void wave_lds() {
 struct Span {
     int s, lo, hi, nt; // its session, that session's rows and slots in use
     int slot, prev;    // its slot, and that of the session's row before it (-1: its first)
+    int edge;          // ENDS: the slot of the session's first row, from lane 32 on of its last one
     int phys, sub, t;  // page, block of it and token of the block
     bool mine;         // it is some session's row
     bool in;           // and its slot holds a token's place
 };
 
+template <bool ENDS>
 __device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
     const int lane = lane_id(), r = r0 + (lane & 31);
     Span x{};
@@ -127,6 +130,10 @@ __device__ __forceinline__ Span span_of(const RowCall& c, int r0, int& status) {
     x.nt = nt;
     x.slot = c.row_slot != nullptr ? c.row_slot[r] : nt - (x.hi - r);
     x.prev = r <= x.lo ? -1 : c.row_slot != nullptr ? c.row_slot[r - 1] : x.slot - 1;
+    if constexpr (ENDS) {
+        const int at = lane < 32 ? x.lo : x.hi - 1;
+        x.edge = c.row_slot != nullptr ? c.row_slot[at] : nt - (x.hi - at);
+    }
     x.in = x.slot >= 0 && x.slot < nt;
     if (!x.in) {
         status |= MD_DEV_BAD_ROW;
@@ -196,23 +203,31 @@ struct SessionRows {
         return first_from(a, b, least);
     }
 
-    // The rows of the last block that rows up to `end` (not itself) reach: lane
-    // m's is that of token m, or -1; `base`: its first slot (-1: no row is there).
-    __device__ __forceinline__ int last_block(int end, int& base) const {
-        int from = -1;
-        base = -1;
+    // The rows of the last block that rows up to `end` (not itself) reach.
+    struct Block {
+        int base;    // its first slot (-1: no row is there)
+        int begin;   // its first row
+        int from;    // lane m's: that of token m, or -1
+        uint32_t have;
+        // Its tokens up to the last one (0: some are missing).
+        __device__ __forceinline__ int tokens() const { return (have & (have + 1)) == 0 ? __popc(have) : 0; }
+    };
+    __device__ __forceinline__ Block last_block(int end) const {
+        Block b{-1, end, -1, 0};
         for (int q = end; q > lo; q -= 64) {
             const int r = q - 1 - lane_id(), x = r >= lo ? slot(r) : -1;
             uint64_t in = __ballot(there(x));
             while (in != 0) {
                 const int i = __ffsll((unsigned long long)in) - 1, at = __builtin_amdgcn_readlane(x, i);
                 in &= in - 1;
-                if (base < 0) base = at & ~15;
-                if ((at & ~15) != base) return from;
-                if (from < 0 && (at & 15) == (lane_id() & 15)) from = q - 1 - i;
+                if (b.base < 0) b.base = at & ~15;
+                if ((at & ~15) != b.base) return b;
+                b.begin = q - 1 - i;
+                b.have |= 1u << (at & 15);
+                if (b.from < 0 && (at & 15) == (lane_id() & 15)) b.from = b.begin;
             }
         }
-        return from;
+        return b;
     }
 };
 
@@ -223,16 +238,18 @@ struct SessionRows {
 // whose slots are not there may lie anywhere between (the search by halves
 // gives way to one that passes over them where it meets one).  Keys go as they
 // come, 1 KiB of a block at a time; values turn in LDS, from rows of dims to
-// dims of four tokens.
+// dims of four tokens.  Six waves a SIMD: left to five by its registers, 16 x
+// 32,768 rows with 8-bit values took 177 us instead of 171, by lists of slots 217
+// instead of 207.
 template <bool CODES>
-__global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(6))) k_write_rows(RowCall c) {
     __shared__ __align__(16) uint16_t turn[kWaves][16 * kPitch];
     const int lane = lane_id(), wv = threadIdx.x >> 6;
     const int64_t task = (int64_t)blockIdx.x * kWaves + wv;
     const int r0 = (int)(task / c.Hkv) * 16, kv = (int)(task % c.Hkv);
     if (r0 >= c.n_rows) return;
     int status = 0;
-    const Span x = span_of(c, r0, status);
+    const Span x = span_of<CODES>(c, r0, status);
     const int r = r0 + (lane & 31);
     // the slot of the session's row before it that is there, as far as these 32 rows
     // and the one in front of them tell (below 0: none)
@@ -317,12 +334,43 @@ __global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
         }
         const bool last = others == 0 && (more || rows.hi <= r0 + 32);   // no row behind it is there
         // whether it is the session's first, and whether that starts with a block
-        bool first = row == rows.lo, starts_block = true;
-        if (CODES && c.v != nullptr && !first && (last || o > 0)) {
+        const int head = CODES ? __builtin_amdgcn_readlane(x.edge, i) : 0, tail = CODES ? __builtin_amdgcn_readlane(x.edge, i + 32) : 0;
+        const bool ends = rows.there(head) && rows.there(tail);   // the session's first and last rows are there
+        bool first = row == rows.lo, starts_block = (head & 15) == 0;
+        if (CODES && __builtin_expect(!ends, 0)) {
             const int begin = uni(rows.first_from(rows.lo, row, 0));
             first = begin == row;
-            starts_block = first || (uni(rows.slot(begin)) & 15) == 0;
+            starts_block = (uni(rows.slot(begin)) & 15) == 0;
         }
+        // Where a token in front of the group's last one is not among the rows, it is
+        // in the open block or the one before that, whichever is this one: the
+        // session's first group looks, which alone may (the others' blocks are not
+        // there yet).  Told of neither the open block is taken for it.
+        const int id = phys * (c.P >> 4) + sub;
+        const size_t open_at = CODES ? ((((size_t)s * c.L + c.layer) * c.Hkv + kv) * 16 + m) * kHeadDim + 8 * g : 0;
+        uint16_t* const open = CODES ? c.values.v_open + open_at : nullptr;
+        uint16_t* const before = CODES ? c.held.before + open_at : nullptr;
+        int4* const held_at = CODES && c.held.at != nullptr
+                                  ? reinterpret_cast<int4*>(c.held.at) + ((size_t)s * c.L + c.layer) * c.Hkv + kv : nullptr;
+        const uint16_t* source = open;
+        int known = first ? o : 0;   // tokens of it that count
+        int4 held{-1, 0, -1, 0};
+        if (held_at != nullptr) {
+            if (first && (last || o > 0)) {
+                held = *held_at;
+                held = int4{uni(held.x), uni(held.y), uni(held.z), uni(held.w)};
+            }
+            known = 0;
+            if (have != (2u << top) - 1u) {
+                if (first && o > 0 && held.x == id) known = min(held.y, top);
+                else if (first && o > 0 && held.z == id) known = min(held.w, top), source = before;
+                if (known == 0) {   // what the block holds is not known: it stays
+                    status |= MD_DEV_BAD_ROW;
+                    have = 0;
+                }
+            }
+        }
+        const bool refused = have == 0;
         // lane (m, g): dims 8g .. of token m
         const bool has = (have >> m) & 1u;
         const int64_t at = (int64_t)from * c.stride + kv * kHeadDim + 8 * g;
@@ -340,9 +388,8 @@ __global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
         u32x4 w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = u32x4{0u, 0u, 0u, 0u};
-        uint16_t* const open = CODES ? c.values.v_open + ((((size_t)s * c.L + c.layer) * c.Hkv + kv) * 16 + m) * kHeadDim + 8 * g : nullptr;
-        if (has || (CODES && first && m < o)) {
-            const uint16_t* from = has ? static_cast<const uint16_t*>(c.v) + at : open;
+        if (has || (CODES && m < known)) {
+            const uint16_t* from = has ? static_cast<const uint16_t*>(c.v) + at : source;
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4*>(from + 32 * j);
         }
@@ -351,30 +398,90 @@ __global__ void __launch_bounds__(64 * kWaves) k_write_rows(RowCall c) {
         for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(buf + m * kPitch + 32 * j + 8 * g) = w[j];
         wave_lds();
         if constexpr (CODES) {
-            // The open block becomes the session's last one.  Where the rows go
-            // on inside a block, this wave alone has read it, and writes it too:
-            // from the rows, for a block that is another wave's.
-            if (last && (first || starts_block)) {
+            // The open block becomes the session's last one, and the one before it the
+            // last but one, each by its own wave.  Where the rows go on inside a block,
+            // the first block's wave alone has read them, and writes both: from the
+            // rows, for blocks that are other waves'.
+            auto keep = [&](uint16_t* to) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(open + 32 * j) = w[j];
-            } else if (first && o > 0) {
-                int base;
-                const int from = rows.last_block(rows.hi, base);   // the row of token m
+                for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(to + 32 * j) = w[j];
+            };
+            auto keep_rows = [&](uint16_t* to, int from) {   // from: the row of token m, or -1
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     u32x4 y{0u, 0u, 0u, 0u};
                     if (from >= 0)
                         y = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(c.v) + (int64_t)from * c.stride +
                                                             kv * kHeadDim + 8 * g + 32 * j);
-                    *reinterpret_cast<u32x4*>(open + 32 * j) = y;
+                    *reinterpret_cast<u32x4*>(to + 32 * j) = y;
+                }
+            };
+            auto id_of = [&](int slot) {
+                return c.page_table[(size_t)s * c.MP + (slot >> c.Pshift)] * (c.P >> 4) + ((slot & (c.P - 1)) >> 4);
+            };
+            const bool alone = first && last;
+            const bool second = others != 0 && ends && starts_block &&   // the last but one
+                                __builtin_amdgcn_readlane(x.slot, __ffs(others | 0x80000000u) - 1) >> 4 == tail >> 4;
+            if ((alone && !refused) || (last && !first && starts_block)) {
+                int4 now{-1, 0, -1, 0};
+                if (held_at != nullptr && alone) {
+                    if (held.x == id) {
+                        now = held;
+                    } else if (o == 0 && held.x >= 0) {   // a new block: the open one becomes the one before it
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<u32x4*>(before + 32 * j) = *reinterpret_cast<const u32x4*>(open + 32 * j);
+                        now = int4{-1, 0, held.x, held.y};
+                    }
+                } else if (held_at != nullptr && !refused && !ends) {   // (else the last but one does this)
+                    const SessionRows::Block b = rows.last_block(row);
+                    if (b.tokens() > 0) {
+                        keep_rows(before, b.from);
+                        now = int4{-1, 0, id_of(b.base), b.tokens()};
+                    }
+                }
+                if (!refused) {
+                    keep(open);
+                    now.x = id;
+                    now.y = top + 1;
+                }
+                if (held_at != nullptr && lane == 0) {
+                    reinterpret_cast<int2*>(held_at)[0] = int2{now.x, now.y};
+                    if (alone || !ends) reinterpret_cast<int2*>(held_at)[1] = int2{now.z, now.w};
+                }
+            } else if (second && held_at != nullptr) {
+                if (!refused) keep(before);
+                if (lane == 0) reinterpret_cast<int2*>(held_at)[1] = refused ? int2{-1, 0} : int2{id, top + 1};
+            } else if (first && o > 0 && !last) {
+                const SessionRows::Block b = rows.last_block(rows.hi);
+                keep_rows(open, b.from);
+                if (held_at != nullptr) {
+                    int4 now{-1, 0, -1, 0};
+                    if (b.tokens() > 0) {
+                        now = int4{id_of(b.base), b.tokens(), -1, 0};
+                        const SessionRows::Block f = rows.last_block(b.begin);
+                        if (f.base >> 4 == block) {   // this one
+                            if (!refused) {
+                                keep(before);
+                                now.z = id;
+                                now.w = top + 1;
+                            }
+                        } else if (f.tokens() > 0) {
+                            keep_rows(before, f.from);
+                            now.z = id_of(f.base);
+                            now.w = f.tokens();
+                        }
+                    }
+                    if (lane == 0) *held_at = now;
                 }
             }
-            uint32_t top = 0;
+            if (refused) continue;
+            uint32_t largest = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) top = max(top, top_of(w[j][k]));
-            const float scale = scale_of(wave_max_u32(top));
+                for (int k = 0; k < 4; ++k) largest = max(largest, top_of(w[j][k]));
+            const float scale = scale_of(wave_max_u32(largest));
             uint8_t* to = c.values.v_codes + tile + 16 * lane;
 #pragma unroll
             for (int a = 0; a < 2; ++a) *reinterpret_cast<u32x4*>(to + 1024 * a) = block_codes(buf, a, scale);
@@ -436,7 +543,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_read_rows(RowCall c) {
     const int r0 = (int)(task / c.Hkv) * 16, kv = (int)(task % c.Hkv);
     if (r0 >= c.n_rows) return;
     int status = 0;
-    Span x = span_of(c, r0, status);
+    Span x = span_of<false>(c, r0, status);
     const int m = lane & 15, g = lane >> 4;
     // lane (m, g) works on row m
     const int phys = __shfl(x.phys, m), sub = __shfl(x.sub, m), t = __shfl(x.t, m);
@@ -542,14 +649,20 @@ __global__ void __launch_bounds__(64 * kWaves) k_read_rows(RowCall c) {
 // only grow within a block, and max and division keep their order under
 // rounding: scale = max(scale before, |v|'s own), so a token that does not
 // raise it costs its own 128 codes.  One that does has the block's codes
-// written anew, from the open block's values.
+// written anew, from the open block's values; so has one behind tokens that were
+// taken back, which the scale still knows of (HELD: they are told by what the
+// blocks held).
+template <bool HELD>
 __global__ void __launch_bounds__(64 * kWaves) k_append_codes(Dims dm, View v, const uint16_t* __restrict__ new_v,
-                                                              md_values values) {
+                                                              md_values values, Held kept, int32_t* status) {
     __shared__ __align__(16) uint16_t turn[kWaves][16 * kPitch];
     const int lane = lane_id(), wv = threadIdx.x >> 6, s = blockIdx.y;
     const int row = blockIdx.x * kWaves + wv;   // (layer, KV head)
     if (row >= dm.LHkv) return;
     const uint32_t mine = reinterpret_cast<const uint32_t*>(new_v)[((size_t)s * dm.LHkv + row) * (kHeadDim / 2) + lane];
+    int4* const held_at = HELD ? reinterpret_cast<int4*>(kept.at) + (size_t)s * dm.LHkv + row : nullptr;
+    int4 held{-1, 0, -1, 0};
+    if constexpr (HELD) held = *held_at;
     const int np = v.n_pages[s], nt = v.n_tokens[s];
     if (!counters_ok(np, nt, dm) || np == 0) return;
     const int p = v.page_table[(size_t)s * dm.MP + np - 1];
@@ -558,16 +671,45 @@ __global__ void __launch_bounds__(64 * kWaves) k_append_codes(Dims dm, View v, c
     if (v.t_ins[(size_t)p * dm.P + slot] != v.clock[s]) return;
     const size_t tile = ((size_t)p * dm.LHkv + row) * dm.P * kHeadDim + (size_t)(slot & ~15) * kHeadDim;
     float* const scale_p = values.v_scale + ((size_t)p * dm.LHkv + row) * (dm.P >> 4) + (slot >> 4);
-    uint32_t* const open = reinterpret_cast<uint32_t*>(values.v_open) + ((size_t)s * dm.LHkv + row) * 16 * (kHeadDim / 2) + lane;
-    const float before = o > 0 ? *scale_p : 0.0f;
-    const uint32_t own_top = wave_max_u32(top_of(mine));
-    const float own_scale = scale_of(own_top);
-    open[o * (kHeadDim / 2)] = mine;
+    const size_t open_at = ((size_t)s * dm.LHkv + row) * 16 * (kHeadDim / 2) + lane;
+    uint32_t* const open = reinterpret_cast<uint32_t*>(values.v_open) + open_at;
+    const uint32_t* source = open;
+    int known = o;          // tokens of the source that count
+    bool again = false;     // the scale may know of tokens that are no more
+    if constexpr (HELD) {
+        uint32_t* const before = reinterpret_cast<uint32_t*>(kept.before) + open_at;
+        const int id = p * (dm.P >> 4) + (slot >> 4);
+        int4 now{id, o + 1, held.z, held.w};
+        if (held.x == id) {
+            again = held.y > o;
+            known = min(o, held.y);
+        } else if (o > 0 && held.z == id) {
+            again = true;
+            known = min(o, held.w);
+            source = before;
+            now.z = -1;
+        } else if (o > 0) {   // what the block holds is not known: it stays
+            if (lane == 0) atomicOr(status, MD_DEV_BAD_ROW);
+            return;
+        } else {              // a new block: the open one becomes the one before it
+            now.z = held.x;
+            now.w = held.y;
+            if (held.x >= 0) {
+#pragma unroll
+                for (int t = 0; t < 16; ++t) before[t * (kHeadDim / 2)] = open[t * (kHeadDim / 2)];
+            }
+        }
+        if (lane == 0) *held_at = now;
+    }
+    const float scale_before = o > 0 ? *scale_p : 0.0f;
+    uint32_t top = top_of(mine);
     uint8_t* const codes = values.v_codes + tile;
-    if (o > 0 && (own_scale <= before || before != before)) {
+    float own_scale = scale_of(wave_max_u32(top));
+    if (o > 0 && !again && (own_scale <= scale_before || scale_before != scale_before)) {
+        open[o * (kHeadDim / 2)] = mine;
         const int e = 2 * lane;   // dims e and e + 1: neighbours m, m + 1 of the same 16
-        const uint32_t w = four_codes(in_scale(bf16_value((uint16_t)mine), before), in_scale(bf16_value((uint16_t)(mine >> 16)), before),
-                                      0.0f, 0.0f);
+        const uint32_t w = four_codes(in_scale(bf16_value((uint16_t)mine), scale_before),
+                                      in_scale(bf16_value((uint16_t)(mine >> 16)), scale_before), 0.0f, 0.0f);
         uint8_t* to = codes + (e / 64) * 1024 + (o / 4) * 256 + (e % 16) * 16 + ((e / 16) % 4) * 4 + o % 4;
         to[0] = (uint8_t)w;
         to[16] = (uint8_t)(w >> 8);
@@ -577,11 +719,13 @@ __global__ void __launch_bounds__(64 * kWaves) k_append_codes(Dims dm, View v, c
 #pragma unroll
     for (int t = 0; t < 16; ++t) {
         uint32_t w = 0u;
-        if (t < o) w = open[t * (kHeadDim / 2)];
+        if (t < known) w = source[t * (kHeadDim / 2)];
         if (t == o) w = mine;
-        if (o == 0 && t > 0) open[t * (kHeadDim / 2)] = 0u;
+        if (again) top = max(top, top_of(w));
+        if (t == o || again || (o == 0 && t > 0)) open[t * (kHeadDim / 2)] = w;
         *reinterpret_cast<uint32_t*>(buf + t * kPitch + 2 * lane) = w;
     }
+    if (again) own_scale = scale_of(wave_max_u32(top));
     wave_lds();
 #pragma unroll
     for (int a = 0; a < 2; ++a) *reinterpret_cast<u32x4*>(codes + 1024 * a + 16 * lane) = block_codes(buf, a, own_scale);
@@ -620,24 +764,41 @@ hipError_t launch(const void* fn, RowCall& c, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_append_codes(const Dims& dm, const View& v, const uint16_t* new_v, const md_values& values, hipStream_t st) {
+static hipError_t launch_append(const void* fn, const Dims& dm, const View& v, int32_t* status, const uint16_t* new_v,
+                                const md_values& values, const Held& held, hipStream_t st) {
     Dims d = dm;
     View vv = v;
     md_values w = values;
-    void* args[] = {&d, &vv, &new_v, &w};
+    Held b = held;
+    void* args[] = {&d, &vv, &new_v, &w, &b, &status};
     const dim3 grid((unsigned)((dm.LHkv + kWaves - 1) / kWaves), (unsigned)dm.S);
-    return hipLaunchKernel(reinterpret_cast<const void*>(&k_append_codes), grid, dim3(64 * kWaves), args, 0, st);
+    return hipLaunchKernel(fn, grid, dim3(64 * kWaves), args, 0, st);
 }
 
-hipError_t launch_write_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
-                             hipStream_t st) {
+hipError_t launch_append_codes(const Dims& dm, const View& v, const uint16_t* new_v, const md_values& values, hipStream_t st) {
+    return launch_append(reinterpret_cast<const void*>(&k_append_codes<false>), dm, v, nullptr, new_v, values, Held{}, st);
+}
+
+hipError_t launch_append_held(const Dims& dm, const View& v, const Scratch& sc, const uint16_t* new_v, const md_values& values,
+                              const Held& held, hipStream_t st) {
+    return launch_append(reinterpret_cast<const void*>(&k_append_codes<true>), dm, v, sc.status, new_v, values, held, st);
+}
+
+hipError_t launch_write_held(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
+                             const Held& held, hipStream_t st) {
     RowCall c = row_call(dm, v, sc, layer, a.rows);
     c.values = a.values;
+    c.held = held;
     c.k = const_cast<uint16_t*>(a.k);
     c.v = const_cast<uint16_t*>(a.v);
     c.stride = a.stride;
     return launch(a.v != nullptr && a.values.v_pool == nullptr ? reinterpret_cast<const void*>(&k_write_rows<true>)
                                                                : reinterpret_cast<const void*>(&k_write_rows<false>), c, st);
+}
+
+hipError_t launch_write_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_write_args& a,
+                             hipStream_t st) {
+    return launch_write_held(dm, v, sc, layer, a, Held{}, st);
 }
 
 hipError_t launch_read_rows(const Dims& dm, const View& v, const Scratch& sc, int layer, const md_read_args& a, hipStream_t st) {

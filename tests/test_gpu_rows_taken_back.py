@@ -1,0 +1,335 @@
+"""Tokens to verify over 8-bit values: drafts enter the cache, attend, and the
+last of them leave again; what goes on from there has the codes of the values
+that are there, as if the others had never been."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_10582_amd import binding as B
+from paper_2607_10582_amd.cache import PagedCache
+from rows_world import BF16, D, World, quantise_slots
+from test_gpu_rows import TYPES, check_rows, check_token, same
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm device")
+    B.load_library()
+
+
+def resize(w, s, n):
+    """The host's copy of a session at n slots."""
+    old = min(n, len(w.live[s]))
+    for name in ("k", "v16", "v"):
+        x = getattr(w, name)[s]
+        y = torch.zeros((n, *x.shape[1:]), dtype=x.dtype)
+        y[:old] = x[:old]
+        getattr(w, name)[s] = y
+    w.live[s] = np.concatenate([w.live[s][:old], np.zeros(n - old, bool)])
+    w.slots[s] = n
+
+
+def place(w, counts):
+    """Room for drafts: row_start, row_slot, and both on the host."""
+    slot = []
+    for s, n in enumerate(counts):
+        # (a draft is of one region: with region-aligned pages each opens a page, and
+        # more than two blocks are further back than the open ones)
+        region = np.full(n, w.rng.integers(0, 7)) if w.aligned else w.rng.integers(0, 7, n)
+        at = w.cache.place_tokens(s, region, w.aligned)
+        resize(w, s, int(w.cache.n_tokens[s]))
+        w.live[s][at] = True
+        slot += at.tolist()
+    start = np.concatenate([[0], np.cumsum(counts)])
+    return w.i32(start), w.i32(slot), start, np.array(slot, dtype=int)
+
+
+def write(w, rows, big=1.0):
+    """Random keys and values of these rows in every layer."""
+    start_d, slot_d, start, slot = rows
+    session = np.repeat(np.arange(w.S), np.diff(start))
+    n = len(slot)
+    for layer in range(w.L):
+        k, v = (w.normal(n, w.Hkv, D) for _ in "kv")
+        k, v = k.to(BF16), (v * big).to(BF16)
+        w.md.write_rows(layer, start_d, k, v, row_slot=slot_d)
+        for r, (s, t) in enumerate(zip(session, slot)):
+            w.k[s][t, layer] = k[r].double().cpu()
+            w.v16[s][t, layer] = v[r].float().cpu()
+
+
+def stored(w, s):
+    """What the pool holds for a session's values."""
+    n, m = w.slots[s], int(w.cache.n_pages[s])
+    ids = w.cache.page_table[s, :m].long()
+    return PagedCache.from_code_layout(w.cache.v_codes[ids], w.cache.v_scale[ids]).flatten(0, 1)[:n].double().cpu()
+
+
+def check(w, dirty=()):
+    """Every block's values, but for the (session, block) that tokens were taken
+    from and that nothing was written to since."""
+    for s in range(w.S):
+        n = w.slots[s]
+        assert int(w.cache.n_tokens[s]) == n
+        got, want = stored(w, s), quantise_slots(w.v16[s].flatten(1, 2)).view(n, w.L, w.Hkv, D).double()
+        look = w.live[s].copy()
+        for z, b in dirty:
+            if z == s:
+                look[16 * b:16 * b + 16] = False
+        look = torch.as_tensor(look)
+        assert same(got[look], want.float()[look]), s
+        w.v[s] = got
+
+
+def take(w, s, n):
+    w.cache.take_back(s, n)
+    resize(w, s, int(w.cache.n_tokens[s]))
+
+
+@pytest.mark.parametrize("P,aligned", [(16, False), (64, False), (64, True), (16, True)])
+@pytest.mark.parametrize("steps", [False, True], ids=["rows", "steps"])
+def test_drafts_of_which_some_are_taken_back(steps, P, aligned):
+    print("[drafts]", steps, P, aligned, flush=True)
+    w = World(2, 4, 2, P, [14, 0, 30, 100, 16, 5], seed=231, aligned=aligned, spare=60, extra=60)
+    w.md.observe(0, None)
+    for s in range(w.S):   # (the clock went on without a token)
+        w.cache.clock[s] = len(w.regions[s])
+    dirty = set()
+    for turn in range(1, 25):
+        counts = w.rng.integers(0, 17, w.S)
+        rows = place(w, counts)
+        write(w, rows, 8.0 if turn % 3 == 0 else 1.0)
+        assert w.md.device_status() == 0
+        dirty -= {(s, t // 16) for s, t in zip(np.repeat(np.arange(w.S), counts), rows[3])}
+        check(w, dirty)
+        if counts.sum() and turn % 4 == 1:
+            q = w.normal(int(counts.sum()), w.Hq, D)
+            out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=w.dev)
+            w.md.attend_rows(1, q, out, rows[0], row_slot=rows[1], lse=lse, window=60, sinks=2)
+            check_rows(w, 1, q, out, lse, rows[2], rows[3], window=60, sinks=2, some=range(0, len(q), 5))
+        for s in range(w.S):
+            n = int(w.rng.integers(0, counts[s] + 1))
+            take(w, s, n)
+            if n and w.slots[s]:
+                dirty.add((s, (w.slots[s] - 1) // 16))
+        check(w, dirty)
+        if steps:
+            nk, nv = (w.normal(w.S, w.L, w.Hkv, D, dtype=BF16) for _ in "kv")
+            region = torch.as_tensor(w.rng.integers(0, 7, w.S).astype(np.uint8), device=w.dev)
+            q = w.normal(w.S, w.Hq, D)
+            out, lse = torch.empty_like(q), torch.empty((w.S, w.Hq), device=w.dev)
+            w.md.attend(0, q, out, new_k=nk[:, 0].contiguous(), new_v=nv[:, 0].contiguous(), lse=lse)
+            check_token(w, 0, q, out, lse, nk[:, 0], nv[:, 0])
+            w.md.observe(turn, None, nk, region)
+            w.md.append_values(nv)
+            assert w.md.device_status() == 0
+            for s in range(w.S):
+                resize(w, s, int(w.cache.n_tokens[s]))
+                w.live[s][-1] = True
+                w.k[s][-1], w.v16[s][-1] = nk[s].double().cpu(), nv[s].float().cpu()
+            dirty -= {(s, (w.slots[s] - 1) // 16) for s in range(w.S)}
+            check(w, dirty)
+    assert all(n > 60 for n in w.slots)
+
+
+def test_the_accepted_prefix_stays():
+    """Drafts at slots 14 .. 18 of which the first is accepted: the block goes on
+    with its own tokens, not with those of the block that the drafts reached."""
+    w = World(1, 2, 2, 16, [14], seed=232, spare=4)
+    write(w, place(w, [5]), 16.0)
+    take(w, 0, 4)
+    write(w, place(w, [1]))
+    assert w.md.device_status() == 0 and w.slots[0] == 16
+    check(w)
+    assert w.cache.v_held[0, 0, 0, :3].tolist() == [int(w.cache.page_table[0, 0]), 16, -1]
+    assert same(w.cache.v_open[0, 0].permute(1, 0, 2), w.v16[0][:, 0])
+
+
+def test_a_scale_that_only_tokens_taken_back_raised():
+    """A step's token behind them: the block's scale is that of what is there."""
+    for many in (2, 1):   # taken back to inside the block, and to right behind another token
+        w = World(1, 2, 2, 16, [5], seed=233, spare=4)
+        w.md.observe(0, None)
+        w.cache.clock[0] = 5
+        write(w, place(w, [many]), 64.0)
+        take(w, 0, many)
+        nk, nv = (w.normal(1, 1, 2, D, dtype=BF16) for _ in "kv")
+        w.md.observe(1, None, nk, torch.zeros(1, dtype=torch.uint8, device=w.dev))
+        w.md.append_values(nv)
+        resize(w, 0, 6)
+        w.live[0][-1], w.v16[0][-1] = True, nv[0].float().cpu()
+        check(w)
+        assert bool((w.cache.v_open[0, :, :, 6:] == 0).all())
+
+
+def test_values_that_were_not_finite_and_are_taken_back():
+    w = World(1, 2, 2, 16, [14], seed=234, spare=4)
+    rows = place(w, [2])
+    k = w.normal(2, 2, D, dtype=BF16)
+    w.md.write_rows(0, rows[0], k, torch.full_like(k, math.inf), row_slot=rows[1])
+    assert bool(w.cache.v_scale[int(w.cache.page_table[0, 0])].isnan().all())
+    take(w, 0, 2)
+    write(w, place(w, [1]))
+    check(w)
+
+
+def test_further_back_than_the_open_blocks():
+    """The block is left as it is, and told of; from its first token it goes on."""
+    w = World(1, 2, 2, 16, [14], seed=235, spare=8, extra=8)
+    w.md.observe(0, None)
+    w.cache.clock[0] = 14
+    write(w, place(w, [40]))
+    check(w)
+    take(w, 0, 44)
+    assert w.slots[0] == 10
+    pools = lambda: [x.clone().view(torch.uint8) for x in (w.cache.k_pool, w.cache.v_codes, w.cache.v_scale, w.cache.v_open,
+                                                           w.cache.v_before, w.cache.v_held)]
+    w.cache.place_tokens(0, [1, 1, 1])
+    before = pools()
+    k = w.normal(3, 2, D, dtype=BF16)
+    w.md.write_rows(0, w.i32([0, 3]), k, k, row_slot=w.i32([10, 11, 12]))
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW
+    assert all(torch.equal(a, b) for a, b in zip(before, pools()))
+    w.cache.take_back(0, 3)
+    nk = w.normal(1, 1, 2, D, dtype=BF16)
+    w.md.observe(1, None, nk, torch.zeros(1, dtype=torch.uint8, device=w.dev))
+    before = pools()
+    w.md.append_values(nk)
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW
+    assert all(torch.equal(a, b) for a, b in zip(before, pools()))
+    resize(w, 0, 11)
+    w.live[0][:] = True
+    write(w, (w.i32([0, 11]), w.i32(np.arange(11)), np.array([0, 11]), np.arange(11)))
+    assert w.md.device_status() == 0
+    check(w)
+    write(w, place(w, [7]))
+    assert w.md.device_status() == 0
+    check(w)
+
+
+def test_tokens_left_out_in_the_middle_of_a_block():
+    """In the open block they keep their values, in another the rows do not count."""
+    w = World(1, 2, 2, 16, [40], seed=236, spare=4)
+    rows = lambda slot: (w.i32([0, len(slot)]), w.i32(slot), np.array([0, len(slot)]), np.array(slot))
+    write(w, rows([33, 36, 39]))
+    assert w.md.device_status() == 0
+    check(w)
+    before = w.cache.v_codes.clone(), w.cache.k_pool.clone()
+    k = w.normal(5, 2, D, dtype=BF16)
+    for slot in ([3, 4, 5, 9, 10], [0, 2, 3, 4, 5]):
+        w.md.write_rows(0, w.i32([0, 5]), k, k, row_slot=w.i32(slot))
+        assert w.md.device_status() == B.MD_DEV_BAD_ROW
+        assert torch.equal(before[0], w.cache.v_codes) and torch.equal(before[1].view(torch.uint8), w.cache.k_pool.view(torch.uint8))
+    # a block that begins anew, then one that does not: the first counts
+    slot = list(range(16)) + [20, 21]
+    k = w.normal(18, 2, D, dtype=BF16)
+    w.md.write_rows(0, w.i32([0, 18]), k, k, row_slot=w.i32(slot))
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW
+    w.v16[0][:16, 0] = k[:16].float().cpu()
+    check(w)
+    assert w.cache.v_held[0, 0, 0, 0] == -1   # (what v_open holds is not known now)
+
+
+def test_blocks_of_the_callers_own():
+    """A caller's own open blocks: taken for the block that the rows go on in."""
+    w = World(1, 2, 2, 16, [20], seed=237, spare=4)
+    w.cache.v_open = w.cache.v_open.clone()
+    assert w.cache.v_before is None and w.cache.v_held is None
+    write(w, place(w, [9]))
+    assert w.md.device_status() == 0
+    check(w)
+
+
+def test_a_session_that_begins_anew():
+    """What the open blocks hold of the one before it does not count."""
+    w = World(1, 2, 2, 16, [20], seed=238, spare=4)
+    w.cache.place_session(0, [1] * 20, w.ids[0], budget=20, clock=20)
+    k = w.normal(2, 2, D, dtype=BF16)
+    w.md.write_rows(0, w.i32([0, 2]), k, k)
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW
+    write(w, (w.i32([0, 20]), w.i32(np.arange(20)), np.array([0, 20]), np.arange(20)))
+    assert w.md.device_status() == 0
+    check(w)
+
+
+def test_drafts_captured_and_replayed():
+    """The same graph verifies at every turn: rows of fixed places, -1 where there is none."""
+    side = torch.cuda.Stream()
+    w = World(1, 4, 2, 16, [14, 30], seed=239, spare=30, extra=30, stream=side)
+    n = 6
+    start, slot = w.i32([0, n, 2 * n]), w.i32([-1] * (2 * n))
+    k, v = (torch.zeros((2 * n, 2, D), dtype=BF16, device=w.dev) for _ in "kv")
+    q, out, lse = (torch.zeros(x, device=w.dev) for x in ((2 * n, 4, D), (2 * n, 4, D), (2 * n, 4)))
+
+    def calls():
+        w.md.write_rows(0, start, k, v, row_slot=slot)
+        w.md.attend_rows(0, q, out, start, row_slot=slot, lse=lse)
+
+    torch.cuda.synchronize()
+    calls()   # (nothing is there)
+    torch.cuda.synchronize()
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for turn in range(12):
+        counts = w.rng.integers(1, n + 1, 2)
+        _, _, own, at = place(w, counts)
+        full = np.full(2 * n, -1)
+        for s in range(2):
+            full[s * n:s * n + counts[s]] = at[own[s]:own[s + 1]]
+        slot.copy_(w.i32(full))
+        for x in (k, v, q):
+            x.copy_(w.normal(*x.shape).to(x.dtype))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        w.md.device_status()
+        for r in np.flatnonzero(full >= 0):
+            w.k[r // n][full[r], 0], w.v16[r // n][full[r], 0] = k[r].double().cpu(), v[r].float().cpu()
+        check(w)
+        check_rows(w, 0, q, out, lse, np.array([0, n, 2 * n]), full, some=np.flatnonzero(full >= 0).tolist())
+        assert bool((out[torch.as_tensor(full < 0, device=w.dev)] == 0).all())
+        for s in range(2):
+            take(w, s, int(w.rng.integers(0, counts[s] + 1)))
+
+
+@pytest.mark.parametrize("types", TYPES[:2], ids=["bf16", "f32"])
+def test_verify_then_evict(types):
+    """Drafts, acceptance, a step that observes, scores and evicts, and again."""
+    w = World(1, 4, 2, 16, [90, 40], seed=240, spare=30, extra=30)
+    w.cache.budget.fill_(64)
+    for step in range(12):
+        counts = w.rng.integers(1, 9, 2)
+        rows = place(w, counts)
+        write(w, rows)
+        check(w)
+        q = w.normal(len(rows[3]), 4, D).to(types[0])
+        out, lse = torch.empty_like(q).to(types[1]), torch.empty(q.shape[:2], device=w.dev)
+        w.md.attend_rows(0, q, out, rows[0], row_slot=rows[1], lse=lse)
+        check_rows(w, 0, q, out, lse, rows[2], rows[3])
+        for s in range(2):
+            take(w, s, int(w.rng.integers(0, counts[s])))
+        nk, nv = (w.normal(2, 1, 2, D, dtype=BF16) for _ in "kv")
+        serial = [w.cache.page_serial[s, :int(w.cache.n_pages[s])].tolist() for s in range(2)]
+        w.md.observe(step, w.normal(2, 1, 1, 4, D), nk, torch.ones(2, dtype=torch.uint8, device=w.dev))
+        w.md.append_values(nv)
+        for s in range(2):
+            resize(w, s, int(w.cache.n_tokens[s]))
+            w.live[s][-1] = True
+            w.k[s][-1], w.v16[s][-1] = nk[s].double().cpu(), nv[s].float().cpu()
+            serial[s] = w.cache.page_serial[s, :int(w.cache.n_pages[s])].tolist()
+        w.md.score()
+        w.md.select_compact()
+        assert w.md.device_status() == 0
+        for s in range(2):
+            left = w.cache.page_serial[s, :int(w.cache.n_pages[s])].tolist()
+            keep = np.isin(np.repeat(serial[s], 16)[:w.slots[s]], left)
+            w.k[s], w.v16[s], w.v[s] = (x[s][torch.as_tensor(keep)] for x in (w.k, w.v16, w.v))
+            w.live[s], w.slots[s] = w.live[s][keep], int(keep.sum())
+        check(w)

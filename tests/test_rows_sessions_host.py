@@ -1,0 +1,117 @@
+"""Tokens placed behind a session's last and taken back, on the host: the same
+tables as a session that was placed at once."""
+import os
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_10582_amd import binding as B
+from paper_2607_10582_amd.cache import PagedCache
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+KW = dict(L=2, Hq=2, Hkv=1, d=128, P=16, S=2, max_pages=8, n_phys=20, device="cpu")
+
+
+def region_of(rng, n):
+    return np.repeat(rng.integers(0, 7, n // 3 + 1), rng.integers(1, 7, n // 3 + 1))[:n] if n else np.zeros(0, int)
+
+
+def state(c, s):
+    m = int(c.n_pages[s])
+    ids, n = c.page_table[s, :m].long(), int(c.n_tokens[s])
+    flat = lambda x: x[ids].flatten()[:n].tolist()
+    return (m, n, int(c.n_live[s]), int(c.clock[s]), flat(c.region), flat(c.t_ins), flat(c.t_ref), flat(c.importance),
+            c.page_format[ids].tolist())
+
+
+@pytest.mark.parametrize("aligned", [False, True])
+def test_placed_in_pieces_as_at_once(aligned):
+    for seed in range(40):
+        rng = np.random.default_rng(seed)
+        region = region_of(rng, int(rng.integers(1, 60)))
+        n, cut = len(region), int(rng.integers(0, 61)) % (len(region) + 1)
+        if PagedCache.pages_for(region, 16, aligned) > 8:
+            continue
+        one, two = PagedCache(**KW), PagedCache(**KW)
+        m = PagedCache.pages_for(region, 16, aligned)
+        one.place_session(1, region, list(range(m)), budget=9, clock=n, t_ins=np.arange(1, n + 1), region_aligned=aligned)
+        first = PagedCache.pages_for(region[:cut], 16, aligned)
+        two.place_session(1, region[:cut], list(range(first)), budget=9, clock=cut, t_ins=np.arange(1, cut + 1), region_aligned=aligned)
+        two.set_free_pages(list(range(19, first - 1, -1)))
+        at = two.place_tokens(1, region[cut:], aligned)
+        assert state(one, 1) == state(two, 1), seed
+        assert at.tolist() == PagedCache.positions(region, 16, aligned)[cut:].tolist()
+        assert torch.equal(one.page_table, two.page_table) and torch.equal(one.page_serial, two.page_serial)
+        assert int(two.free_count[0]) == 20 - m and int(two.next_serial[1]) == m
+        # and back to the cut
+        was = PagedCache(**KW)
+        was.place_session(1, region[:cut], list(range(first)), budget=9, clock=cut, t_ins=np.arange(1, cut + 1), region_aligned=aligned)
+        two.take_back(1, n - cut)
+        assert state(was, 1) == state(two, 1), seed
+        assert torch.equal(was.page_table, two.page_table) and int(two.free_count[0]) == 20 - first
+        assert sorted(two.free_list[:20 - first].tolist()) == list(range(first, 20))
+        again = two.place_tokens(1, region[cut:], aligned)
+        assert again.tolist() == at.tolist() and state(one, 1) == state(two, 1)
+
+
+def test_what_is_refused_changes_nothing():
+    c = PagedCache(**KW)
+    c.place_session(0, [1] * 20, [0, 1], budget=20, clock=20)
+    c.set_free_pages([2, 3])
+    names = ["region", "t_ins", "page_table", "page_serial", "n_pages", "n_tokens", "n_live", "clock", "free_count", "free_list"]
+    before = {x: getattr(c, x).clone() for x in names}
+    for call in (lambda: c.place_tokens(0, [1] * 45), lambda: c.take_back(0, 21), lambda: c.take_back(0, -1),
+                 lambda: c.place_tokens(0, [1] * 200)):
+        with pytest.raises(ValueError):
+            call()
+    c.page_format[0] = 1
+    with pytest.raises(ValueError):   # it would go on in a page of 8-bit keys
+        c.take_back(0, 8)
+    assert all(torch.equal(before[x], getattr(c, x)) for x in names)
+    c.take_back(0, 4)                 # which ends it: the next token opens a page
+    assert int(c.n_tokens[0]) == 16 and c.place_tokens(0, []).tolist() == [] and c.place_tokens(0, [2]).tolist() == [16]
+    c.take_back(0, 0)
+    c = PagedCache(**{**KW, "device": "cpu"})
+    c.offload_pages = 1
+    for call in (lambda: c.place_tokens(0, [1]), lambda: c.take_back(0, 1)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_what_the_open_blocks_hold():
+    c = PagedCache(**KW, values="e4m3")
+    assert bool((c.v_held == -1).all())
+    c.load_session(1, torch.randn(37, 2, 1, 128), [0] * 37, [5, 3, 7], budget=37, clock=37)
+    c.load_values(1, torch.randn(37, 2, 1, 128).bfloat16())
+    assert bool((c.v_held[1] == torch.tensor([7, 5, -1, -1])).all()) and bool((c.v_held[0] == -1).all())
+    c.place_session(1, [0] * 20, [5, 3], budget=20, clock=20)
+    assert bool((c.v_held == -1).all())
+    c = PagedCache(**{**KW, "P": 64}, values="e4m3")
+    c.load_session(0, torch.randn(90, 2, 1, 128), [0] * 90, [5, 3], budget=90, clock=90)
+    c.load_values(0, torch.randn(90, 2, 1, 128).bfloat16())
+    assert bool((c.v_held[0] == torch.tensor([3 * 4 + 1, 10, -1, -1])).all())
+    mine = c.v_open.clone()
+    c.v_open = mine
+    assert c.v_open is mine and c.v_held is None and c.v_before is None
+    c.place_session(0, [0] * 20, [5], budget=20, clock=20)   # nothing to note
+
+
+def test_open_blocks_without_a_handle():
+    lib = B.load_library()
+    assert lib.md_open_blocks(None, None, None) == B.MD_E_INVALID
+    assert lib.md_open_blocks(None, 0x1000, 0x1000) == B.MD_E_INVALID
+
+
+def test_open_blocks_arguments_under_sanitizers(tmp_path):
+    exe = tmp_path / "open_args"
+    cmd = ["g++", "-std=c++17", "-g", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", os.path.join(ROOT, "include"),
+           "-fsanitize=address,undefined", "-fno-sanitize-recover=all", os.path.join(ROOT, "tests", "open_args.cpp"),
+           "-Wl,--unresolved-symbols=ignore-in-object-files", "-o", str(exe)]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:halt_on_error=1", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=120)
+    assert r.returncode == 0, r.stdout + r.stderr
+    assert "open blocks passed" in r.stdout
