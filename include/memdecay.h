@@ -116,7 +116,10 @@ enum {
                                 /* got a row_start that does not ascend, a row  */
                                 /* whose slot its session does not hold, or     */
                                 /* (md_write_rows) that is not above the row    */
-                                /* before it or sits in a page of 8-bit keys    */
+                                /* before it, or a key for a page of 8-bit      */
+                                /* keys; or md_write_rows or md_append_codes    */
+                                /* was to go on inside a block that the open    */
+                                /* blocks do not hold (md_open_blocks)          */
 #define MD_DEV_TIMEOUT    0x10  /* a bounded wait between the workgroups of the */
                                 /* fused observation kernel ran out; the step's */
                                 /* attention mass is not valid (the session     */
@@ -770,8 +773,8 @@ md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v
  * among the others (MD_DEV_BAD_ROW).  The slots of the others ascend; where
  * they do not, a row that is not above those before it is left out, and others
  * of its session may be with it (MD_DEV_BAD_ROW; no slot is written twice, and
- * the same rows every time).  A row whose page holds 8-bit keys does not count
- * (MD_DEV_BAD_ROW).
+ * the same rows every time).  A key whose page holds 8-bit keys is left out
+ * (MD_DEV_BAD_ROW), the row's value is written.
  * In the 8-bit pool a session's rows go on in one block after another, without
  * leaving tokens out: the slots of a block behind the last row written to it get
  * the code 0, and one in front of it that is neither among the rows nor known

@@ -5,8 +5,9 @@ import pytest
 import torch
 
 from paper_2607_10582_amd import binding as B
-from rows_world import BF16, D, World
-from test_gpu_rows import check_written, kv_rows, pool_slots
+from paper_2607_10582_amd.cache import PagedCache
+from rows_world import BF16, D, World, quantise_slots
+from test_gpu_rows import check_written, kv_rows, pool_slots, same
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +132,24 @@ def test_a_row_in_front_that_is_not_there_in_the_middle_of_a_block():
                            torch.full((behind, 2, D), 9.0, dtype=BF16, device=w.dev)]) for x in rows)
         w.md.write_rows(0, w.i32([0, len(slot)]), k, v, row_slot=w.i32(slot))
     check_written(w, [0])
+
+
+@pytest.mark.parametrize("coded", [True, False])
+def test_a_key_for_a_page_of_codes_is_left_out_and_its_value_written(coded):
+    w = World(1, 2, 2, 16, [70], seed=216, quant=1.0, coded=coded)
+    keys = w.cache.k_pool.clone()
+    pages = w.cache.page_format.bool()
+    assert int(pages.sum()) == 4
+    k, v = (w.normal(70, 2, D, dtype=BF16) for _ in "kv")
+    w.md.write_rows(0, w.i32([0, 70]), k, v)
+    assert w.md.device_status() == B.MD_DEV_BAD_ROW
+    assert torch.equal(keys[pages].view(torch.uint8), w.cache.k_pool[pages].view(torch.uint8))
+    last = torch.as_tensor(w.ids[0][4:], device=w.dev)
+    assert torch.equal(PagedCache.from_pool_layout(w.cache.k_pool[last])[0, :6, 0], k[64:])
+    want = v.float().cpu()
+    if coded:
+        want = quantise_slots(want).float()
+        assert same(w.cache.v_open[0, 0, :, :6], v[64:].transpose(0, 1))
+    assert same(pool_slots(w, 0)[1][:70, 0], want)
+    w.md.write_rows(0, w.i32([0, 70]), v=v)
+    assert w.md.device_status() == 0
