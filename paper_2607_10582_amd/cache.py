@@ -29,7 +29,9 @@ class PagedCache:
         # values: a pool of values beside the keys (MemDecay.attend), True for
         # bf16 ones, "e4m3" for 8-bit codes with a scale per 16 tokens and KV
         # head; bounds: 8-bit bounds of each page's keys (MemDecay.select_blocks)
-        if values not in (False, True, "e4m3"):
+        if values is None or values in (False, True):
+            values = bool(values)
+        elif values != "e4m3":
             raise ValueError('values are True (bf16), "e4m3" or False')
         self.L, self.Hq, self.Hkv, self.d, self.P = L, Hq, Hkv, d, P
         self.S, self.max_pages, self.n_phys = S, max_pages, n_phys

@@ -115,3 +115,9 @@ def test_open_blocks_arguments_under_sanitizers(tmp_path):
     r = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=120)
     assert r.returncode == 0, r.stdout + r.stderr
     assert "open blocks passed" in r.stdout
+
+
+@pytest.mark.parametrize("values,pool", [(True, True), (1, True), (np.True_, True), (False, False), (0, False), (None, False)])
+def test_values_that_are_true_make_a_pool(values, pool):
+    c = PagedCache(**KW, values=values)
+    assert (c.v_pool is not None) == pool and c.v_codes is None
