@@ -198,12 +198,15 @@ class PagedCache:
         n = int(keys.shape[0])
         if len(region) != n:
             raise ValueError("need one region code per token")
-        ids, posd, m = self.place_session(s, region, page_ids, budget, clock, t_ins, region_aligned)
-        k = keys.to(self.device, torch.bfloat16)
-        full = torch.zeros((m * P,) + tuple(k.shape[1:]), dtype=k.dtype, device=k.device)
-        full[posd] = k
+        # (the keys first, so that a call that is refused leaves the session as it was)
+        pos = self.positions(region, P, region_aligned)
+        m = (int(pos[-1]) + P) // P if n else 0
+        full = torch.zeros((m * P,) + tuple(keys.shape[1:]), dtype=torch.bfloat16, device=self.device)
+        full[torch.as_tensor(pos, device=self.device)] = keys.to(self.device, torch.bfloat16)
         # [m][P][L][Hkv][d] -> [m][L][Hkv][P][d]
-        self.k_pool.index_copy_(0, ids, self.to_pool_layout(full.view(m, P, self.L, self.Hkv, self.d)))
+        pages = self.to_pool_layout(full.view(m, P, self.L, self.Hkv, self.d))
+        ids, _, _ = self.place_session(s, region, page_ids, budget, clock, t_ins, region_aligned)
+        self.k_pool.index_copy_(0, ids, pages)
 
     def place_session(self, s: int, region, page_ids: Sequence[int], budget: int, clock: int, t_ins=None,
                       region_aligned: bool = False):
@@ -218,6 +221,8 @@ class PagedCache:
         m = (n_pos + P - 1) // P
         if len(page_ids) != m or m > self.max_pages:
             raise ValueError("need one page id per page of the layout, within max_pages")
+        if t_ins is not None and len(t_ins) != n:
+            raise ValueError("need one time per token")
         ids = torch.as_tensor(np.asarray(page_ids, dtype=np.int64), device=self.device)
         posd = torch.as_tensor(pos, device=self.device)
         reg = torch.as_tensor(np.asarray(region, dtype=np.uint8), device=self.device)

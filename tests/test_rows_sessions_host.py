@@ -121,3 +121,20 @@ def test_open_blocks_arguments_under_sanitizers(tmp_path):
 def test_values_that_are_true_make_a_pool(values, pool):
     c = PagedCache(**KW, values=values)
     assert (c.v_pool is not None) == pool and c.v_codes is None
+
+
+@pytest.mark.parametrize("how", ["shape", "heads", "region", "pages", "times"])
+def test_a_session_that_is_refused_stays_as_it_was(how):
+    c = PagedCache(**KW, values="e4m3")
+    c.load_session(0, torch.randn(20, 2, 1, 128), [1] * 20, [4, 6], budget=20, clock=20)
+    c.load_values(0, torch.randn(20, 2, 1, 128).bfloat16())
+    names = [x for x, t in vars(c).items() if isinstance(t, torch.Tensor)]
+    before = {x: getattr(c, x).clone() for x in names}
+    args = dict(keys=torch.randn(40, 2, 1, 128), region=[2] * 40, page_ids=[4, 6, 9], budget=40, clock=40)
+    args.update({"shape": dict(keys=torch.randn(40, 2, 1, 64)), "heads": dict(keys=torch.randn(40, 2, 2, 128)),
+                 "region": dict(region=[2] * 39), "pages": dict(page_ids=[4, 6]), "times": dict(t_ins=[1, 2])}[how])
+    with pytest.raises((ValueError, RuntimeError)):
+        c.load_session(0, **args)
+    assert all(torch.equal(before[x].view(torch.uint8), getattr(c, x).view(torch.uint8)) for x in names)
+    c.load_session(0, torch.randn(40, 2, 1, 128), [2] * 40, [4, 6, 9], budget=40, clock=40)
+    assert int(c.n_tokens[0]) == 40
