@@ -827,7 +827,10 @@ md_status md_attend_values(md_handle h, int32_t layer, const md_attend_args* a, 
  * products of bf16 queries, and softmax weights rounded to bf16 once, whose
  * sum is that of the rounded ones.  Else queries and weights enter the
  * products as three bf16 terms, as in md_attend_token.  A row without any
- * token gets zeros and lse = -infinity.  The same inputs give the same bits.
+ * token, or whose slot is not there, gets zeros and lse = -infinity.  Values
+ * that are not finite reach the rows that see them alone: a NaN its dimension, an
+ * infinity too (as an infinity of its sign or, where weights are three terms, as
+ * NaN).  The same inputs give the same bits.
  * MD_E_UNSUPPORTED with an offload tier, and where n_rows Hq / Hkv + 256 S
  * comes to 2^31.
  */

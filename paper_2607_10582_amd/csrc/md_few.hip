@@ -311,13 +311,17 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
             for (int i = 0; i < 16; ++i) z = fmaf(o[d][i], 0.0f, z);
         z = add_halves(z);
         uint32_t bad = (uint32_t)__ballot(col.own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
+        auto blocks = [&](int i) __attribute__((always_inline)) { return describe(i >> 1); };
+        if (bad != 0 && !reached_unseen<V8>(c, seen, smin, smax, 2 * count, blocks)) bad = 0;
         float* const y_lds = reinterpret_cast<float*>(v_lds);
         while (bad != 0) {
             const int who = __ffs(bad) - 1;
             bad &= bad - 1;
             const float2 y = column_again<QT, V8>(
                 c, seen, lane_int(col.own, who), lane_float(__float_as_int(m), who), t.row_lo + (t.col + who) / c.G,
-                lane_int(col.head, who), 2 * count, [&](int i) { return describe(i >> 1); });
+                lane_int(col.head, who), 2 * count, y_lds, blocks);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
             y_lds[2 * lane] = y.x;
             y_lds[2 * lane + 1] = y.y;
             asm volatile("" ::: "memory");

@@ -313,14 +313,69 @@ __device__ __forceinline__ int64_t lane_tile(const Block& b, int i) {
 // values with another (or none: NaN) is summed again.
 __device__ __forceinline__ bool scale_fits(float s) { return s > 0x1p-96f && s < 0x1p96f; }
 
-// One column's sum of weighted values again, token by token (dims e and e + 1,
-// e = 2 lane), from `count` blocks of which describe(k) tells 64 lanes: for
-// values that are not finite, which reach, as 0 times them, the columns of their
-// product that do not see them.
+// Whether some column of the wave may hold what it does not see: a value that is
+// not finite in a block that not every column sees in full, which reaches the
+// others as 0 times it, or a scale that does not fit, which every column that sees
+// it lacks.  A column without either that is not finite sees a value that is not,
+// and stays.  (Telling costs a look at the blocks that some column does not see in
+// full; without it every column that sees such a value would be summed again.
+// 2,048 rows of 16 heads take 75 us, with a NaN in the first token 93; in the last
+// but eight 2,960, where one workgroup's columns are summed again.)  describe(i): what lanes know of blocks i .. i + 63 of the wave's `count`.
+template <bool V8, typename F>
+__device__ __forceinline__ bool reached_unseen(const PromptCall& c, const Seen& x, int smin, int smax, int count, F&& describe) {
+    for (int i = 0; i < count; i += 64) {
+        const Block b = describe(i);
+        const bool mine = i + lane_id() < count && b.live > 0;
+        if constexpr (V8) {
+            const float vs = __int_as_float(b.vs);
+            if (__any(mine && vs == vs && vs != 0.0f && !scale_fits(vs))) return true;
+        }
+        const bool full = (b.live == 16) & (b.at + 15 <= smin) & ((b.at > smax - x.win) | (b.at + 15 < c.sinks));
+        for (uint64_t left = __ballot(mine && !full); left != 0; left &= left - 1) {
+            const int k = __ffsll((unsigned long long)left) - 1;
+            const int64_t tile = lane_tile(b, k);
+            const int k4 = lane_int(b.live, k) - 4 * (lane_id() >> 4);   // tokens of this lane's four that there are
+            bool odd = false;
+            if constexpr (V8) {
+                const uint32_t there = k4 >= 4 ? ~0u : k4 <= 0 ? 0u : (1u << (8 * k4)) - 1u;
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(c.v_codes + tile + 1024 * a + 16 * lane_id());
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // a byte of 0x7F or 0xFF
+                        const uint32_t y = ~(w[e] | 0x80808080u) | ~there;
+                        odd |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+                    }
+                }
+            } else {
+                const uint32_t m0 = k4 >= 2 ? ~0u : k4 == 1 ? 0xFFFFu : 0u, m1 = k4 >= 4 ? ~0u : k4 == 3 ? 0xFFFFu : 0u;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(c.v_pool + tile + 512 * a + 8 * lane_id());
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t y = w[e] & (e & 1 ? m1 : m0);
+                        odd |= (y & 0x7F80u) == 0x7F80u || (y & 0x7F800000u) == 0x7F800000u;
+                    }
+                }
+            }
+            if (__any(odd)) return true;
+        }
+    }
+    return false;
+}
+
+constexpr int kAgainWords = kHeadDim + 64;   // of column_again's LDS
+
+// One column's sum of weighted values again (dims e and e + 1, e = 2 lane), from
+// `count` blocks of which describe(k) tells 64 lanes, 64 tokens at a time: a
+// lane's token's weight, then all tokens' values for its dims.  For values that
+// are not finite, which reach, as 0 times them, the columns of their product that
+// do not see them.  lds: the wave's own.
 template <bool QT, bool V8, typename F>
 __device__ __forceinline__ float2 column_again(const PromptCall& c, const Seen& x, int own, float top, int64_t row, int head,
-                                               int count, F&& describe) {
-    const int e = 2 * lane_id();
+                                               int count, float* lds, F&& describe) {
+    const int lane = lane_id(), e = 2 * lane;
     const int64_t at_q = row * c.q_stride + head * kHeadDim + e;
     float q0, q1, y0 = 0.0f, y1 = 0.0f;
     if (c.q_f32) {
@@ -331,32 +386,74 @@ __device__ __forceinline__ float2 column_again(const PromptCall& c, const Seen& 
         q0 = bf16_lo(w);
         q1 = bf16_hi(w);
     }
+    lds[e] = q0;
+    lds[e + 1] = q1;
+    float* const weight = lds + kHeadDim;
     Block b{};
-    for (int i = 0; i < count; ++i) {
+    for (int i = 0; i < count; i += 4) {
         if ((i & 63) == 0) b = describe(i);
-        const int at = lane_int(b.at, i & 63), live = lane_int(b.live, i & 63);
-        const int64_t tile = lane_tile(b, i & 63);
-        const bool coded = QT && lane_int(b.coded, i & 63) != 0;
-        const float ks = lane_float(b.ks, i & 63), vs = lane_float(b.vs, i & 63);
-        for (int t = 0; t < live; ++t) {
-            if (at + t > own || (at + t <= own - x.win && at + t >= c.sinks)) continue;
-            uint32_t kw;
-            if (coded)
-                kw = codes_pair_to_bf16<false>(*reinterpret_cast<const uint16_t*>(
-                    reinterpret_cast<const uint8_t*>(c.k_pool + tile) + 1024 * (e / 64) + 16 * (t + 16 * ((e / 8) % 4)) +
-                    8 * ((e / 32) % 2) + e % 8));
-            else
-                kw = *reinterpret_cast<const uint32_t*>(c.k_pool + tile + (e / 8) * 128 + t * 8 + e % 8);
-            const float w = hw_exp2(wave_sum(fmaf(q0, bf16_lo(kw), q1 * bf16_hi(kw))) * ks * kLogitScale - top);
-            if constexpr (V8) {
-                const uint8_t* v = c.v_codes + tile + (e / 64) * 1024 + (t / 4) * 256 + (e % 16) * 16 + ((e / 16) % 4) * 4 + t % 4;
-                const uint32_t pair = codes_pair_to_bf16<false>((uint32_t)v[0] | ((uint32_t)v[16] << 8));
-                y0 = fmaf(w, vs * bf16_lo(pair), y0);
-                y1 = fmaf(w, vs * bf16_hi(pair), y1);
-            } else {
-                const uint16_t* v = c.v_pool + tile + (e / 32) * 512 + (t / 4) * 128 + (e % 16) * 8 + ((e / 16) % 2) * 4 + t % 4;
-                y0 = fmaf(w, bf16_lo(v[0]), y0);
-                y1 = fmaf(w, bf16_lo(v[8]), y1);
+        // ---- lane 16 k + t: token t of block i + k
+        const int k = lane >> 4, t = lane & 15, of = (i & 63) + k;
+        const int at = __shfl(b.at, of) + t, all = __shfl(b.live, of), live = i + k < count ? all : 0;
+        const int64_t tile = (int64_t)((uint64_t)(uint32_t)__shfl((int)(uint32_t)b.tile, of) |
+                                       ((uint64_t)(uint32_t)__shfl((int)(b.tile >> 32), of) << 32));
+        const int coded_of = __shfl(b.coded, of);
+        const bool coded = QT && coded_of != 0;
+        const float ks = QT ? __int_as_float(__shfl(b.ks, of)) : 1.0f;
+        const bool sees = t < live && at <= own && (at > own - x.win || at < c.sinks);
+        const uint64_t seen = __ballot(sees);
+        if (seen == 0) continue;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        float dot = 0.0f;
+        if (sees) {
+#pragma unroll 8
+            for (int j = 0; j < 16; ++j) {   // dims 8 j ..
+                u32x4 w;
+                if (coded) {   // codes (a, g, t): dims 64 a + 8 g .. and 64 a + 32 + 8 g ..
+                    const u32x4 z = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(c.k_pool + tile) +
+                                                                    1024 * (j >> 3) + 16 * (t + 16 * (j & 3)));
+                    w = j & 4 ? codes_to_bf16<1>(z) : codes_to_bf16<0>(z);
+                } else {
+                    w = *reinterpret_cast<const u32x4*>(c.k_pool + tile + 128 * j + 8 * t);
+                }
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                    dot = fmaf(lds[8 * j + 2 * z], bf16_lo(w[z]), fmaf(lds[8 * j + 2 * z + 1], bf16_hi(w[z]), dot));
+            }
+        }
+        weight[lane] = sees ? hw_exp2(dot * ks * kLogitScale - top) : 0.0f;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        // ---- this lane's dims of the blocks' tokens, four at a time
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t mask = (uint32_t)(seen >> (16 * k)) & 0xFFFFu;
+            if (mask == 0) continue;
+            const int64_t tile = lane_tile(b, (i & 63) + k);
+            const float vs = V8 ? lane_float(b.vs, (i & 63) + k) : 1.0f;
+            u32x2 v0[4], v1[4];   // bf16 values of tokens 4 g .. of dims e and e + 1
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if constexpr (V8) {
+                    const uint8_t* v = c.v_codes + tile + (e / 64) * 1024 + g * 256 + (e % 16) * 16 + ((e / 16) % 4) * 4;
+                    const uint32_t a = *reinterpret_cast<const uint32_t*>(v), z = *reinterpret_cast<const uint32_t*>(v + 16);
+                    v0[g] = u32x2{codes_pair_to_bf16<false>(a), codes_pair_to_bf16<true>(a)};
+                    v1[g] = u32x2{codes_pair_to_bf16<false>(z), codes_pair_to_bf16<true>(z)};
+                } else {
+                    const uint16_t* v = c.v_pool + tile + (e / 32) * 512 + g * 128 + (e % 16) * 8 + ((e / 16) % 2) * 4;
+                    v0[g] = *reinterpret_cast<const u32x2*>(v);
+                    v1[g] = *reinterpret_cast<const u32x2*>(v + 8);
+                }
+            }
+#pragma unroll
+            for (int z = 0; z < 16; ++z) {
+                const float w = weight[16 * k + z];
+                const uint32_t a = v0[z >> 2][(z >> 1) & 1], d = v1[z >> 2][(z >> 1) & 1];
+                const float n0 = fmaf(w, vs * (z & 1 ? bf16_hi(a) : bf16_lo(a)), y0);
+                const float n1 = fmaf(w, vs * (z & 1 ? bf16_hi(d) : bf16_lo(d)), y1);
+                const bool counts = (mask >> z) & 1u;
+                y0 = counts ? n0 : y0;
+                y1 = counts ? n1 : y1;
             }
         }
     }

@@ -486,14 +486,20 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W /
             for (int i = 0; i < 16; ++i) z = fmaf(o[d][i], 0.0f, z);
         z = add_halves(z);
         uint32_t bad = (uint32_t)__ballot(own >= 0 && l * 0.0f == 0.0f && z != 0.0f);
-        float* const y_lds = reinterpret_cast<float*>(kl[0]) + kHeadDim * wv;
+        auto blocks = [&](int i) __attribute__((always_inline)) {
+            return describe(4 * begin + i, page_of(c, t, seen, 4 * begin + i + lane));
+        };
+        const int count = min(seen.n_blocks, 4 * end) - 4 * begin;
+        if (bad != 0 && !reached_unseen<V8>(c, seen, smin, smax, count, blocks)) bad = 0;
+        float* const y_lds = reinterpret_cast<float*>(kl[0]) + kAgainWords * wv;
         while (bad != 0) {
             const int who = __ffs(bad) - 1;
             bad &= bad - 1;
             const float2 y = column_again<QT, V8>(
                 c, seen, of(own, who), lane_float(__float_as_int(m), who), t.row_lo + (t.col + wv * 32 + who) / c.G,
-                of(head, who), min(seen.n_blocks, 4 * end) - 4 * begin,
-                [&](int i) { return describe(4 * begin + i, page_of(c, t, seen, 4 * begin + i + lane)); });
+                of(head, who), count, y_lds, blocks);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
             y_lds[2 * lane] = y.x;
             y_lds[2 * lane + 1] = y.y;
             asm volatile("" ::: "memory");
