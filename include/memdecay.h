@@ -647,7 +647,8 @@ md_status md_attend_token(md_handle h, int32_t layer, const md_attend_args* a);
  *   the token) and, with the quantised tier, the pages that this handle's
  *   md_compact or md_select_compact has turned into codes since its last
  *   md_key_bounds.  Behind the compaction it finds them at once; before it,
- *   at the next step's call.  A session's pages are taken one after another:
+ *   at the next step's call.  Keys that md_write_rows has written since are
+ *   not looked for: 1 after it.  A session's pages are taken one after another:
  *   where a compaction converts most of a cache, 1 is faster.  A handle keeps
  *   one pair of arrays up to date (another pair: 1 first).
  * The keys of a page that holds 8-bit codes are the float32 products of scale
@@ -779,6 +780,7 @@ md_status md_append_codes(md_handle h, const uint16_t* new_v, const md_values* v
  * leaving tokens out: the slots of a block behind the last row written to it get
  * the code 0, and one in front of it that is neither among the rows nor known
  * from before makes the block's rows not count (MD_DEV_BAD_ROW).
+ * Bounds of the pages' keys (md_key_bounds) are not kept up with them.
  * MD_E_UNSUPPORTED with an offload tier.
  */
 typedef struct md_write_args {
@@ -810,9 +812,12 @@ md_status md_read_rows(md_handle h, int32_t layer, const md_read_args* a);
  * md_attend_values — md_attend_token over values in either form, all of the
  * cache or a window of it: with window > 0 the token at slot p (the slot
  * behind the session's last, or without new_k the last one) sees the slots
- * j <= p with p - j < window or j < sinks.  a's own v_pool is not looked at;
- * everything else as for md_attend_token.  MD_E_UNSUPPORTED for a window
- * with lists of blocks.
+ * j <= p with p - j < window or j < sinks.  Both count slots of the cache as it
+ * stands, holes among them, not positions in the text: once pages have been
+ * evicted a window reaches further back in it, and the sinks are the slots
+ * that are first then (pin their region to keep a prompt's own).  a's own
+ * v_pool is not looked at; everything else as for md_attend_token.
+ * MD_E_UNSUPPORTED for a window with lists of blocks.
  */
 md_status md_attend_values(md_handle h, int32_t layer, const md_attend_args* a, const md_values* v, int32_t window,
                            int32_t sinks);
@@ -821,7 +826,7 @@ md_status md_attend_values(md_handle h, int32_t layer, const md_attend_args* a, 
  * md_attend_rows — attention of ragged rows in one layer over their sessions'
  * cached tokens, their own among them (md_write_rows comes first): the row at
  * slot p sees the tokens at slots j <= p, with window > 0 those of them with
- * p - j < window or j < sinks.
+ * p - j < window or j < sinks (slots, as for md_attend_values).
  *   out_h = sum_i softmax_i(q_h . k_i / sqrt(d)) v_i,  lse_h = ln sum_i exp(q_h . k_i / sqrt(d))
  * Logits, statistics and sums are float32.  bf16 queries with bf16 outputs:
  * products of bf16 queries, and softmax weights rounded to bf16 once, whose

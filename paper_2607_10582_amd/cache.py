@@ -589,9 +589,11 @@ class MemDecay:
                    v: Optional[torch.Tensor] = None, *, row_slot: Optional[torch.Tensor] = None):
         """Keys and values bf16 [n][Hkv][d] (rows any distance apart) of one
         layer into the pools, values as codes in a cache of 8-bit values.  A
-        session's slots ascend, and its rows are written in order.  Keys of
-        pages that hold 8-bit keys are left alone.  Runs on the handle's
-        stream, whatever stream is current.
+        session's slots ascend, and its rows are written in order; rows whose
+        slot is not there (-1) may lie among them.  Keys of pages that hold
+        8-bit keys are left alone.  Page bounds do not follow: behind it
+        update_bounds(True).  k and v have rows the same distance apart.  Runs
+        on the handle's stream, whatever stream is current.
 
         Of tokens to verify (PagedCache.place_tokens) the last ones may leave
         again (PagedCache.take_back): with 8-bit values rows and steps then go on
@@ -622,7 +624,8 @@ class MemDecay:
                     lse: Optional[torch.Tensor] = None):
         """Attention of rows [n][Hq][d] over their sessions' cached tokens up to
         their own (write_rows comes first); with window > 0 over those less
-        than ``window`` slots back and the first ``sinks``.  q and out float32
+        than ``window`` slots back and the first ``sinks`` slots (of the cache
+        as it stands, as in attend).  q and out float32
         or bfloat16, rows any distance apart, lse float32 [n][Hq].  bf16 q and
         out take the faster products; float32 on either side the exact ones.
         Runs on the handle's stream, whatever stream is current, in a work
@@ -662,7 +665,9 @@ class MemDecay:
         space, so captured calls of it are not replayed at the same time.
         With window > 0 the token (the slot behind the session's last, or
         without new_k the last one) sees the slots less than ``window`` back
-        and the first ``sinks`` ones; not together with blocks."""
+        and the first ``sinks`` ones; not together with blocks.  Slots are those
+        of the cache as it stands, holes among them: behind an eviction a window
+        reaches further back in the text, and other slots are the first."""
         c, dev = self.cache, self._device
         S = c.S
         q_at, q_pitch = _rows(q, torch.float32, S, c.Hq, c.d, dev)
@@ -706,7 +711,7 @@ class MemDecay:
         """Bounds of the keys, once per step behind its compaction: of each
         session's last page and, with the quantised tier, of the pages that
         became codes since the last call; or of every page (after the prompts
-        are loaded; also faster where most of a cache has become codes).
+        are loaded, and behind write_rows; also faster where most of a cache has become codes).
         Runs on the handle's stream, whatever stream is current."""
         B.md_key_bounds(self.handle, int(all_pages), *self._bounds())
 
