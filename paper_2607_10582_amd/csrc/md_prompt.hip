@@ -14,13 +14,12 @@
 //          feeds tokens 4h .. 4h+3 and 8+4h .. 8+4h+3 of a block, the very
 //          weights it has, so they never leave their registers
 // Keys and values lie in LDS in the order of the products' operands, 16 bytes a
-// lane side by side, which leaves no bank conflicts (in the order of the pools
-// 36% of the LDS's cycles were conflicts).
+// lane side by side, which leaves 9% of the LDS's cycles to bank conflicts (in the
+// order of the pools they were 36%).
 //
-// What bounds it: the matrix cores, 4 d operations per column and token.  They
-// are busy for 84% of the time that a large library product takes for as many
-// operations: a prompt of 16,384 rows (16 query heads on 2) takes 1.08 ms,
-// 1,020 TFLOP/s.  Without the weights it would take 0.89 ms, without the loads
+// What bounds it: the matrix cores, 4 d operations per column and token.  A
+// large library product does as many operations in 84% of the time: a prompt of
+// 16,384 rows (16 query heads on 2) takes 1.08 ms, 1,020 TFLOP/s.  Without the weights it would take 0.89 ms, without the loads
 // 1.02.
 
 #include <algorithm>
@@ -569,7 +568,9 @@ constexpr int kWideCols = kWideWaves * 32;   // columns of its tile
 // 6,144 200 / 156; 8,192 tokens, 8 KV heads, 2,048 columns 111 / 118,
 // 8,192 384 / 284.  (Only the device knows the rows of each session: a long prompt
 // beside many sessions without a row is taken for few rows of each, 942 for 700
-// us with 8,192 rows of it.)
+// us with 8,192 rows of it.)  Between 144 and 288 columns a session the narrow
+// kernel still is the faster one in three of the four, and by far the slower one
+// in the fourth, of many short sessions: the limit is where that one turns.
 constexpr int kFewCols = 128, kFewAll = 2048;
 // Parts that the tiles of a call may come to, and their arrivals' words.
 int most_parts(int n_cu) { return n_cu * (kWideCols / kFewTile); }

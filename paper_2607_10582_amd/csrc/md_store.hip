@@ -5,10 +5,11 @@
 //
 // Each moves a value once and turns it by a few operations, so long calls are
 // bound by HBM, and a decode step's by the launch and its chain of loads
-// (sessions' bounds, slot, page, bytes).  Rows in: 4 x 8,192 of two KV heads, 13.8
-// us, 4.2 TB/s of reads and writes; 64 uneven chunks, 14.  Rows out: 16 x 32,768
-// into float32, 311 us, 4.4 TB/s (a copy of 4 GiB runs at 4.8); 32 x 1,700, 25.9
-// us.  The values of a decode step of 32 sessions, 36 layers: 6.0 us from Python.
+// (sessions' bounds, slot, page, bytes).  Rows in: 4 x 8,192 of two KV heads, 14.2
+// us, 4.1 TB/s of reads and writes (14.8 where the open blocks are kept); 64 uneven
+// chunks, 14.4.  Rows out: 16 x 32,768 into float32, 311 us, 4.4 TB/s (a copy of 4
+// GiB runs at 4.8); 32 x 1,700, 26.8 us, 20.4 in a graph of such calls.  The values
+// of a decode step of 32 sessions, 36 layers: 5.8 us from Python, 5.0 in a graph.
 
 #include "md_decode.h"
 #include "md_device.h"
