@@ -428,6 +428,8 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
                 if (held_at != nullptr && alone) {
                     if (held.x == id) {
                         now = held;
+                    } else if (o == 0 && block > 0 && held.z >= 0 && held.z == uni(id_of(16 * block - 1))) {
+                        now = held;   // (the open one was taken back whole)
                     } else if (o == 0 && held.x >= 0) {   // a new block: the open one becomes the one before it
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
@@ -693,11 +695,16 @@ __global__ void __launch_bounds__(64 * kWaves) k_append_codes(Dims dm, View v, c
             if (lane == 0) atomicOr(status, MD_DEV_BAD_ROW);
             return;
         } else {              // a new block: the open one becomes the one before it
-            now.z = held.x;
-            now.w = held.y;
-            if (held.x >= 0) {
+            int front = -1;   // (unless it was taken back whole)
+            if (slot > 0) front = id - 1;
+            else if (np > 1) front = v.page_table[(size_t)s * dm.MP + np - 2] * (dm.P >> 4) + (dm.P >> 4) - 1;
+            if (held.z < 0 || held.z != front) {
+                now.z = held.x;
+                now.w = held.y;
+                if (held.x >= 0) {
 #pragma unroll
-                for (int t = 0; t < 16; ++t) before[t * (kHeadDim / 2)] = open[t * (kHeadDim / 2)];
+                    for (int t = 0; t < 16; ++t) before[t * (kHeadDim / 2)] = open[t * (kHeadDim / 2)];
+                }
             }
         }
         if (lane == 0) *held_at = now;

@@ -212,6 +212,36 @@ def test_further_back_than_the_open_blocks():
     check(w)
 
 
+@pytest.mark.parametrize("step", [False, True])
+@pytest.mark.parametrize("P", [16, 64])
+def test_a_block_of_drafts_that_all_fail(P, step):
+    """The next ones begin it again, on another page: the block before it is the
+    one in front of it, not that of the drafts."""
+    w = World(1, 2, 2, P, [P, 3], seed=241, spare=8, extra=8)
+    w.md.observe(0, None)
+    w.cache.clock[0], w.cache.clock[1] = P, 3
+    write(w, place(w, [3, 0]))
+    page = int(w.cache.page_table[0, 1])
+    take(w, 0, 3)
+    write(w, place(w, [0, P]))     # takes that page
+    assert int(w.cache.page_table[1, 1]) == page
+    if step:
+        nk, nv = (w.normal(2, 1, 2, D, dtype=BF16) for _ in "kv")
+        w.md.observe(1, None, nk, torch.zeros(2, dtype=torch.uint8, device=w.dev))
+        w.md.append_values(nv)
+        for s in range(2):
+            resize(w, s, int(w.cache.n_tokens[s]))
+            w.live[s][-1], w.v16[s][-1] = True, nv[s].float().cpu()
+    else:
+        write(w, place(w, [1, 0]))
+    assert int(w.cache.page_table[0, 1]) != page
+    check(w)
+    take(w, 0, 3)                  # two of the block in front of it
+    write(w, place(w, [1, 0]))
+    assert w.md.device_status() == 0
+    check(w)
+
+
 def test_tokens_left_out_in_the_middle_of_a_block():
     """In the open block they keep their values, in another the rows do not count."""
     w = World(1, 2, 2, 16, [40], seed=236, spare=4)
